@@ -57,8 +57,11 @@ enum { POSS_K_OTHER = 0, POSS_K_GATHER_X = 1, POSS_K_EMBED_ROWS = 2, POSS_K_RMSN
        POSS_K_SILU_MUL = 13, POSS_K_CAST = 14, POSS_K_GEMM_SIMT = 15, POSS_K_TOPK_PARTIAL = 16, POSS_K_TOPK_MERGE =
        17, POSS_K_TOPK_MERGE_EXPAND = 18, POSS_K_ARGMAX_PARTIAL = 19, POSS_K_RERANK = 20, POSS_K_ACCEPT_WALK = 21,
        POSS_K_SAMPLE_WALK = 22, POSS_K_KV_COMPACT = 23, POSS_K_CHAIN_MASK = 24, POSS_K_TILE_CONTRIB = 25,
+       POSS_K_PAGED_ATTN = 26, POSS_K_PAGED_ATTN_COMBINE = 27, POSS_K_PAGES_APPEND = 28, POSS_K_PAGES_COMPACT = 29,
+       POSS_K_PAGES_REMAP = 30, POSS_K_PAGES_COPY = 31,
        POSS_K_GEMM_FC = 32, POSS_K_GEMM_QKV = 33, POSS_K_GEMM_O = 34, POSS_K_GEMM_GATE_UP = 35, POSS_K_GEMM_DOWN =
-       36,        POSS_K_GEMM_LM_HEAD = 37, POSS_K_GEMM_OTHER = 38, POSS_K_COUNT = 39 };
+       36,        POSS_K_GEMM_LM_HEAD = 37, POSS_K_GEMM_OTHER = 38, POSS_K_BEAM_LISTS = 39,
+       POSS_K_BEAM_MERGE = 40, POSS_K_COUNT = 41 };
 POSS_API int poss_timeline_read(poss_ctx* ctx, int capacity, int32_t* h_kernel, int64_t* h_time_ns, int* h_count,
                        poss_stream stream);
 
@@ -80,6 +83,13 @@ POSS_API int poss_debug_lose_load(poss_ctx* ctx, int launches);
  * Takes effect from the next call on this context.  Errors: INVALID. */
 enum { POSS_OPT_ATTENTION_TCGEN05 = 0, POSS_OPT_SWIGLU_IN_KERNEL = 1 };
 POSS_API int poss_debug_option(poss_ctx* ctx, int option, int value);
+
+/* Host-only query (no device is touched): where the paged kernels look for a slot of a sequence whose table h_table
+ * (HOST, int32[max_pages]) is given: *h_page = the page, -1 where there is none to follow (a slot behind the table, a
+ * negative entry, an entry >= n_pages), *h_offset = the slot inside it.  Errors: INVALID (NULL, max_pages, page_slots
+ * or n_pages < 1). */
+POSS_API int poss_debug_page_of_slot(const int32_t* h_table, int max_pages, int page_slots, int n_pages, int64_t slot,
+                            int* h_page, int* h_offset);
 
 /* Number of kernels this context has launched so far (host counter). */
 POSS_API int64_t poss_launch_count(const poss_ctx* ctx);

@@ -23,6 +23,8 @@ KERNEL_NAMES = {0: "other", 1: "gather_x", 2: "embed_rows", 3: "rmsnorm", 4: "re
                 11: "splitk_reduce", 12: "splitk_swiglu", 13: "silu_mul", 14: "cast", 15: "gemm_simt",
                 16: "topk_partial", 17: "topk_merge", 18: "topk_merge_expand", 19: "argmax_partial", 20: "rerank",
                 21: "accept_walk", 22: "sample_walk", 23: "kv_compact", 24: "chain_mask", 25: "tile_contrib",
+                26: "paged_attn", 27: "paged_attn_combine", 28: "pages_append", 29: "pages_compact",
+                30: "pages_remap", 31: "pages_copy", 39: "beam_lists", 40: "beam_merge",
                 32: "gemm_fc", 33: "gemm_qkv", 34: "gemm_o", 35: "gemm_gate_up", 36: "gemm_down", 37: "gemm_lm_head",
                 38: "gemm_other"}
 STATUS = {0: "POSS_OK", 1: "POSS_E_INVALID", 2: "POSS_E_SHAPE", 3: "POSS_E_CAPACITY", 4: "POSS_E_WORKSPACE",
@@ -52,6 +54,10 @@ class poss_layer_w(C.Structure):
 class poss_weights(C.Structure):
     _fields_ = [("embed", C.c_void_p), ("lm_head", C.c_void_p), ("target_final_norm", C.c_void_p),
                 ("h_specialist", C.POINTER(poss_layer_w)), ("h_target", C.POINTER(poss_layer_w))]
+
+
+class poss_page_pool(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("n_layers", "n_pages", "n_kv_heads", "page_slots", "head_dim", "dtype")]
 
 
 EXPORTS = {
@@ -96,6 +102,22 @@ EXPORTS = {
     "poss_debug_option": (C.c_int, [C.c_void_p, C.c_int, C.c_int]),
     "poss_tree_attention_noalloc": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int,
                                               C.c_int, C.c_int, C.c_void_p, C.c_float, C.c_void_p, C.c_void_p]),
+    "poss_pages_append": (C.c_int, [C.POINTER(poss_page_pool), C.c_int, C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int,
+                                    C.c_void_p, C.c_void_p, C.c_int64] + [C.c_void_p] * 4),
+    "poss_paged_attention_workspace_bytes": (C.c_size_t, [C.POINTER(poss_page_pool)] + [C.c_int] * 4),
+    "poss_paged_tree_attention": (C.c_int, [C.POINTER(poss_page_pool), C.c_int, C.c_void_p, C.c_void_p] + [C.c_int] * 4 +
+                                  [C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_float, C.c_void_p,
+                                   C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]),
+    "poss_pages_compact": (C.c_int, [C.POINTER(poss_page_pool), C.c_void_p, C.c_void_p, C.c_int, C.c_int] +
+                           [C.c_void_p] * 6),
+    "poss_pages_remap_workspace_bytes": (C.c_size_t, [C.POINTER(poss_page_pool)] + [C.c_int] * 3),
+    "poss_pages_remap": (C.c_int, [C.POINTER(poss_page_pool)] + [C.c_void_p] * 3 + [C.c_int] * 3 + [C.c_void_p] * 8 +
+                         [C.c_size_t, C.c_void_p, C.c_void_p]),
+    "poss_beam_select_workspace_bytes": (C.c_size_t, [C.c_int] * 3),
+    "poss_beam_select": (C.c_int, [C.c_void_p] + [C.c_int] * 4 + [C.c_void_p, C.c_void_p, C.c_int] + [C.c_void_p] * 5 +
+                         [C.c_size_t, C.c_void_p]),
+    "poss_debug_page_of_slot": (C.c_int, [C.POINTER(C.c_int32), C.c_int, C.c_int, C.c_int, C.c_int64,
+                                          C.POINTER(C.c_int), C.POINTER(C.c_int)]),
 }
 
 _lib = None
