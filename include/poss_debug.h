@@ -91,6 +91,11 @@ POSS_API int poss_debug_option(poss_ctx* ctx, int option, int value);
 POSS_API int poss_debug_page_of_slot(const int32_t* h_table, int max_pages, int page_slots, int n_pages, int64_t slot,
                             int* h_page, int* h_offset);
 
+/* The failure-detection hook of poss_paged_tree_attention (as poss_debug_lose_load): the next `launches` tensor-core
+ * launches of the process withhold their value tiles, the bounded wait runs out after about a second, the call's status
+ * word becomes POSS_E_TIMEOUT and its output is undefined. */
+POSS_API int poss_debug_paged_lose_load(int launches);
+
 /* Number of kernels this context has launched so far (host counter). */
 POSS_API int64_t poss_launch_count(const poss_ctx* ctx);
 

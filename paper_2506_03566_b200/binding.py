@@ -116,6 +116,7 @@ EXPORTS = {
     "poss_beam_select_workspace_bytes": (C.c_size_t, [C.c_int] * 3),
     "poss_beam_select": (C.c_int, [C.c_void_p] + [C.c_int] * 4 + [C.c_void_p, C.c_void_p, C.c_int] + [C.c_void_p] * 5 +
                          [C.c_size_t, C.c_void_p]),
+    "poss_debug_paged_lose_load": (C.c_int, [C.c_int]),
     "poss_debug_page_of_slot": (C.c_int, [C.POINTER(C.c_int32), C.c_int, C.c_int, C.c_int, C.c_int64,
                                           C.POINTER(C.c_int), C.POINTER(C.c_int)]),
 }

@@ -285,6 +285,19 @@ def test_captured_attention_replays_with_new_lengths_tables_and_contents(dtype, 
     a.check(a.o)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+def test_a_wait_that_runs_out_is_reported_and_the_next_call_is_sound(d):
+    """The value tiles of one launch are withheld: its bounded waits run out, the status word says so, nothing faults."""
+    c = Case(18, BF, 8, 2, d, 16, [300, 5], 9)
+    want = c.want()
+    c.check(c.run(), want)
+    assert lib().load_library().poss_debug_paged_lose_load(1) == 0
+    c.run()
+    assert int(c.gpu_status) == 6
+    c.check(c.run(), want)
+    assert int(c.gpu_status) == 0
+
+
 def test_attention_on_another_stream():
     c = Case(16, BF, 8, 2, 128, 16, [300, 5], 9)
     want = c.want()
