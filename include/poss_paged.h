@@ -64,7 +64,8 @@ POSS_API size_t poss_paged_attention_workspace_bytes(const poss_page_pool* pool,
  * each).  Output rows behind n_rows[b] are left as they were; a row that sees nothing becomes zeros.  What is not seen
  * has no influence, whatever it holds (infinities and NaN too).  A missing page's slots count as unseen, a sequence
  * with lengths out of range has no rows (status).
- * rows <= POSS_MAX_ROWS.  bf16 with head dimension 64 or 128 and a page size of 16, 32, 64, 128 or 256 slots runs on
+ * rows <= POSS_MAX_ROWS; batch * n_kv_heads * ceil(rows * (query heads per KV head) / 256) * ceil(max_pages * page_slots
+ * / 128) < 2^31.  bf16 with head dimension 64 or 128 and a page size of 16, 32, 64, 128 or 256 slots runs on
  * the tensor cores; the probabilities enter the second product rounded to bf16 there, sums and the output's
  * accumulation are fp32.  How the keys are cut, and so the last bits of a result, depends on the whole batch's
  * lengths; equal calls give equal bits.  Errors: INVALID, SHAPE, CAPACITY, WORKSPACE (too small, not 256-byte

@@ -291,7 +291,7 @@ size_t poss_paged_attention_workspace_bytes(const poss_page_pool* pool, int batc
   if (page_pool_check(pool) != POSS_OK || page_table_check(pool, max_pages, batch) != POSS_OK) return 0;
   if (rows < 1 || rows > POSS_MAX_ROWS || n_q_heads < 1 || n_q_heads % pool->n_kv_heads) return 0;
   size_t n = paged_attn_simt_workspace(batch, rows, n_q_heads, pool->n_kv_heads, pool->head_dim);
-  if (paged_attn_tc_supported(*pool, 1.f)) {
+  if (paged_attn_tc_supported(*pool, n_q_heads / pool->n_kv_heads, 1.f)) {
     const size_t m = paged_attn_tc_workspace(*pool, batch, rows, n_q_heads, max_pages);
     if (m > n) n = m;
   }
@@ -328,7 +328,7 @@ int poss_paged_tree_attention(const poss_page_pool* pool, int layer, const void*
   a.layer = layer; a.batch = batch; a.rows = rows; a.Hq = n_q_heads; a.G = n_q_heads / pool->n_kv_heads;
   a.q = q; a.ld_q = ld_q; a.prefix_len = prefix_len; a.n_rows = n_rows; a.mask = anc_mask;
   a.mask_words = (rows + 63) / 64; a.scale = scale; a.out = out; a.ws = workspace; a.status = status;
-  if (paged_attn_tc_supported(*pool, scale)) launch_paged_attn_tc(L, a, kv_pages, *pool);
+  if (paged_attn_tc_supported(*pool, a.G, scale)) launch_paged_attn_tc(L, a, kv_pages, *pool);
   else launch_paged_attn_simt(L, a, kv_pages, pool->dtype);
   return L.err;
 }

@@ -20,8 +20,9 @@ struct PagedAttnArgs {
 size_t paged_attn_simt_workspace(int batch, int rows, int Hq, int Hkv, int d);
 void launch_paged_attn_simt(Launcher& L, const PagedAttnArgs& a, const void* pool, int dtype);
 
-// tcgen05 kernel: bf16, head dimension 64 or 128, pages of 16 .. 256 slots (powers of two)
-bool paged_attn_tc_supported(const poss_page_pool& p, float scale);
+// tcgen05 kernel: bf16, head dimension 64 or 128, pages of 16 .. 256 slots (powers of two), at most 128 query heads per KV head,
+// scale > 0
+bool paged_attn_tc_supported(const poss_page_pool& p, int G, float scale);
 size_t paged_attn_tc_workspace(const poss_page_pool& p, int batch, int rows, int Hq, int max_pages);
 void launch_paged_attn_tc(Launcher& L, const PagedAttnArgs& a, const void* pool, const poss_page_pool& p);
 

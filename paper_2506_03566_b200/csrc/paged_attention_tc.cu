@@ -1,21 +1,22 @@
 // Tree-masked attention over pages on the 5th-generation tensor cores (bf16, head dimension 64 or 128).
 //
 // The G = Hq / Hkv query heads of a KV head and a sequence's tree rows form one matrix of query rows (row * G + head), cut
-// into items of up to 256: (sequence, KV head, 256 query rows).  A unit of work is one item's product with 128 keys; the
+// into items of up to 256: (sequence, KV head, two slots of floor(128 / G) tree rows).  A unit of work is one item's product with 128 keys; the
 // units of the whole batch, in order of sequence, head, item and key, are cut into one contiguous range per CTA, one CTA
 // per SM, so that every SM streams the same number of keys however long the sequences are.  The part of an item that
 // falls into one CTA is a segment: one pass over its keys with the running maximum and sum of a softmax.  A segment that is
 // the whole item writes the output, any other leaves fp32 partials that a second kernel merges in key order.
 //
 // Inside a CTA two "slots" of 128 query rows share the key tiles:
-//   * items with more than 128 query rows: slot = half of the rows, both use every tile (each key is read once);
+//   * items with rows for both slots: each has its own, both use every tile (each key is read once);
 //   * smaller items: both slots hold the same rows and take the even / the odd tiles; they are merged at the end.
-// Warps 0-3 / 4-7 do the softmax of slot 0 / 1 (one thread per query row), one thread of warp 8 issues the products,
-// warp 9 the copies:
+// Warps 0-3 / 4-7 do the softmax of slot 0 / 1 (one thread per query row), warps 8 and 11 issue the copies of keys and of
+// values, one lane each of warps 9 and 10 the products of slot 0 and 1:
 //   * copies: TMA, one box per page and 64 columns, keys and values of a tile in turn through a ring of stages.  A page that
-//     is missing or behind the last slot is read from behind the pool: zeros;
-//   * S = Q K^T (fp32, TMEM); the softmax thread reads its row of S once (128 registers), masks it where the tile reaches the
-//     tree, takes the maximum, writes P = 2^(s - m) as bf16 over S in TMEM; O += P V with P as the TMEM operand;
+//     is missing or behind the last slot is read from behind the pool: zeros.  The next segment's queries come the same
+//     way while the last one ends;
+//   * S = Q K^T (fp32, TMEM); the softmax thread masks its row of S in place where the tile reaches the tree, takes its
+//     maximum, writes P = 2^(s - m) as bf16 over S in TMEM; O += P V with P as the TMEM operand;
 //   * the reference maximum m moves only when a row's maximum has grown by more than 2^8 (P stays below 2^8, which bf16
 //     and the fp32 sums hold as well as 1): then the thread scales its row of O in TMEM.  Otherwise O is never touched;
 //   * while one slot's softmax runs, the other slot's products do.
@@ -44,32 +45,46 @@ namespace {
 
 using namespace tcptx;
 
-constexpr int KT = 128;                 // keys per tile
+constexpr int KT = 64;                  // keys per tile
 constexpr int QR = 128;                 // query rows per slot
-constexpr int ITEM_ROWS = 2 * QR;
 constexpr int N_SOFTMAX = 256;
-constexpr int N_THREADS = N_SOFTMAX + 64;
-constexpr int WARP_MMA = 8, WARP_TMA = 9;
-constexpr int BLOCK = QR * 128;         // bytes of 128 rows x 64 bf16
+constexpr int N_THREADS = N_SOFTMAX + 128;
+constexpr int WARP_KEYS = 8, WARP_MMA = 9, WARP_VALUES = 11;   // WARP_MMA + slot issues the slot's products
+constexpr int GONE_RING = 32;           // tiles whose "a page is missing" is remembered: more than the copies run ahead
+constexpr int BLOCK = QR * 128;         // bytes of 128 query rows x 64 bf16
+constexpr int KV_BLOCK = KT * 128;      // bytes of a tile's 64 keys x 64 bf16
 constexpr int MAX_STAGES = 8;
 constexpr float RESCALE_LOG2 = 8.f;
 constexpr uint32_t TMEM_COLS = 512;
+constexpr int S_COLS = 2 * KT;          // a slot's scores: two buffers, in turn (P lies over its scores)
 
 template <int HD> struct Shape {
   static constexpr int CB = HD / 64;                      // 64-column blocks
-  static constexpr int TILE = CB * BLOCK;                 // bytes of a key, value or query tile
-  static constexpr int STAGES = HD == 128 ? 5 : 8;
-  static constexpr int Q_OFF = 0, KV_OFF = 2 * TILE, CTL_OFF = KV_OFF + STAGES * TILE;
+  static constexpr int Q_TILE = CB * BLOCK, TILE = CB * KV_BLOCK;   // bytes of a slot's queries, of a tile's keys or values
+  // Keys and values have a ring of stages each: a stage that both copy warps used in turn would let one of them, half a
+  // turn ahead, take the other's phase for its own.  Values stay until the second product, keys until the first.
+  static constexpr int NK = HD == 128 ? 4 : 8, NV = HD == 128 ? 6 : 8;
+  static_assert(NK % 2 == 0 && NV % 2 == 0, "a slot that takes every other tile keeps to its own stages");
+  static constexpr int Q_OFF = 0, K_OFF = 2 * Q_TILE, V_OFF = K_OFF + NK * TILE, CTL_OFF = V_OFF + NV * TILE;
 };
 
+// Barriers are waited for by parity, so no role may be able to fall, or run, two phases behind another on one barrier:
+//   s_full / p_full / pv_done [slot][step & 1]: S of step y + 2 is issued behind the second product of step y, which waits for
+//     P of step y -- a softmax that has seen S of step y knows that the products of step y - 2 are complete;
+//   kv_full / kv_empty [keys, values][stage]: filled in order by one warp, but copies land in any order.  A slot that uses every
+//     tile sees every phase; one that uses every other tile must meet the same stages again and no others, so that it has seen
+//     a stage's last phase itself: the rings have even lengths.  (At a segment's start all earlier phases are over: q_full
+//     follows q_empty, which follows all of the last segment's first products, and o_free all of its second ones.)
+//   q_full, q_empty, o_free: one phase per segment.  A slot without steps in a segment waits for no o_free there, but a slot
+//     with steps gives q_empty up only behind its wait for the o_free before: whoever has seen q_full of segment s + 1 knows
+//     that o_free of segment s - 1 is complete.
 struct Ctl {
-  uint64_t kv_full[MAX_STAGES], kv_empty[MAX_STAGES], q_full, s_full[2], p_full[2], pv_done[2], o_free, drain;
+  uint64_t kv_full[2][MAX_STAGES], kv_empty[2][MAX_STAGES], q_full, q_empty, s_full[2][2], p_full[2][2], pv_done[2][2], o_free, drain[2];
   uint32_t tmem;
   int abort;
-  int missing[2];                       // by parity of the segment: a page that the segment needs is not there
-  unsigned long long nonfinite[2][2];   // by parity: tree slots whose values hold infinities or NaN
-  long long total;                      // units of the batch
-  long long offset0;                    // the CTA's first unit inside its first sequence
+  uint8_t gone[GONE_RING];              // by tile: a page of it is missing
+  unsigned long long nonfinite[2][N_SOFTMAX / 32][2];   // by parity and warp: tree slots whose values hold infinities or NaN
+  uint32_t total, offset0;              // units of the batch; the CTA's first unit inside its first sequence
   int seq0, grid;                       // that sequence; CTAs that share the units
   float2 ml[2][QR];                     // a slot's maximum and sum, for the merge of two slots with the same rows
 };
@@ -77,8 +92,8 @@ static_assert(sizeof(Ctl) <= 3072, "the control block lies behind the tiles");
 
 struct TcArgs {
   PagedAttnArgs a;
-  float scale_log2;                     // |scale| log2 e
-  uint32_t q_flip;                      // sign bits of two bf16 where the scale is negative
+  float scale_log2;                     // scale times log2 e, positive
+  int slot_rows;                        // tree rows per slot: floor(128 / G); a slot's lines are (tree row, head)
   int row_cap;                          // query rows that a partial has room for
   int rows_total;                       // rows of the pool's layer: the first coordinate behind it
   int inject_lost_load;
@@ -88,46 +103,44 @@ struct TcArgs {
 
 // ---- the units of a sequence
 struct SeqWork {
-  int prefix, rows, total, tiles, nq, groups;   // groups: items per KV head
-  long long units;
+  int prefix, rows, total, tiles, groups;       // groups: items per KV head
+  uint32_t units;                       // (a batch's units fit 31 bits: checked on the host)
   bool bad;
 };
-__device__ __forceinline__ SeqWork seq_work(const PagedAttnArgs& a, int b) {
+__device__ __forceinline__ SeqWork seq_work(const TcArgs& k, int b) {
+  const PagedAttnArgs& a = k.a;
   const SeqLen n = seq_len_of(a.prefix_len[b], a.n_rows ? a.n_rows[b] : a.rows, a.rows,
                               (long long)a.g.max_pages * a.g.page);
   SeqWork s;
   s.bad = n.bad; s.prefix = n.prefix; s.rows = n.rows;
   s.total = n.prefix + n.rows;
   s.tiles = (s.total + KT - 1) / KT;
-  s.nq = n.rows * a.G;
-  s.groups = (s.nq + ITEM_ROWS - 1) / ITEM_ROWS;
-  s.units = (long long)s.groups * a.g.Hkv * s.tiles;      // no rows: no groups
+  s.groups = (n.rows + 2 * k.slot_rows - 1) / (2 * k.slot_rows);
+  s.units = (uint32_t)s.groups * a.g.Hkv * s.tiles;       // no rows: no groups
   return s;
 }
-// One warp: units of all sequences, and of those before sequence `upto`.
-__device__ __forceinline__ void count_units(const PagedAttnArgs& a, int upto, long long* total, long long* before) {
+// CTAs that share `total` units, and the cut: the first total % grid of them take one unit more.
+__device__ __forceinline__ int unit_grid(uint32_t total, uint32_t ctas) { return (int)(total < ctas ? total : ctas); }
+struct Cut {
+  uint32_t each, more;
+  __device__ __forceinline__ Cut(uint32_t total, uint32_t grid) { each = total / grid; more = total - each * grid; }
+  __device__ __forceinline__ uint32_t begin(uint32_t c) const { return c * each + (c < more ? c : more); }
+  __device__ __forceinline__ int cta_of(uint32_t u) const {
+    const uint32_t longer = more * (each + 1);            // units of the CTAs with one more
+    return u < longer ? u / (each + 1) : more + (u - longer) / each;
+  }
+};
+// One warp: the units of all sequences.  For up to 32 sequences every lane keeps its own one's in *mine.
+__device__ __forceinline__ uint32_t count_units(const TcArgs& k, uint32_t* mine) {
   const int lane = threadIdx.x & 31;
-  long long t = 0, f = 0;
-  for (int b = lane; b < a.batch; b += 32) {
-    const long long u = seq_work(a, b).units;
+  uint32_t t = 0;
+  *mine = 0;
+  for (int b = lane; b < k.a.batch; b += 32) {
+    const uint32_t u = seq_work(k, b).units;
+    if (b < 32) *mine = u;
     t += u;
-    if (b < upto) f += u;
   }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    t += __shfl_xor_sync(0xffffffffu, t, o);
-    f += __shfl_xor_sync(0xffffffffu, f, o);
-  }
-  *total = t;
-  *before = f;
-}
-// CTAs that share `total` units
-__device__ __forceinline__ int unit_grid(long long total, int ctas) {
-  return total < ctas ? (total < 1 ? 1 : (int)total) : ctas;
-}
-__device__ __forceinline__ long long range_begin(long long c, long long total, int grid) { return c * total / grid; }
-__device__ __forceinline__ int cta_of_unit(long long u, long long total, int grid) {
-  return (int)(((u + 1) * grid + total - 1) / total - 1);   // the largest c with range_begin(c) <= u
+  return __reduce_add_sync(0xffffffffu, t);
 }
 
 struct Segment {
@@ -136,37 +149,45 @@ struct Segment {
 };
 // A CTA's segments in order; every role walks them by itself.
 struct Walk {
-  long long u, u_end, offset;
+  uint32_t u, u_end, offset;
   int b;
   __device__ __forceinline__ void start(const Ctl& c) {
-    u = blockIdx.x < c.grid ? range_begin(blockIdx.x, c.total, c.grid) : c.total;
-    u_end = blockIdx.x < c.grid ? range_begin(blockIdx.x + 1, c.total, c.grid) : c.total;
+    u = u_end = 0;
+    if ((int)blockIdx.x < c.grid) {
+      const Cut cut(c.total, c.grid);
+      u = cut.begin(blockIdx.x);
+      u_end = cut.begin(blockIdx.x + 1);
+    }
     b = c.seq0;
     offset = c.offset0;
   }
-  __device__ __forceinline__ bool next(const PagedAttnArgs& a, Segment* g) {
+  __device__ __forceinline__ bool next(const TcArgs& k, Segment* g) {
     if (u >= u_end) return false;
-    g->s = seq_work(a, b);
+    g->s = seq_work(k, b);
     while (offset >= g->s.units) {
       offset -= g->s.units;
-      if (++b >= a.batch) return false;                   // (not reached: the range lies inside the batch's units)
-      g->s = seq_work(a, b);
+      if (++b >= k.a.batch) return false;                   // (not reached: the range lies inside the batch's units)
+      g->s = seq_work(k, b);
     }
     g->b = b;
-    const long long item = offset / g->s.tiles;
+    const uint32_t item = offset / (uint32_t)g->s.tiles;
     g->tile0 = (int)(offset - item * g->s.tiles);
-    g->head = (int)(item / g->s.groups);
-    g->group = (int)(item - (long long)g->head * g->s.groups);
-    const long long left = u_end - u;
-    g->n = g->s.tiles - g->tile0;
-    if (g->n > left) g->n = (int)left;
+    g->head = (int)item;
+    g->group = 0;
+    if (g->s.groups > 1) {
+      g->head = (int)(item / (uint32_t)g->s.groups);
+      g->group = (int)item - g->head * g->s.groups;
+    }
+    g->n = min(g->s.tiles - g->tile0, (int)(u_end - u));
     u += g->n;
     offset += g->n;
     return true;
   }
 };
 // two slots of different rows (true) or of the same rows and alternating tiles
-__device__ __forceinline__ bool two_halves(const Segment& g) { return g.s.nq - g.group * ITEM_ROWS > QR; }
+__device__ __forceinline__ bool two_halves(const TcArgs& k, const Segment& g) {
+  return g.s.rows - g.group * 2 * k.slot_rows > k.slot_rows;
+}
 
 // ---- PTX
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t* r) {
@@ -199,6 +220,19 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* r) {
 }
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+      ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1)
+      : "memory");
+}
+__device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int col, int head, int row,
+                                            int seq) {
+  asm volatile(
+      "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];"
+      ::"r"(dst), "l"(map), "r"(bar), "r"(col), "r"(0), "r"(head), "r"(row), "r"(seq)
+      : "memory");
+}
 // orders the use of registers behind the wait for the loads that fill them
 __device__ __forceinline__ void tie32(uint32_t* r) {
 #pragma unroll
@@ -217,24 +251,71 @@ __device__ __forceinline__ void umma_bf16_ts(uint32_t tmem_d, uint32_t tmem_a, u
       : "memory");
 }
 // MN-major operand, 128-byte swizzle: 64 columns are one 128-byte line, consecutive keys consecutive lines, 8-line groups
-// 1024 bytes apart, the next 64 columns one BLOCK further
+// 1024 bytes apart, the next 64 columns one KV_BLOCK further
 __device__ __forceinline__ uint64_t smem_desc_values(uint32_t addr) {
   uint64_t d = 0;
   d |= (uint64_t)((addr & 0x3FFFFu) >> 4);
-  d |= (uint64_t)(BLOCK >> 4) << 16;
+  d |= (uint64_t)(KV_BLOCK >> 4) << 16;
   d |= (uint64_t)(1024u >> 4) << 32;
   d |= 1ull << 46;
   d |= 2ull << 61;
   return d;
+}
+__device__ __forceinline__ bool elect_one() {
+  uint32_t e;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(e));
+  return e != 0;
 }
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// two fp32 operations per instruction
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n\t.reg .b64 x, y, z, w;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\t"
+      "fma.rn.f32x2 w, x, y, z;\n\tmov.b64 {%0, %1}, w;\n\t}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 x, y, w;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tadd.rn.f32x2 w, x, y;\n\t"
+      "mov.b64 {%0, %1}, w;\n\t}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<uint32_t*>(&v);
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+__device__ __forceinline__ float max32(const uint32_t* s, float m) {
+  float a = __uint_as_float(s[0]), b = __uint_as_float(s[1]);
+#pragma unroll
+  for (int x = 2; x < 30; x += 4) {
+    a = max3(a, __uint_as_float(s[x]), __uint_as_float(s[x + 1]));
+    b = max3(b, __uint_as_float(s[x + 2]), __uint_as_float(s[x + 3]));
+  }
+  a = max3(a, __uint_as_float(s[30]), __uint_as_float(s[31]));
+  return max3(a, b, m);
+}
+// p = 2^(s * scale + off) for 32 scores, packed to bf16; their sum goes to l0, l1.  (A part of the 2^x as a polynomial on the
+// multiply-add pipe was measured too: it loses, 261 against 249 us for 16 trees of 61 rows over 16383 slots.)
+__device__ __forceinline__ void exp32(const uint32_t* s, float2 scale, float2 off, uint32_t* p, float2& l0, float2& l1) {
+#pragma unroll
+  for (int x = 0; x < 32; x += 2) {
+    const float2 a = fma2(make_float2(__uint_as_float(s[x]), __uint_as_float(s[x + 1])), scale, off);
+    const float2 e = make_float2(ex2(a.x), ex2(a.y));
+    if (x & 2) l1 = add2(l1, e);
+    else l0 = add2(l0, e);
+    p[x >> 1] = pack_bf16(e.x, e.y);
+  }
 }
 __device__ __forceinline__ void softmax_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 __device__ __forceinline__ bool nonfinite2(uint32_t w) {
@@ -253,37 +334,43 @@ __device__ __forceinline__ float* partial_of(const TcArgs& k, int hd, int cta, i
 }
 
 // ---------------------------------------------------------------------------------------------------- the kernel
+// Every role walks the CTA's segments by itself, in one loop that they share: code that a launch runs once costs its
+// instruction fetches (about 25 cycles per instruction that no warp of the SM has run yet), so there is one copy of it.
 template <int HD>
-__global__ void __launch_bounds__(N_THREADS, 1) k_paged_attn_tc(const __grid_constant__ CUtensorMap map, const TcArgs k) {
+__global__ void __launch_bounds__(N_THREADS, 1) k_paged_attn_tc(const __grid_constant__ CUtensorMap map,
+                                                                 const __grid_constant__ CUtensorMap map_q,
+                                                                 const TcArgs k) {
   using Z = Shape<HD>;
   extern __shared__ __align__(1024) uint8_t smem[];
   Ctl& c = *reinterpret_cast<Ctl*>(smem + Z::CTL_OFF);
   const uint32_t base = smem_u32(smem);
   const PagedAttnArgs& a = k.a;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   auto bar = [&](uint64_t& x) { return smem_u32(&x); };
 
   if (warp == WARP_MMA) {
     if (lane == 0) {
       // (tiles start on 1024 bytes and fit: checked on the host, and here)
       c.abort = (base & 1023u) || Z::CTL_OFF + sizeof(Ctl) > k.smem_bytes ? 1 : 0;
-      c.missing[0] = c.missing[1] = 0;
-      for (int i = 0; i < 2; ++i) c.nonfinite[i][0] = c.nonfinite[i][1] = 0;
-      for (int i = 0; i < Z::STAGES; ++i) {
-        mbar_init(bar(c.kv_full[i]), 1);
-        mbar_init(bar(c.kv_empty[i]), 1);
+      for (int i = 0; i < 2 * MAX_STAGES; ++i) {
+        mbar_init(bar(c.kv_full[i / MAX_STAGES][i % MAX_STAGES]), 1);
+        mbar_init(bar(c.kv_empty[i / MAX_STAGES][i % MAX_STAGES]), 2);
       }
-      mbar_init(bar(c.q_full), N_SOFTMAX);
+      mbar_init(bar(c.q_full), 1);
+      mbar_init(bar(c.q_empty), 2);
       mbar_init(bar(c.o_free), N_SOFTMAX);
-      mbar_init(bar(c.drain), 1);
       for (int i = 0; i < 2; ++i) {
-        mbar_init(bar(c.s_full[i]), 1);
-        mbar_init(bar(c.p_full[i]), QR);
-        mbar_init(bar(c.pv_done[i]), 1);
+        mbar_init(bar(c.drain[i]), 1);
+        for (int j = 0; j < 2; ++j) {
+          mbar_init(bar(c.s_full[i][j]), 1);
+          mbar_init(bar(c.p_full[i][j]), QR);
+          mbar_init(bar(c.pv_done[i][j]), 1);
+        }
       }
       asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       prefetch_tensormap(&map);
+      prefetch_tensormap(&map_q);
     }
     __syncwarp();
     tmem_alloc(smem_u32(&c.tmem), TMEM_COLS);
@@ -292,7 +379,7 @@ __global__ void __launch_bounds__(N_THREADS, 1) k_paged_attn_tc(const __grid_con
   __syncthreads();
   tc_fence_after();
   volatile int* abort_flag = &c.abort;
-  const uint32_t tm = c.tmem;
+  const uint32_t tm = __shfl_sync(0xffffffffu, c.tmem, 0);
   // The successor may start only now that this CTA holds its TMEM columns: one that took columns on this SM first would
   // keep them until this grid has finished.
   pdl_begin();
@@ -300,17 +387,17 @@ __global__ void __launch_bounds__(N_THREADS, 1) k_paged_attn_tc(const __grid_con
 
   if (warp == 0) {
     // the batch's units, and the sequence that the CTA's first one lies in
-    long long total, none;
-    count_units(a, 0, &total, &none);
-    const int grid = unit_grid(total, (int)gridDim.x);
-    if ((int)blockIdx.x < grid && total > 0) {
-      long long at = range_begin(blockIdx.x, total, grid);
+    uint32_t u;
+    const uint32_t total = count_units(k, &u);
+    const int grid = unit_grid(total, gridDim.x);
+    if ((int)blockIdx.x < grid) {
+      uint32_t at = Cut(total, grid).begin(blockIdx.x);
       for (int b0 = 0; b0 < a.batch; b0 += 32) {
-        const long long u = b0 + lane < a.batch ? seq_work(a, b0 + lane).units : 0;
-        long long x = u;
+        if (b0 > 0) u = b0 + lane < a.batch ? seq_work(k, b0 + lane).units : 0;
+        uint32_t x = u;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-          const long long y = __shfl_up_sync(0xffffffffu, x, o);
+          const uint32_t y = __shfl_up_sync(0xffffffffu, x, o);
           if (lane >= o) x += y;
         }
         const unsigned here = __ballot_sync(0xffffffffu, at < x);
@@ -327,297 +414,157 @@ __global__ void __launch_bounds__(N_THREADS, 1) k_paged_attn_tc(const __grid_con
     }
     if (lane == 0) {
       c.total = total;
-      c.grid = total > 0 ? grid : 0;
+      c.grid = grid;
     }
-    if (blockIdx.x == 0)
-      for (int b = lane; b < a.batch; b += 32)
-        if (seq_work(a, b).bad) raise_status(a.status, POSS_E_INVALID);
   }
   __syncthreads();
 
   Walk walk;
   walk.start(c);
+  const uint32_t u_first = walk.u;
   Segment g;
+  // what a role carries from segment to segment
+  bool ok = __all_sync(0xffffffffu, *abort_flag == 0);
+  int tiles_before = 0;                                   // tiles of the segments before
+  int n_own = 0, n_partly = 0;                            // softmax and products: steps of the slot; copies: tiles
+  // copies: stage and phase of the next keys or values
+  uint32_t c_ph = 0, elected = 0;
+  int c_st = 0;
+  if (warp == WARP_MMA || warp == WARP_MMA + 1) elected = elect_one();
+  constexpr uint32_t ROW16 = 2;                           // 16 bf16 = 32 bytes, in 16-byte address units
+  constexpr uint32_t idesc_s = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(KT >> 3) << 17) | ((uint32_t)(QR >> 4) << 24);
+  constexpr uint32_t idesc_o = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(HD >> 3) << 17) |
+                               ((uint32_t)(QR >> 4) << 24) | (1u << 16);       // the values are MN-major
+  const uint64_t q_desc = smem_desc_sw128(base + Z::Q_OFF), k_desc = smem_desc_sw128(base + Z::K_OFF),
+                 v_desc = smem_desc_values(base + Z::V_OFF);
+  auto wait = [&](uint64_t& b, int phase) {
+    if (ok) ok = mbar_wait(bar(b), (uint32_t)(phase & 1), abort_flag);
+  };
 
-  if (warp == WARP_TMA) {
-    // ---------------------------------------------------------------- copies
-    const int page = a.g.page, per_tile = page < KT ? KT / page : 1;
-    const uint64_t policy = policy_evict_normal();
-    int idx = 0;                                          // tiles loaded so far, keys and values counted apart
-    bool ok = __all_sync(0xffffffffu, *abort_flag == 0);
-    while (ok && walk.next(a, &g)) {
-      const int32_t* table = a.g.tables + (size_t)g.b * a.g.max_pages;
-      // the lane's page of a tile (lanes below per_tile), fetched one tile ahead
-      auto fetch = [&](int tile) {
-        const int key0 = tile * KT + lane * page;
-        int p = -1;
-        if (lane < per_tile && key0 < g.s.total) {
-          p = page_at(table, a.g.max_pages, a.g.n_pages, key0 / page);
-          if (p < 0) raise_status(a.status, POSS_E_INVALID);
-        }
-        return p;
-      };
-      int p_next = fetch(g.tile0);
-      for (int t = 0; ok && t < g.n; ++t) {
-        const int p = p_next;
-        if (t + 1 < g.n) p_next = fetch(g.tile0 + t + 1);
-        const int in_page = page > KT ? (g.tile0 + t) * KT % page : 0;
-#pragma unroll
-        for (int kv = 0; kv < 2; ++kv, ++idx) {
-          const int st = idx % Z::STAGES, turn = idx / Z::STAGES;
-          if (turn > 0) ok = mbar_wait(bar(c.kv_empty[st]), (uint32_t)((turn - 1) & 1), abort_flag);
-          ok = __all_sync(0xffffffffu, ok);
-          if (!ok) break;
-          const uint32_t full = bar(c.kv_full[st]), dst = base + Z::KV_OFF + st * Z::TILE;
-          if (lane == 0) mbar_expect_tx(full, Z::TILE);
-          __syncwarp();
-          if (lane < per_tile && !(k.inject_lost_load && kv)) {
-            const int row = p >= 0 ? ((p * 2 + kv) * a.g.Hkv + g.head) * page + in_page : k.rows_total;
-#pragma unroll
-            for (int cb = 0; cb < Z::CB; ++cb)
-              tma_load_2d(dst + cb * BLOCK + lane * page * 128, &map, full, cb * 64, row, policy);
-          }
-          __syncwarp();
-        }
-      }
-    }
-    if (*abort_flag) {
-      // the copies under way must land before the CTA's shared memory goes away
-      const uint64_t t0 = global_ns();
-      for (int i = idx > Z::STAGES ? idx - Z::STAGES : 0; i < idx; ++i)
-        while (!mbar_try_wait(bar(c.kv_full[i % Z::STAGES]), (uint32_t)((i / Z::STAGES) & 1)) &&
-               global_ns() - t0 < WAIT_LIMIT_NS / 2)
-          __nanosleep(64);
-    }
-  } else if (warp == WARP_MMA) {
-    // ---------------------------------------------------------------- products
-    if (lane == 0) {
-      const uint32_t idesc_s = instr_desc_bf16(QR, KT);
-      const uint32_t idesc_o = instr_desc_bf16(QR, HD) | (1u << 16);     // the values are MN-major
-      int tiles_before = 0, seg = 0;
-      int n_pv[2] = {0, 0};                               // second products issued per slot
-      bool ok = *abort_flag == 0;
-      auto wait = [&](uint64_t& b, int phase) { ok = ok && mbar_wait(bar(b), (uint32_t)(phase & 1), abort_flag); };
-      for (; ok && walk.next(a, &g); ++seg) {
-        const bool halves = two_halves(g);
-        const int steps = halves ? 2 * g.n : g.n;
-        auto tile_of = [&](int x) { return halves ? x >> 1 : x; };
-        auto issue_s = [&](int x) {
-          const int slot = x & 1, i = 2 * (tiles_before + tile_of(x)), st = i % Z::STAGES;
-          if (!halves || !(x & 1)) wait(c.kv_full[st], i / Z::STAGES);
-          if (!ok) return;
-          tc_fence_after();
-          const uint32_t d = tm + slot * KT, kb = base + Z::KV_OFF + st * Z::TILE, qb = base + Z::Q_OFF + slot * Z::TILE;
-#pragma unroll
-          for (int cb = 0; cb < Z::CB; ++cb) {
-            const uint64_t ad = smem_desc_sw128(qb + cb * BLOCK), bd = smem_desc_sw128(kb + cb * BLOCK);
-#pragma unroll
-            for (int kk = 0; kk < 4; ++kk)                // 16 bf16 = 32 bytes = 2 address units
-              umma_bf16(d, ad + (uint64_t)(2 * kk), bd + (uint64_t)(2 * kk), idesc_s, (cb | kk) ? 1u : 0u);
-          }
-          umma_commit(bar(c.s_full[slot]));
-          if (!halves || (x & 1)) umma_commit(bar(c.kv_empty[st]));
-        };
-        wait(c.q_full, seg);
-        // P of a slot lies over its S: the last segment's second products must have read theirs
-        for (int s = 0; s < 2; ++s)
-          if (n_pv[s] > 0) wait(c.pv_done[s], n_pv[s] - 1);
-        issue_s(0);
-        if (steps > 1) issue_s(1);
-        for (int x = 0; ok && x < steps; ++x) {
-          const int slot = x & 1, t = tile_of(x), i = 2 * (tiles_before + t) + 1, st = i % Z::STAGES;
-          wait(c.p_full[slot], n_pv[slot]);
-          if (x == 0 && seg > 0) wait(c.o_free, seg - 1);
-          if (!halves || !(x & 1)) wait(c.kv_full[st], i / Z::STAGES);
-          if (!ok) break;
-          tc_fence_after();
-          const int keys = g.s.total - (g.tile0 + t) * KT, n16 = keys >= KT ? KT / 16 : (keys + 15) / 16;
-          const uint32_t d = tm + 2 * KT + slot * HD, p = tm + slot * KT, vb = base + Z::KV_OFF + st * Z::TILE;
-          for (int ks = 0; ks < n16; ++ks)
-            umma_bf16_ts(d, p + ks * 8, smem_desc_values(vb + ks * 2048), idesc_o, (x >= 2 || ks > 0) ? 1u : 0u);
-          umma_commit(bar(c.pv_done[slot]));
-          if (!halves || (x & 1)) umma_commit(bar(c.kv_empty[st]));
-          ++n_pv[slot];
-          if (x + 2 < steps) {
-            wait(c.pv_done[slot], n_pv[slot] - 1);        // P has been read: S may take its place
-            issue_s(x + 2);
-          }
-        }
-        tiles_before += g.n;
-      }
-      if (*abort_flag) {
-        // the products under way must end before the CTA's TMEM and shared memory go away
-        const uint64_t t0 = global_ns();
-        umma_commit(bar(c.drain));
-        while (!mbar_try_wait(bar(c.drain), 0) && global_ns() - t0 < WAIT_LIMIT_NS / 2) __nanosleep(64);
-      }
-    }
-    __syncwarp();
-  } else {
-    // ---------------------------------------------------------------- softmax, one thread per query row
-    const int wg = warp >> 2, row = (warp & 3) * 32 + lane, tid = threadIdx.x;
-    const uint32_t t_lane = tm + ((uint32_t)((warp & 3) * 32) << 16);
-    const uint32_t t_s = t_lane + wg * KT, t_o = t_lane + 2 * KT + wg * HD;
-    int tiles_before = 0, n_s = 0, n_other = 0;           // steps of this slot / of the other one so far
-    bool ok = true;
-    auto wait = [&](uint64_t& b, int phase) { ok = ok && mbar_wait(bar(b), (uint32_t)(phase & 1), abort_flag); };
-    for (int seg = 0; walk.next(a, &g); ++seg) {
-      const bool halves = two_halves(g);
-      const int par = seg & 1;
-      softmax_sync();                                     // both slots have left the segment before
-      if (tid == 0) {
-        c.missing[par ^ 1] = 0;
-        c.nonfinite[par ^ 1][0] = c.nonfinite[par ^ 1][1] = 0;
-      }
-      const int32_t* table = a.g.tables + (size_t)g.b * a.g.max_pages;
-      {
-        const int end = min((g.tile0 + g.n) * KT, g.s.total);
-        for (int i = g.tile0 * KT / a.g.page + tid; i * a.g.page < end; i += N_SOFTMAX)
-          if (page_at(table, a.g.max_pages, a.g.n_pages, i) < 0) c.missing[par] = 1;
-      }
-      // ---- the slot's queries into shared memory: 128 rows, 16-byte pieces swizzled by row
-      const int q0 = g.group * ITEM_ROWS + (halves ? wg * QR : 0);
-      {
-        constexpr int PIECES = HD / 8, ROWS_AT_ONCE = 128 / PIECES;
-        const int piece = (tid & 127) % PIECES, r0 = (tid & 127) / PIECES;
-        const char* q = reinterpret_cast<const char*>(a.q);
-        uint4 v[QR / ROWS_AT_ONCE];
-#pragma unroll
-        for (int j = 0; j < QR / ROWS_AT_ONCE; ++j) {
-          const int qi = q0 + r0 + j * ROWS_AT_ONCE;
-          v[j] = make_uint4(0, 0, 0, 0);
-          if (qi < g.s.nq) {
-            const int r = qi / a.G;
-            v[j] = *reinterpret_cast<const uint4*>(
-                q + (((size_t)g.b * a.rows + r) * a.ld_q + (size_t)(g.head * a.G + qi - r * a.G) * HD + piece * 8) * 2);
-            v[j].x ^= k.q_flip; v[j].y ^= k.q_flip; v[j].z ^= k.q_flip; v[j].w ^= k.q_flip;
-          }
-        }
-        uint8_t* dst = smem + Z::Q_OFF + wg * Z::TILE + (piece >> 3) * BLOCK;
-#pragma unroll
-        for (int j = 0; j < QR / ROWS_AT_ONCE; ++j) {
-          const int r = r0 + j * ROWS_AT_ONCE;
-          *reinterpret_cast<uint4*>(dst + r * 128 + (((piece & 7) ^ (r & 7)) << 4)) = v[j];
-        }
-      }
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      mbar_arrive(bar(c.q_full));
-      softmax_sync();
-      const bool missing = *(volatile int*)&c.missing[par] != 0;
+  for (int seg = 0; walk.next(k, &g); ++seg) {
+    const bool halves = two_halves(k, g);
+    const int par = seg & 1;
+    const int32_t* const table = a.g.tables + (size_t)g.b * a.g.max_pages;
 
-      const int qi = q0 + row;
-      const bool valid = qi < g.s.nq, live = q0 + (row & ~31) < g.s.nq;   // live: some row of the warp exists
-      const int r = valid ? qi / a.G : 0;
+    if (warp < N_SOFTMAX / 32) {
+      // -------------------------------------------------------------- softmax, one thread per query row
+      const int wg = warp >> 2, row = (warp & 3) * 32 + lane;
+      const uint32_t t_lane = tm + ((uint32_t)((warp & 3) * 32) << 16);
+      const uint32_t t_s = t_lane + wg * S_COLS, t_o = t_lane + 2 * S_COLS + wg * HD;
+      // the thread's line of the slot: tree row and head
+      const int r0 = (2 * g.group + (halves ? wg : 0)) * k.slot_rows, in_slot = row / a.G, head = row - in_slot * a.G;
+      const bool valid = in_slot < k.slot_rows && r0 + in_slot < g.s.rows;
+      const bool live = __any_sync(0xffffffffu, valid);   // some line of the warp exists
+      const int r = valid ? r0 + in_slot : 0;
       uint64_t lo = 0, hi = 0;
       if (valid) paged_row_mask(a.mask, (size_t)g.b * a.rows + r, a.mask_words, g.s.rows, &lo, &hi);
+      if (lane == 0) c.nonfinite[par][warp][0] = c.nonfinite[par][warp][1] = 0;
+      __syncwarp();
       float m = -INFINITY, l = 0.f;                       // reference maximum (scores times scale_log2), sum
-      const int steps = halves ? g.n : (g.n - wg + 1) >> 1;
-      for (int i = 0; i < steps; ++i, ++n_s) {
+      const int steps = halves ? g.n : (g.n - wg + 1) >> 1;   // the slot's tiles: all, or every other one
+      const float2 sc = make_float2(k.scale_log2, k.scale_log2);
+#pragma unroll 1
+      for (int i = 0; i < steps; ++i, ++n_own) {
         const int t = halves ? i : 2 * i + wg, key0 = (g.tile0 + t) * KT;
         const bool partly = key0 + KT > g.s.prefix;       // the tile reaches the tree
-        wait(c.s_full[wg], n_s);
-        tc_fence_after();
         if (partly && (!halves || wg == 0)) {
           // values behind the last slot, and infinities and NaN of tree slots, become zeros; one thread per key
-          const int iv = 2 * (tiles_before + t) + 1, st = iv % Z::STAGES;
-          wait(c.kv_full[st], iv / Z::STAGES);
+          // (once the scores are there, the slot's last values but one have been used: the stage is in this tile's turn)
+          const int st = (tiles_before + t) % Z::NV;
+          wait(c.s_full[wg][n_own & 1], n_own >> 1);
+          wait(c.kv_full[1][st], (tiles_before + t) / Z::NV);
           const int key = key0 + row, n16 = min(KT, (g.s.total - key0 + 15) & ~15);
           if (ok && row < n16 && key >= g.s.prefix) {
-            uint8_t* v = smem + Z::KV_OFF + st * Z::TILE + row * 128;
+            uint8_t* v = smem + Z::V_OFF + st * Z::TILE + row * 128;
             bool found = false;
-#pragma unroll
+#pragma unroll 4
             for (int j = 0; j < HD / 8; ++j) {
-              uint4* p = reinterpret_cast<uint4*>(v + (j >> 3) * BLOCK + (((j & 7) ^ (row & 7)) << 4));
+              uint4* p = reinterpret_cast<uint4*>(v + (j >> 3) * KV_BLOCK + (((j & 7) ^ (row & 7)) << 4));
+              uint4 x = *p;
               if (key >= g.s.total) {
                 *p = make_uint4(0, 0, 0, 0);
-              } else {
-                uint4 x = *p;
-                if (nonfinite2(x.x) || nonfinite2(x.y) || nonfinite2(x.z) || nonfinite2(x.w)) {
-                  found = true;
-                  *p = make_uint4(finite2(x.x), finite2(x.y), finite2(x.z), finite2(x.w));
-                }
+              } else if (nonfinite2(x.x) || nonfinite2(x.y) || nonfinite2(x.z) || nonfinite2(x.w)) {
+                found = true;
+                *p = make_uint4(finite2(x.x), finite2(x.y), finite2(x.z), finite2(x.w));
               }
             }
             const int j = key - g.s.prefix;
-            if (found) atomicOr(&c.nonfinite[par][j >> 6], 1ull << (j & 63));
+            if (found) atomicOr(&c.nonfinite[par][warp][j >> 6], 1ull << (j & 63));
           }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         }
+        if (partly && halves) {
+          // slot 1's product reads what slot 0's warps have put right.  (A segment has at most three such tiles; of the next
+          // one's, slot 0 can reach two while slot 1 has two of this one's before it: six barriers in turn.)
+          const int id = 2 + n_partly % 6;
+          if (wg == 0) asm volatile("bar.arrive %0, 256;" ::"r"(id) : "memory");
+          else asm volatile("bar.sync %0, 256;" ::"r"(id) : "memory");
+          ++n_partly;
+        }
+        const int buf = n_own & 1;
+        wait(c.s_full[wg][buf], n_own >> 1);
+        tc_fence_after();
+        const bool missing = *(volatile uint8_t*)&c.gone[(tiles_before + t) % GONE_RING] != 0;   // (written before the keys' copies)
         if (live) {
-          uint32_t s[KT];
-#pragma unroll
-          for (int j = 0; j < KT; j += 32) tmem_ld32(t_s + j, s + j);
+          uint32_t sa[32], sb[32], p[32];
+          tmem_ld32(t_s + buf * KT, sa);
+          tmem_ld32(t_s + buf * KT + 32, sb);
           tmem_wait_ld();
-#pragma unroll
-          for (int j = 0; j < KT; j += 32) tie32(s + j);
+          tie32(sa);
+          tie32(sb);
           if (partly || missing) {
-#pragma unroll
-            for (int j = 0; j < KT; j += 32) {
-              uint32_t vis = paged_visible32(key0 + j, g.s.prefix, lo, hi);
-              if (missing) {
+            uint32_t va = paged_visible32(key0, g.s.prefix, lo, hi), vb = paged_visible32(key0 + 32, g.s.prefix, lo, hi);
+            if (missing) {
 #pragma unroll 1
-                for (int x = 0; x < 32; x += 16)          // a page holds 16 slots or a multiple
-                  if (page_at(table, a.g.max_pages, a.g.n_pages, (key0 + j + x) / a.g.page) < 0) vis &= ~(0xffffu << x);
+              for (int x = 0; x < 32; x += 16) {        // a page holds 16 slots or a multiple
+                if (page_at(table, a.g.max_pages, a.g.n_pages, (key0 + x) / a.g.page) < 0) va &= ~(0xffffu << x);
+                if (page_at(table, a.g.max_pages, a.g.n_pages, (key0 + 32 + x) / a.g.page) < 0) vb &= ~(0xffffu << x);
               }
+            }
 #pragma unroll
-              for (int x = 0; x < 32; ++x)
-                if (!((vis >> x) & 1u)) s[j + x] = 0xff800000u;
+            for (int x = 0; x < 32; ++x) {
+              if (!((va >> x) & 1u)) sa[x] = 0xff800000u;
+              if (!((vb >> x) & 1u)) sb[x] = 0xff800000u;
             }
           }
-          float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-          for (int j = 0; j < KT; ++j) m4[j & 3] = fmaxf(m4[j & 3], __uint_as_float(s[j]));
-          const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * k.scale_log2;
+          const float mx = max32(sb, max32(sa, -INFINITY)) * k.scale_log2;
           if (i == 0) {
             m = mx;
           } else if (__any_sync(0xffffffffu, mx > m + RESCALE_LOG2)) {
-            // (the scores' completion was committed behind that of the slot's last second product)
+            wait(c.pv_done[wg][buf ^ 1], (n_own - 1) >> 1);   // O is at rest until this step's P is there
+            tc_fence_after();
             const float now = mx > m + RESCALE_LOG2 ? mx : m;
             const float f = now == m ? 1.f : (m == -INFINITY ? 0.f : ex2(m - now));
             m = now;
             l *= f;
 #pragma unroll 1
-            for (int j = 0; j < HD; j += 32) {
-              uint32_t o[32];
-              tmem_ld32(t_o + j, o);
-              tmem_wait_ld();
-              tie32(o);
+            for (int j = 0; j < HD; j += 16) {
+              uint32_t o[16];
+              tmem_ld16(t_o + j, reinterpret_cast<float*>(o));
 #pragma unroll
-              for (int x = 0; x < 32; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * f);
-              tmem_st32(t_o + j, o);
+              for (int x = 0; x < 16; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * f);
+              tmem_st16(t_o + j, o);
             }
           }
-          const float off = m == -INFINITY ? 0.f : m;     // nothing seen so far: 2^(-inf) = 0
-          float l4[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int j = 0; j < KT; j += 32) {
-            uint32_t p[16];
-#pragma unroll
-            for (int x = 0; x < 32; x += 2) {
-              const float p0 = ex2(fmaf(__uint_as_float(s[j + x]), k.scale_log2, -off));
-              const float p1 = ex2(fmaf(__uint_as_float(s[j + x + 1]), k.scale_log2, -off));
-              l4[x & 3] += p0;
-              l4[(x & 3) + 1] += p1;
-              p[x >> 1] = pack_bf16(p0, p1);
-            }
-            tmem_st16(t_s + (j >> 1), p);
-          }
-          l += (l4[0] + l4[1]) + (l4[2] + l4[3]);
+          const float off = m == -INFINITY ? 0.f : -m;  // nothing seen so far: 2^(-inf) = 0
+          const float2 of = make_float2(off, off);
+          float2 l0 = make_float2(0.f, 0.f), l1 = l0;
+          exp32(sa, sc, of, p, l0, l1);
+          exp32(sb, sc, of, p + 16, l0, l1);
+          tmem_st32(t_s + buf * KT, p);                 // (over the scores)
+          l += (l0.x + l0.y) + (l1.x + l1.y);
           tmem_wait_st();
         }
         tc_fence_before();
-        mbar_arrive(bar(c.p_full[wg]));
+        mbar_arrive(bar(c.p_full[wg][buf]));
       }
-
       // ---- the segment's output: final where it is the whole item, else partials
-      const int other = halves ? g.n : (g.n - (wg ^ 1) + 1) >> 1;
-      n_other += other;
-      if (steps > 0) wait(c.pv_done[wg], n_s - 1);
+      if (steps > 0) wait(c.pv_done[wg][(n_own - 1) & 1], (n_own - 1) >> 1);
       float c0 = 1.f, c1 = 0.f;                           // weights of slot 0's and slot 1's outputs (same rows)
       if (!halves) {
         c.ml[wg][row] = make_float2(m, l);
-        if (other > 0) wait(c.pv_done[wg ^ 1], n_other - 1);
-        softmax_sync();
+        tc_fence_before();
+        softmax_sync();                                   // both slots' outputs are complete
         const float2 x0 = c.ml[0][row], x1 = c.ml[1][row];
         m = fmaxf(x0.x, x1.x);
         // a slot that has seen nothing has sum 0 and is left out; one whose scores were all NaN has not
@@ -630,16 +577,23 @@ __global__ void __launch_bounds__(N_THREADS, 1) k_paged_attn_tc(const __grid_con
         const bool whole = g.tile0 == 0 && g.n == g.s.tiles;
         const int rr = halves ? wg * QR + row : row;      // row inside the item
         const float inv = l == 0.f ? 0.f : 1.f / l;       // a row that sees nothing: zeros
-        uint64_t nf_lo = c.nonfinite[par][0] & lo, nf_hi = c.nonfinite[par][1] & hi;
+        uint64_t nf_lo = 0, nf_hi = 0;
+#pragma unroll 1
+        for (int w = 0; w < N_SOFTMAX / 32; ++w) {
+          nf_lo |= c.nonfinite[par][w][0];
+          nf_hi |= c.nonfinite[par][w][1];
+        }
+        nf_lo &= lo;
+        nf_hi &= hi;
         float* part = nullptr;
         if (!whole) {
-          const bool first = g.tile0 > 0 || range_begin(blockIdx.x, c.total, c.grid) == walk.u - g.n;
-          part = partial_of(k, HD, blockIdx.x, first ? 0 : 1);
+          // the CTA's first segment, or its last
+          part = partial_of(k, HD, blockIdx.x, g.tile0 > 0 || u_first == walk.u - g.n ? 0 : 1);
           if (valid && (halves || wg == 0))
             __stcg(reinterpret_cast<float2*>(part + (size_t)k.row_cap * HD) + rr, make_float2(m, l));
         }
         bf16* const out = reinterpret_cast<bf16*>(a.out) +
-                          (((size_t)g.b * a.rows + r) * a.Hq + g.head * a.G + (qi - r * a.G)) * HD;
+                          (((size_t)g.b * a.rows + r) * a.Hq + g.head * a.G + head) * HD;
         const int col0 = halves ? 0 : wg * (HD / 2), cols = halves ? HD : HD / 2;
 #pragma unroll 1
         for (int j = col0; j < col0 + cols; j += 32) {
@@ -650,8 +604,8 @@ __global__ void __launch_bounds__(N_THREADS, 1) k_paged_attn_tc(const __grid_con
             tie32(o);
           } else {
             uint32_t o1[32];
-            tmem_ld32(t_lane + 2 * KT + j, o);
-            tmem_ld32(t_lane + 2 * KT + HD + j, o1);
+            tmem_ld32(t_lane + 2 * S_COLS + j, o);
+            tmem_ld32(t_lane + 2 * S_COLS + HD + j, o1);
             tmem_wait_ld();
             tie32(o);
             tie32(o1);
@@ -690,20 +644,175 @@ __global__ void __launch_bounds__(N_THREADS, 1) k_paged_attn_tc(const __grid_con
                 *reinterpret_cast<uint4*>(out + j + x) = make_uint4(w[0], w[1], w[2], w[3]);
               }
             } else {
+              uint4* dst = reinterpret_cast<uint4*>(part) + (size_t)(j >> 2) * k.row_cap + rr;
 #pragma unroll
-              for (int x = 0; x < 32; x += 4)
-                __stcg(reinterpret_cast<uint4*>(part) + (size_t)((j + x) >> 2) * k.row_cap + rr,
-                       make_uint4(o[x], o[x + 1], o[x + 2], o[x + 3]));
+              for (int x = 0; x < 32; x += 4, dst += k.row_cap) __stcg(dst, make_uint4(o[x], o[x + 1], o[x + 2], o[x + 3]));
             }
           }
         }
       }
       tc_fence_before();
       mbar_arrive(bar(c.o_free));                         // the accumulators may take the next segment
-      tiles_before += g.n;
+    } else if (warp == WARP_KEYS || warp == WARP_VALUES) {
+      // -------------------------------------------------------------- keys (and queries), values: a warp each, since a page's
+      // box is one lane's instruction and small pages make many of them
+      const int kv = warp == WARP_VALUES, n_stages = kv ? Z::NV : Z::NK;
+      const int page = a.g.page, per_tile = page < KT ? KT / page : 1;
+      // the lane's page of a tile (lanes below per_tile), fetched one tile ahead
+      auto fetch = [&](int tile) {
+        const int key0 = tile * KT + lane * page;
+        return lane < per_tile && key0 < g.s.total ? page_at(table, a.g.max_pages, a.g.n_pages, key0 / page) : -1;
+      };
+      int p_next = fetch(g.tile0);
+      // the queries: (tree row, head) lines of both slots (of the same rows twice where they share them)
+      auto load_queries = [&] {
+        if (seg > 0) wait(c.q_empty, seg - 1);            // the last segment's first products have read theirs
+        ok = __all_sync(0xffffffffu, ok);
+        if (ok && lane == 0) {
+          mbar_expect_tx(bar(c.q_full), 2 * k.slot_rows * a.G * HD * 2);
+#pragma unroll 1
+          for (int i = 0; i < 2 * Z::CB; ++i) {
+            const int slot = i & 1, cb = i >> 1;
+            tma_load_5d(base + Z::Q_OFF + slot * Z::Q_TILE + cb * BLOCK, &map_q, bar(c.q_full), cb * 64, g.head,
+                        (2 * g.group + (halves ? slot : 0)) * k.slot_rows, g.b);
+          }
+        }
+        __syncwarp();
+      };
+#pragma unroll 1
+      for (int t = 0; ok && t < g.n; ++t) {
+        const int p = p_next;
+        if (t + 1 < g.n) p_next = fetch(g.tile0 + t + 1);
+        const int in_page = page > KT ? (g.tile0 + t) * KT % page : 0;
+        if (!kv) {
+          const bool gone = __any_sync(0xffffffffu, p < 0 && lane < per_tile && (g.tile0 + t) * KT + lane * page < g.s.total);
+          if (lane == 0) {
+            c.gone[(tiles_before + t) % GONE_RING] = gone;
+            if (gone) raise_status(a.status, POSS_E_INVALID);
+          }
+        }
+        if (n_own >= n_stages) wait(c.kv_empty[kv][c_st], c_ph ^ 1);   // (a stage's first use waits for nobody)
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        const uint32_t full = bar(c.kv_full[kv][c_st]);
+        const uint32_t dst = base + (kv ? Z::V_OFF : Z::K_OFF) + c_st * Z::TILE + lane * page * 128;
+        if (lane == 0) mbar_expect_tx(full, Z::TILE);
+        __syncwarp();
+        if (lane < per_tile && !(k.inject_lost_load && kv)) {
+          const int at = p >= 0 ? ((p * 2 + kv) * a.g.Hkv + g.head) * page + in_page : k.rows_total;
+#pragma unroll
+          for (int cb = 0; cb < Z::CB; ++cb) tma_load(dst + cb * KV_BLOCK, &map, full, cb * 64, at);
+        }
+        __syncwarp();
+        ++n_own;
+        if (++c_st == n_stages) { c_st = 0; c_ph ^= 1; }
+        // (behind the first tile: keys need not wait for the last segment to give its queries' place up)
+        if (ok && t == 0 && !kv) load_queries();
+      }
+    } else {
+      // -------------------------------------------------------------- products
+      // The whole warp walks, one elected lane issues (operands stay warp-uniform).  The tensor core takes 512 cycles for the
+      // eight products of a step: what the warp does between two steps has to fit behind them, so stages and phases are
+      // counted along and a wait that has nothing to wait for costs one poll.
+      const uint32_t slot = warp - WARP_MMA;
+      const int steps = halves ? g.n : (g.n - (int)slot + 1) >> 1;
+      // One lane walks and issues.  The tensor core needs about 700 cycles for a step's products of one slot; what the lane does
+      // between them has to stay well below that, or the other slot's products alone cannot keep it busy.
+      if (elected && ok) {
+        const uint32_t bars = base + Z::CTL_OFF;
+        auto at = [&](const void* b) { return bars + (uint32_t)(reinterpret_cast<const char*>(b) - reinterpret_cast<const char*>(&c)); };
+        auto pass = [&](uint32_t b, uint32_t phase) { if (!mbar_try_wait(b, phase)) ok = mbar_wait(b, phase, abort_flag); };
+        const uint32_t b_s = at(&c.s_full[0][0]) + slot * 16, b_p = at(&c.p_full[0][0]) + slot * 16, b_o = at(&c.pv_done[0][0]) + slot * 16;
+        const uint32_t b_kf = at(&c.kv_full[0][0]), b_vf = at(&c.kv_full[1][0]), b_ke = at(&c.kv_empty[0][0]), b_ve = at(&c.kv_empty[1][0]);
+        const uint32_t d_s = tm + slot * S_COLS, d_o = tm + 2 * S_COLS + slot * HD;
+        const uint64_t q = q_desc + (uint64_t)(slot * (Z::Q_TILE >> 4));
+        const int stride = halves ? 1 : 2;
+        // stage and phase of the slot's next keys and values
+        const int skip = halves ? 0 : (int)slot, t0 = tiles_before + skip;
+        uint32_t k_st = t0 % Z::NK, k_ph = (t0 / Z::NK) & 1, v_st = t0 % Z::NV, v_ph = (t0 / Z::NV) & 1;
+        int keys = g.s.total - (g.tile0 + skip) * KT;     // keys from the step's first one on
+        auto advance = [&](uint32_t& st, uint32_t& ph, uint32_t n) {
+          st += stride;
+          if (st >= n) { st -= n; ph ^= 1; }
+        };
+        // a stage is free after two arrivals: one of each slot, or both of the one slot that uses the tile
+        auto release = [&](uint32_t b) {
+          umma_commit(b);
+          if (!halves) umma_commit(b);
+        };
+        pass(at(&c.q_full), par);
+        if (steps == 0) mbar_arrive(at(&c.q_empty));
+#pragma unroll 1
+        for (int y = -2; y < steps; ++y) {
+          // ---- O += P V of step y, then S = Q K^T of step y + 2 over the P that was read: one thread's products run in order.
+          // The slot's softmax works on step y + 1 meanwhile.  (Phases run on over the segments: n_own steps before this one.)
+          const uint32_t buf = (n_own + y) & 1;
+          if (y >= 0) {
+            if (y == 0) {
+              if (seg > 0) pass(at(&c.o_free), par ^ 1);
+              if (steps <= 2) umma_commit(at(&c.q_empty));   // (see Ctl; with more steps, behind the last first product)
+            }
+            pass(b_vf + v_st * 8, v_ph);
+            pass(b_p + buf * 8, ((n_own + y) >> 1) & 1);
+            if (!ok) break;
+            tc_fence_after();
+            const uint32_t p = d_s + buf * KT, acc = y > 0;
+            const uint64_t v = v_desc + (uint64_t)(v_st * (Z::TILE >> 4));
+            if (keys >= KT) {
+              umma_bf16_ts(d_o, p, v, idesc_o, acc);
+#pragma unroll
+              for (int ks = 1; ks < KT / 16; ++ks)        // 16 keys = 2048 bytes further each
+                umma_bf16_ts(d_o, p + ks * 8, v + (uint64_t)(ks * 128), idesc_o, 1u);
+            } else {
+#pragma unroll 1
+              for (int ks = 0; ks * 16 < keys; ++ks) umma_bf16_ts(d_o, p + ks * 8, v + (uint64_t)(ks * 128), idesc_o, ks ? 1u : acc);
+            }
+            umma_commit(b_o + buf * 8);
+            release(b_ve + v_st * 8);
+            advance(v_st, v_ph, Z::NV);
+            keys -= stride * KT;
+          }
+          if (y + 2 < steps) {
+            pass(b_kf + k_st * 8, k_ph);
+            if (!ok) break;
+            tc_fence_after();
+            const uint32_t d = d_s + buf * KT;
+            const uint64_t kd = k_desc + (uint64_t)(k_st * (Z::TILE >> 4));
+#pragma unroll
+            for (int cb = 0; cb < Z::CB; ++cb)
+#pragma unroll
+              for (int kk = 0; kk < 4; ++kk)
+                umma_bf16(d, q + (uint64_t)(cb * (BLOCK >> 4) + ROW16 * kk), kd + (uint64_t)(cb * (KV_BLOCK >> 4) + ROW16 * kk),
+                          idesc_s, (cb | kk) ? 1u : 0u);
+            umma_commit(b_s + buf * 8);
+            release(b_ke + k_st * 8);
+            advance(k_st, k_ph, Z::NK);
+            if (y >= 0 && y + 3 == steps) umma_commit(at(&c.q_empty));
+          }
+        }
+      }
+      n_own += steps;
+      __syncwarp();
     }
+    tiles_before += g.n;
   }
 
+  if (*abort_flag) {
+    // copies and products under way must end before the CTA's shared memory and TMEM go away
+    const uint64_t t0 = global_ns();
+    if (warp == WARP_KEYS || warp == WARP_VALUES) {
+      const int kv = warp == WARP_VALUES, n = kv ? Z::NV : Z::NK;
+      for (int i = n_own > n ? n_own - n : 0; i < n_own; ++i)
+        while (!mbar_try_wait(bar(c.kv_full[kv][i % n]), (uint32_t)((i / n) & 1)) && global_ns() - t0 < WAIT_LIMIT_NS / 2)
+          __nanosleep(64);
+    } else if (elected) {
+      umma_commit(bar(c.drain[warp - WARP_MMA]));
+      while (!mbar_try_wait(bar(c.drain[warp - WARP_MMA]), 0) && global_ns() - t0 < WAIT_LIMIT_NS / 2) __nanosleep(64);
+    }
+  }
+  if (blockIdx.x == 0 && warp == WARP_KEYS)
+    for (int b = lane; b < a.batch; b += 32)
+      if (seq_work(k, b).bad) raise_status(a.status, POSS_E_INVALID);
   tc_fence_before();
   __syncthreads();
   if (warp == WARP_MMA) tmem_dealloc(tm, TMEM_COLS);
@@ -715,38 +824,46 @@ __global__ void __launch_bounds__(N_THREADS, 1) k_paged_attn_tc(const __grid_con
 template <int HD>
 __global__ void __launch_bounds__(256) k_paged_attn_tc_merge(const TcArgs k, int ctas, int max_groups) {
   constexpr int NV = HD / 32;                             // float4 per thread
-  __shared__ long long s_total, s_before;
+  __shared__ uint32_t s_total, s_before;
   pdl_enter(POSS_K_PAGED_ATTN_COMBINE);
   const PagedAttnArgs& a = k.a;
   const int b = blockIdx.z, head = blockIdx.y / max_groups, group = blockIdx.y - head * max_groups;
-  const SeqWork s = seq_work(a, b);
-  if (group >= s.groups || group * ITEM_ROWS + (int)blockIdx.x * 32 >= s.nq) return;
+  const SeqWork s = seq_work(k, b);
+  // line rr of the item: slot, tree row and head
+  const int rr = blockIdx.x * 32 + (threadIdx.x & 31), slice = threadIdx.x >> 5, line = rr % QR;
+  const int in_slot = line / a.G, r = (2 * group + rr / QR) * k.slot_rows + in_slot, qh = line - in_slot * a.G;
+  if (group >= s.groups) return;
   if (threadIdx.x < 32) {
-    long long total, before;
-    count_units(a, b, &total, &before);
+    uint32_t total = 0, before = 0;
+    for (int x = threadIdx.x; x < a.batch; x += 32) {
+      const uint32_t u = seq_work(k, x).units;
+      total += u;
+      if (x < b) before += u;
+    }
+    total = __reduce_add_sync(0xffffffffu, total);
+    before = __reduce_add_sync(0xffffffffu, before);
     if (threadIdx.x == 0) { s_total = total; s_before = before; }
   }
   __syncthreads();
-  const int grid = unit_grid(s_total, ctas);
-  const long long u0 = s_before + ((long long)head * s.groups + group) * s.tiles;
-  const int first = cta_of_unit(u0, s_total, grid), last = cta_of_unit(u0 + s.tiles - 1, s_total, grid);
+  const Cut cut(s_total, unit_grid(s_total, ctas));
+  const uint32_t u0 = s_before + ((uint32_t)head * s.groups + group) * s.tiles;
+  const int first = cut.cta_of(u0), last = cut.cta_of(u0 + s.tiles - 1);
   if (first == last) return;                              // written by its CTA
-  const int rr = blockIdx.x * 32 + (threadIdx.x & 31), slice = threadIdx.x >> 5, qi = group * ITEM_ROWS + rr;
-  if (qi >= s.nq) return;
+  if (in_slot >= k.slot_rows || r >= s.rows) return;
   // the first CTA's segment is its last one unless its range starts with the item; every later one's is its first
-  auto part_of = [&](int cta) {
-    return partial_of(k, HD, cta, cta == first && range_begin(first, s_total, grid) < u0 ? 1 : 0);
-  };
+  const int which = cut.begin(first) < u0 ? 1 : 0;
+  auto part_of = [&](int cta) { return partial_of(k, HD, cta, cta == first ? which : 0); };
   auto ml_of = [&](int cta) {
     return __ldcg(reinterpret_cast<const float2*>(part_of(cta) + (size_t)k.row_cap * HD) + rr);
   };
   float m = -INFINITY;
+#pragma unroll 4
   for (int i = first; i <= last; ++i) m = fmaxf(m, ml_of(i).x);
   float l = 0.f;
   float4 o[NV];
 #pragma unroll
   for (int v = 0; v < NV; ++v) o[v] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 2
+#pragma unroll 4
   for (int i = first; i <= last; ++i) {
     const float2 x = ml_of(i);
     const float4* p = reinterpret_cast<const float4*>(part_of(i));
@@ -763,9 +880,7 @@ __global__ void __launch_bounds__(256) k_paged_attn_tc_merge(const TcArgs k, int
     }
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
-  const int r = qi / a.G;
-  bf16* out = reinterpret_cast<bf16*>(a.out) +
-              (((size_t)b * a.rows + r) * a.Hq + head * a.G + (qi - r * a.G)) * HD + slice * (HD / 8);
+  bf16* out = reinterpret_cast<bf16*>(a.out) + (((size_t)b * a.rows + r) * a.Hq + head * a.G + qh) * HD + slice * (HD / 8);
 #pragma unroll
   for (int v = 0; v < NV; ++v)
     *reinterpret_cast<uint2*>(out + 4 * v) =
@@ -789,13 +904,11 @@ EncodeTiledFn encode_fn() {
 
 std::atomic<int> g_lost_loads{0};
 
-int row_cap_of(int rows, int G) {
-  const int nq = rows * G;
-  return nq >= ITEM_ROWS ? ITEM_ROWS : (nq + 31) / 32 * 32;
-}
+// lines of an item that can hold query rows: one slot's, or both
+int row_cap_of(int rows, int G) { return rows > QR / G ? 2 * QR : (rows * G + 31) / 32 * 32; }
 
 template <int HD>
-void launch(Launcher& L, const TcArgs& k0, const CUtensorMap& map, int max_pages) {
+void launch(Launcher& L, const TcArgs& k0, const CUtensorMap& map, const CUtensorMap& map_q, int max_pages) {
   using Z = Shape<HD>;
   TcArgs k = k0;
   const PagedAttnArgs& a = k.a;
@@ -812,11 +925,12 @@ void launch(Launcher& L, const TcArgs& k0, const CUtensorMap& map, int max_pages
   }
   // one CTA per SM, as many as the fullest tables can give a unit
   const long long tiles = ((long long)max_pages * a.g.page + KT - 1) / KT;
-  const int groups = (a.rows * a.G + ITEM_ROWS - 1) / ITEM_ROWS;
+  const int groups = (a.rows + 2 * k.slot_rows - 1) / (2 * k.slot_rows);
   const long long units = (long long)a.batch * a.g.Hkv * groups * tiles;
   const int sms = current_sm_count();
+  if (units >= (1ll << 31)) { L.err = POSS_E_CAPACITY; return; }
   const int ctas = units < sms ? (int)units : sms;
-  launch_pdl(L, k_paged_attn_tc<HD>, dim3(ctas), dim3(N_THREADS), smem, map, k);
+  launch_pdl(L, k_paged_attn_tc<HD>, dim3(ctas), dim3(N_THREADS), smem, map, map_q, k);
   if (tiles > 1 && L.err == POSS_OK)                      // (an item of one tile is never cut)
     launch_pdl(L, k_paged_attn_tc_merge<HD>, dim3(k.row_cap / 32, a.g.Hkv * groups, a.batch), dim3(256), 0, k, ctas,
                groups);
@@ -824,9 +938,10 @@ void launch(Launcher& L, const TcArgs& k0, const CUtensorMap& map, int max_pages
 
 }  // namespace
 
-bool paged_attn_tc_supported(const poss_page_pool& p, float scale) {
+bool paged_attn_tc_supported(const poss_page_pool& p, int G, float scale) {
+  if (G > QR) return false;
   if (p.dtype != POSS_BF16 || (p.head_dim != 64 && p.head_dim != 128)) return false;
-  if (scale == 0.f) return false;                         // -inf * 0: the SIMT kernel masks after scaling
+  if (!(scale > 0.f)) return false;                       // maxima are taken before scaling
   const int s = p.page_slots;
   return s == 16 || s == 32 || s == 64 || s == 128 || s == 256;
 }
@@ -844,8 +959,8 @@ void launch_paged_attn_tc(Launcher& L, const PagedAttnArgs& a, const void* pool,
   memset(&k, 0, sizeof(k));
   k.a = a;
   k.layer = reinterpret_cast<const bf16*>(pool) + page_offset(a.g, a.layer, 0, 0, 0);
-  k.scale_log2 = fabsf(a.scale) * 1.4426950408889634f;
-  k.q_flip = a.scale < 0.f ? 0x80008000u : 0u;
+  k.scale_log2 = a.scale * 1.4426950408889634f;
+  k.slot_rows = QR / a.G;
   k.row_cap = row_cap_of(a.rows, a.G);
   k.rows_total = a.g.n_pages * 2 * a.g.Hkv * a.g.page;
   int lost = g_lost_loads.load();
@@ -864,8 +979,24 @@ void launch_paged_attn_tc(Launcher& L, const PagedAttnArgs& a, const void* pool,
     L.err = POSS_E_CUDA;
     return;
   }
-  if (a.g.d == 128) launch<128>(L, k, map, a.g.max_pages);
-  else launch<64>(L, k, map, a.g.max_pages);
+  // The queries: columns, heads of a group, groups (KV heads), tree rows, sequences.  A box is a slot's tree rows of one KV
+  // head times 64 columns; rows behind the call's last one arrive as zeros.
+  CUtensorMap map_q;
+  {
+    const cuuint64_t row = (cuuint64_t)a.ld_q * 2;
+    cuuint64_t dim[5] = {(cuuint64_t)a.g.d, (cuuint64_t)a.G, (cuuint64_t)a.g.Hkv, (cuuint64_t)a.rows, (cuuint64_t)a.batch};
+    cuuint64_t str[4] = {(cuuint64_t)a.g.d * 2, (cuuint64_t)a.G * a.g.d * 2, row, row * a.rows};
+    cuuint32_t qbox[5] = {64, (cuuint32_t)a.G, 1, (cuuint32_t)k.slot_rows, 1};
+    cuuint32_t one[5] = {1, 1, 1, 1, 1};
+    if (encode(&map_q, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void*>(a.q), dim, str, qbox, one,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS) {
+      L.err = POSS_E_CUDA;
+      return;
+    }
+  }
+  if (a.g.d == 128) launch<128>(L, k, map, map_q, a.g.max_pages);
+  else launch<64>(L, k, map, map_q, a.g.max_pages);
 }
 
 extern "C" int poss_debug_paged_lose_load(int launches) {
