@@ -7,8 +7,8 @@
 //   a lower bound of the chunk's K-th best value comes for free with the maxima -- the least of K (8 or 16) maxima of
 //   disjoint parts of the chunk has K values at or above it -- so only the values at or above that bound (a few dozen
 //   of 8192 for logits in no order) are ever compared with one another.
-#include "poss_internal.cuh"
-#include "../../include/poss_paged.h"
+#include "paged.cuh"
+#include <float.h>
 
 POSS_TRACE_REGISTER()
 
@@ -32,6 +32,31 @@ struct BeamArgs {
 };
 
 __device__ __forceinline__ float finite_or_banned(float x) { return fabsf(x) < INFINITY ? x : -INFINITY; }
+__device__ __forceinline__ float max_nan(float a, float b, float c) {   // NaN if one of them is
+  float d;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+// two fp32 operations per instruction
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n\t.reg .b64 x, y, z, w;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\t"
+      "fma.rn.f32x2 w, x, y, z;\n\tmov.b64 {%0, %1}, w;\n\t}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 x, y, w;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tadd.rn.f32x2 w, x, y;\n\t"
+      "mov.b64 {%0, %1}, w;\n\t}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 // (value, index): greater value first, then lower index
 __device__ __forceinline__ bool before(float v, int i, float w, int j) { return v > w || (v == w && i < j); }
 
@@ -52,37 +77,57 @@ template <> struct Vec<bf16> {
   }
 };
 
+// the thread's logits of a chunk; places outside the row count as banned
 template <typename T>
-__global__ void __launch_bounds__(THREADS) k_beam_lists(BeamArgs a, const T* logits) {
-  constexpr int N = Vec<T>::N, NV = PER / N;              // values per load, loads per thread
+__device__ __forceinline__ void load_chunk(const T* base, int V, int first, float (&x)[PER]) {
+  constexpr int N = Vec<T>::N;
+  const int t0 = first + (int)threadIdx.x * N;
+  if (first >= 0 && first + CHUNK <= V) {
+#pragma unroll
+    for (int j = 0; j < PER / N; ++j)
+      Vec<T>::get(__ldcs(reinterpret_cast<const uint4*>(base + t0 + j * THREADS * N)), x + j * N);
+  } else {
+#pragma unroll
+    for (int j = 0; j < PER / N; ++j) {
+      const int i = t0 + j * THREADS * N;
+#pragma unroll
+      for (int e = 0; e < N; ++e) x[j * N + e] = i + e >= 0 && i + e < V ? to_f(base[i + e]) : -INFINITY;
+    }
+  }
+}
+
+// Block (chunk, row).
+template <typename T>
+__global__ void __launch_bounds__(THREADS, 4) k_beam_lists(BeamArgs a, const T* logits) {
+  constexpr int N = Vec<T>::N;                            // values per load
   __shared__ float s_max[16], s_sum[WARPS];
   __shared__ int s_count;
   __shared__ float s_val[MAX_CAND];
   __shared__ int s_tok[MAX_CAND];
   pdl_enter(POSS_K_BEAM_LISTS);
-  const int row = blockIdx.y, chunk = blockIdx.x, t = threadIdx.x, lane = t & 31, warp = t >> 5, K = a.K;
+  const int row = blockIdx.y, t = threadIdx.x, lane = t & 31, warp = t >> 5, K = a.K;
   const float score = a.scores[row];
   if (!(fabsf(score) < INFINITY) || (a.finished && a.finished[row])) return;   // (the second kernel skips it too)
   // Chunks start on the 16-byte boundary at or below the row's first logit: every load but those at the row's two ends
   // is whole and aligned.
   const T* const base = logits + (size_t)row * a.V;
   const int shift = (int)((reinterpret_cast<uintptr_t>(base) & 15) / sizeof(T));
+  const int chunk = blockIdx.x, first = chunk * CHUNK - shift;
   float x[PER];
+  load_chunk<T>(base, a.V, first, x);
+  // Maxima of fours and of the thread.  (-inf needs no care, +inf and NaN are rare: they show in the maximum.)
+  float q[PER / 4], m = -INFINITY;
+  auto maxima = [&] {
 #pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    const int i0 = chunk * CHUNK + (j * THREADS + t) * N - shift;              // first token of this load
-    if (i0 >= 0 && i0 + N <= a.V) {
-      Vec<T>::get(__ldcs(reinterpret_cast<const uint4*>(base + i0)), x + j * N);
-    } else {
+    for (int j = 0; j < PER / 4; ++j) q[j] = max_nan(max_nan(x[4 * j], x[4 * j + 1], x[4 * j + 2]), x[4 * j + 3], x[4 * j + 3]);
+    m = max_nan(max_nan(q[0], q[1], q[2]), max_nan(q[3], q[4], q[5]), max_nan(q[6], q[7], q[7]));
+  };
+  static_assert(PER == 32, "eight fours");
+  maxima();
+  if (!(m < INFINITY)) {
 #pragma unroll
-      for (int e = 0; e < N; ++e) x[j * N + e] = i0 + e >= 0 && i0 + e < a.V ? to_f(base[i0 + e]) : -INFINITY;
-    }
-  }
-  float m = -INFINITY;
-#pragma unroll
-  for (int j = 0; j < PER; ++j) {
-    x[j] = finite_or_banned(x[j]);
-    m = fmaxf(m, x[j]);
+    for (int j = 0; j < PER; ++j) x[j] = finite_or_banned(x[j]);
+    maxima();
   }
   // maxima of the 16 half warps
   float mh = m;
@@ -98,36 +143,50 @@ __global__ void __launch_bounds__(THREADS) k_beam_lists(BeamArgs a, const T* log
     mx = fmaxf(mx, fmaxf(lo, hi));
     bound = fminf(bound, K <= WARPS ? fmaxf(lo, hi) : fminf(lo, hi));
   }
-  // sum of exponentials below the chunk's maximum (an all-banned chunk: maximum -inf, sum 0)
-  float sum = 0.f;
-  if (mx > -INFINITY) {
-    float s4[4] = {0.f, 0.f, 0.f, 0.f};
+  bound = fmaxf(bound, -FLT_MAX);                       // banned logits never reach it
+  // candidates: values at or above the bound
+  if (m >= bound) {
 #pragma unroll
-    for (int j = 0; j < PER; ++j) s4[j & 3] += expf(x[j] - mx);
-    sum = (s4[0] + s4[1]) + (s4[2] + s4[3]);
-  }
+    for (int j4 = 0; j4 < PER; j4 += 4) {
+      if (q[j4 / 4] >= bound) {
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-  if (lane == 0) s_sum[warp] = sum;
-  // candidates: values at or above the bound (banned ones never)
-  if (m >= bound && m > -INFINITY) {
-#pragma unroll
-    for (int j = 0; j < PER; ++j) {
-      if (x[j] >= bound && x[j] > -INFINITY) {
-        const int at = atomicAdd(&s_count, 1);
-        if (at < MAX_CAND) {
-          s_val[at] = x[j];
-          s_tok[at] = chunk * CHUNK + ((j / N) * THREADS + t) * N - shift + j % N;
+        for (int j = j4; j < j4 + 4; ++j) {
+          if (x[j] >= bound) {
+            const int at = atomicAdd(&s_count, 1);
+            if (at < MAX_CAND) {
+              s_val[at] = x[j];
+              s_tok[at] = first + ((j / N) * THREADS + t) * N + j % N;
+            }
+          }
         }
       }
     }
   }
+  // Sum of exponentials below the chunk's maximum (an all-banned chunk: maximum -inf, sum 0): 2^(x log2 e - c) with c the
+  // rounded mx log2 e; what c leaves over is put right once for the sum.
+  float sum = 0.f;
+  if (mx > -INFINITY) {
+    const float L2E = 1.4426950408889634f, c = mx * L2E;
+    float2 s0 = make_float2(0.f, 0.f), s1 = s0;
+#pragma unroll
+    for (int j = 0; j < PER; j += 4) {
+      const float2 u = fma2(make_float2(x[j], x[j + 1]), make_float2(L2E, L2E), make_float2(-c, -c));
+      const float2 v = fma2(make_float2(x[j + 2], x[j + 3]), make_float2(L2E, L2E), make_float2(-c, -c));
+      s0 = add2(s0, make_float2(ex2(u.x), ex2(u.y)));   // 2^-22 relative
+      s1 = add2(s1, make_float2(ex2(v.x), ex2(v.y)));
+    }
+    sum = ((s0.x + s0.y) + (s1.x + s1.y)) * ex2(-fmaf(mx, L2E, -c));
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  if (lane == 0) s_sum[warp] = sum;
   __syncthreads();
   const size_t list = (size_t)row * a.n_chunks + chunk;
   float* val = a.cval + list * K;
   int32_t* tok = a.ctok + list * K;
-  if (t == 0) {
+  if (t == THREADS - 1) {
     float s = 0.f;
+#pragma unroll
     for (int w = 0; w < WARPS; ++w) s += s_sum[w];
     a.cmax[list] = mx;
     a.csum[list] = s;
@@ -140,37 +199,38 @@ __global__ void __launch_bounds__(THREADS) k_beam_lists(BeamArgs a, const T* log
       const float v = s_val[c];
       const int i = s_tok[c];
       int r = 0;
+#pragma unroll 4
       for (int o = 0; o < n; ++o) r += before(s_val[o], s_tok[o], v, i);
       if (r < K) { val[r] = v; tok[r] = i; }
     }
     for (int r = n + t; r < K; r += THREADS) tok[r] = -1;
-    return;
-  }
-  // Too many at or above the bound (equal logits by the hundred, or a part of the chunk banned): K rounds, each
-  // taking the best value behind the last one taken.
-  float lv = INFINITY;
-  int li = -1;
-  for (int r = 0; r < K; ++r) {
-    float bv = -INFINITY;
-    int bi = 0x7fffffff;
+  } else {
+    // Too many at or above the bound (equal logits by the hundred, or a part of the chunk banned): K rounds, each
+    // taking the best value behind the last one taken.
+    float lv = INFINITY;
+    int li = -1;
+    for (int r = 0; r < K; ++r) {
+      float bv = -INFINITY;
+      int bi = 0x7fffffff;
 #pragma unroll
-    for (int j = 0; j < PER; ++j) {
-      const int i = chunk * CHUNK + ((j / N) * THREADS + t) * N - shift + j % N;
-      if (x[j] > -INFINITY && before(lv, li, x[j], i) && before(x[j], i, bv, bi)) { bv = x[j]; bi = i; }
-    }
+      for (int j = 0; j < PER; ++j) {
+        const int i = first + ((j / N) * THREADS + t) * N + j % N;
+        if (x[j] > -INFINITY && before(lv, li, x[j], i) && before(x[j], i, bv, bi)) { bv = x[j]; bi = i; }
+      }
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      const float v = __shfl_xor_sync(0xffffffffu, bv, o);
-      const int i = __shfl_xor_sync(0xffffffffu, bi, o);
-      if (before(v, i, bv, bi)) { bv = v; bi = i; }
+      for (int o = 16; o > 0; o >>= 1) {
+        const float v = __shfl_xor_sync(0xffffffffu, bv, o);
+        const int i = __shfl_xor_sync(0xffffffffu, bi, o);
+        if (before(v, i, bv, bi)) { bv = v; bi = i; }
+      }
+      __syncthreads();
+      if (lane == 0) { s_val[warp] = bv; s_tok[warp] = bi; }
+      __syncthreads();
+      for (int w = 0; w < WARPS; ++w)
+        if (before(s_val[w], s_tok[w], bv, bi)) { bv = s_val[w]; bi = s_tok[w]; }
+      if (t == 0) { val[r] = bv; tok[r] = bi; }         // (more than MAX_CAND >= K values: there is always one)
+      lv = bv; li = bi;
     }
-    __syncthreads();
-    if (lane == 0) { s_val[warp] = bv; s_tok[warp] = bi; }
-    __syncthreads();
-    for (int w = 0; w < WARPS; ++w)
-      if (before(s_val[w], s_tok[w], bv, bi)) { bv = s_val[w]; bi = s_tok[w]; }
-    if (t == 0) { val[r] = bv; tok[r] = bi; }             // (more than MAX_CAND >= K values: there is always one)
-    lv = bv; li = bi;
   }
 }
 
@@ -197,14 +257,31 @@ __device__ __forceinline__ Cand warp_best(Cand c) {
   return c;
 }
 
-// One block per group.  The chunks' lists are sorted: a warp takes lists in turn, and its K best come out of K rounds
-// over the lanes' heads; the first warp does the same with the warps' results.
+// One block per group.  The chunks' lists are sorted, so a list whose head is worse than K other heads has nothing to give:
+//   1  the heads are dealt to 8 (or 16) parts of the block; the least of the parts' best heads is a bound that K heads reach
+//   2  the entries that reach it, from the front of each list (a few times K)
+//   3  an entry with r better ones is the (r + 1)-th of the group
+constexpr int MAX_ENTRIES = 1024;
 __global__ void __launch_bounds__(THREADS) k_beam_merge(BeamArgs a) {
   __shared__ double s_lse[KMAX];
   __shared__ int s_kind[KMAX];                            // 0: no continuation, 1: open, 2: finished
-  __shared__ Cand s_best[WARPS][KMAX];
+  __shared__ Cand s_head[16];
+  __shared__ int s_n;
+  __shared__ Cand s_entry[MAX_ENTRIES];
   pdl_enter(POSS_K_BEAM_MERGE);
   const int g = blockIdx.x, t = threadIdx.x, lane = t & 31, warp = t >> 5, K = a.K;
+  Cand none;
+  none.s = 0.0; none.beam = -1; none.tok = -1;
+  // Lists are dealt to the parts in turn: thread t takes lists l0, l0 + THREADS, ...; its first head is on its way while the
+  // sums are worked on.
+  const int lists = K * a.n_chunks, parts = K <= WARPS ? WARPS : 2 * WARPS;
+  const int part = t / (THREADS / parts), l0 = (t % (THREADS / parts)) * parts + part;
+  int pre_tok = -1;
+  float pre_val = 0.f;
+  if (l0 < lists) {
+    pre_tok = a.ctok[((size_t)g * lists + l0) * K];
+    pre_val = a.cval[((size_t)g * lists + l0) * K];
+  }
   for (int b = warp; b < K; b += WARPS) {
     const int row = g * K + b;
     const bool alive = fabsf(a.scores[row]) < INFINITY, done = a.finished && a.finished[row];
@@ -228,66 +305,96 @@ __global__ void __launch_bounds__(THREADS) k_beam_merge(BeamArgs a) {
       s_kind[b] = !alive ? 0 : done ? 2 : 1;
     }
   }
+  if (t == 0) s_n = 0;
   __syncthreads();
-  // entry e of the group: beam e / (n_chunks * K), then chunk, then place in the chunk's list
-  const int per_beam = a.n_chunks * K, total = K * per_beam;
-  auto entry = [&](int e) {
-    Cand c;
-    c.s = 0.0; c.tok = -1;
-    c.beam = e / per_beam;
-    const int i = e - c.beam * per_beam, row = g * K + c.beam;
-    const int kind = s_kind[c.beam];
-    if (kind == 1) {
-      c.tok = a.ctok[(size_t)row * per_beam + i];
-      c.s = (double)a.scores[row] + ((double)a.cval[(size_t)row * per_beam + i] - s_lse[c.beam]);
-      if (c.tok < 0) c.beam = -1;
-    } else if (kind == 2 && i == 0) {
-      c.tok = a.eos;
-      c.s = (double)a.scores[row];
-    } else {
-      c.beam = -1;
+  // entry i of list l (beam l / n_chunks); a finished beam has one, in its first list
+  auto make = [&](int l, int i, int tok, float val) {
+    Cand e = none;
+    const int b = l / a.n_chunks;
+    if (s_kind[b] == 1) {
+      if (tok >= 0) {
+        e.beam = b;
+        e.tok = tok;
+        e.s = (double)a.scores[g * K + b] + ((double)val - s_lse[b]);
+      }
+    } else if (s_kind[b] == 2 && l == b * a.n_chunks && i == 0) {
+      e.beam = b;
+      e.tok = a.eos;
+      e.s = (double)a.scores[g * K + b];
     }
-    return c;
+    return e;
   };
-  Cand last;                                              // the warp's last one taken; beam -1: none yet
-  last.beam = -1; last.s = 0.0; last.tok = -1;
-  for (int r = 0; r < K; ++r) {
-    Cand best;
-    best.beam = -1; best.s = 0.0; best.tok = -1;
-    for (int e = t; e < total; e += THREADS) {
-      const Cand c = entry(e);
-      if ((last.beam < 0 || better(last, c)) && better(c, best)) best = c;
+  auto entry = [&](int l, int i) {
+    const size_t at = ((size_t)g * lists + l) * K + i;
+    return make(l, i, a.ctok[at], a.cval[at]);            // (a beam without lists: whatever lies there is not looked at)
+  };
+  // ---- 1
+  Cand head = l0 < lists ? make(l0, 0, pre_tok, pre_val) : none;
+  const Cand first_head = head;
+  for (int l = l0 + THREADS; l < lists; l += THREADS) {
+    const Cand e = entry(l, 0);
+    if (better(e, head)) head = e;
+  }
+  for (int o = 1; o < THREADS / parts; o <<= 1) {
+    const Cand d = shfl_xor(head, o);
+    if (better(d, head)) head = d;
+  }
+  if (t % (THREADS / parts) == 0) s_head[part] = head;
+  __syncthreads();
+  Cand bound = s_head[0];                                 // (a part without heads: no bound)
+  for (int p = 1; p < parts; ++p)
+    if (better(bound, s_head[p])) bound = s_head[p];
+  // ---- 2
+  for (int l = l0; l < lists; l += THREADS) {
+    for (int i = 0; i < K; ++i) {
+      const Cand e = l == l0 && i == 0 ? first_head : entry(l, i);
+      if (e.beam < 0 || better(bound, e)) break;
+      const int at = atomicAdd(&s_n, 1);                  // (the order of the entries is of no account: no two are equal)
+      if (at < MAX_ENTRIES) s_entry[at] = e;
     }
-    best = warp_best(best);
-    if (lane == 0) s_best[warp][r] = best;
-    if (best.beam < 0) {                                  // nothing left in this warp's share
-      for (int q = r + 1; q < K; ++q)
-        if (lane == 0) s_best[warp][q] = best;
-      break;
-    }
-    last = best;
   }
   __syncthreads();
-  if (warp > 0) return;
-  // lane w < WARPS walks warp w's list
-  int head = 0;
+  const int n = s_n;
+  auto write = [&](int r, const Cand& e) {
+    const int o = g * K + r;
+    a.out_tokens[o] = e.beam < 0 ? -1 : e.tok;
+    a.out_parents[o] = e.beam < 0 ? -1 : g * K + e.beam;
+    a.out_scores[o] = e.beam < 0 ? -INFINITY : (float)e.s;
+    a.out_finished[o] = e.beam < 0 || s_kind[e.beam] == 2 || e.tok == a.eos;
+  };
+  if (n <= MAX_ENTRIES) {
+    // ---- 3
+    for (int c = t; c < n; c += THREADS) {
+      const Cand e = s_entry[c];
+      int r = 0;
+      for (int o = 0; o < n; ++o) r += better(s_entry[o], e);
+      if (r < K) write(r, e);
+    }
+    for (int r = n + t; r < K; r += THREADS) write(r, none);
+    return;
+  }
+  // Too many (a vocabulary of hundreds of chunks with equal logits): K rounds, each taking the best behind the last taken.
+  Cand last = none;
   for (int r = 0; r < K; ++r) {
-    Cand c;
-    c.beam = -1; c.s = 0.0; c.tok = -1;
-    if (lane < WARPS && head < K) c = s_best[lane][head];
-    const Cand best = warp_best(c);
-    if (c.beam >= 0 && c.beam == best.beam && c.tok == best.tok) ++head;
-    if (lane == 0) {
-      const int o = g * K + r;
-      if (best.beam < 0) {
-        a.out_tokens[o] = -1; a.out_parents[o] = -1; a.out_scores[o] = -INFINITY; a.out_finished[o] = 1;
-      } else {
-        a.out_tokens[o] = best.tok;
-        a.out_parents[o] = g * K + best.beam;
-        a.out_scores[o] = (float)best.s;
-        a.out_finished[o] = s_kind[best.beam] == 2 || best.tok == a.eos;
+    Cand best = none;
+    for (int l = t; l < lists; l += THREADS) {
+      for (int i = 0; i < K; ++i) {
+        const Cand e = entry(l, i);
+        if (e.beam < 0) break;
+        if (last.beam < 0 || better(last, e)) {
+          if (better(e, best)) best = e;
+          break;                                          // (the list's next ones are worse)
+        }
       }
     }
+    best = warp_best(best);
+    __syncthreads();
+    if (lane == 0) s_head[warp] = best;
+    __syncthreads();
+    for (int w = 0; w < WARPS; ++w)
+      if (better(s_head[w], best)) best = s_head[w];
+    if (t == 0) write(r, best);
+    last = best;                                          // (more than MAX_ENTRIES >= K entries: there is always one)
   }
 }
 

@@ -50,6 +50,7 @@ constexpr int QR = 128;                 // query rows per slot
 constexpr int N_SOFTMAX = 256;
 constexpr int N_THREADS = N_SOFTMAX + 128;
 constexpr int WARP_KEYS = 8, WARP_MMA = 9, WARP_VALUES = 11;   // WARP_MMA + slot issues the slot's products
+constexpr int MAX_CTAS = 160;           // segments of one item that the merge can hold; a device's SMs otherwise
 constexpr int GONE_RING = 32;           // tiles whose "a page is missing" is remembered: more than the copies run ahead
 constexpr int BLOCK = QR * 128;         // bytes of 128 query rows x 64 bf16
 constexpr int KV_BLOCK = KT * 128;      // bytes of a tile's 64 keys x 64 bf16
@@ -119,8 +120,12 @@ __device__ __forceinline__ SeqWork seq_work(const TcArgs& k, int b) {
   s.units = (uint32_t)s.groups * a.g.Hkv * s.tiles;       // no rows: no groups
   return s;
 }
-// CTAs that share `total` units, and the cut: the first total % grid of them take one unit more.
-__device__ __forceinline__ int unit_grid(uint32_t total, uint32_t ctas) { return (int)(total < ctas ? total : ctas); }
+// CTAs that share `total` units (MIN_UNITS each at least), and the cut: the first total % grid of them take one unit more.
+constexpr uint32_t MIN_UNITS = 2;
+__device__ __forceinline__ int unit_grid(uint32_t total, uint32_t ctas) {
+  const uint32_t n = (total + MIN_UNITS - 1) / MIN_UNITS;
+  return (int)(n < ctas ? n : ctas);
+}
 struct Cut {
   uint32_t each, more;
   __device__ __forceinline__ Cut(uint32_t total, uint32_t grid) { each = total / grid; more = total - each * grid; }
@@ -825,6 +830,7 @@ template <int HD>
 __global__ void __launch_bounds__(256) k_paged_attn_tc_merge(const TcArgs k, int ctas, int max_groups) {
   constexpr int NV = HD / 32;                             // float4 per thread
   __shared__ uint32_t s_total, s_before;
+  __shared__ float2 s_ml[MAX_CTAS][32];
   pdl_enter(POSS_K_PAGED_ATTN_COMBINE);
   const PagedAttnArgs& a = k.a;
   const int b = blockIdx.z, head = blockIdx.y / max_groups, group = blockIdx.y - head * max_groups;
@@ -849,34 +855,50 @@ __global__ void __launch_bounds__(256) k_paged_attn_tc_merge(const TcArgs k, int
   const uint32_t u0 = s_before + ((uint32_t)head * s.groups + group) * s.tiles;
   const int first = cut.cta_of(u0), last = cut.cta_of(u0 + s.tiles - 1);
   if (first == last) return;                              // written by its CTA
-  if (in_slot >= k.slot_rows || r >= s.rows) return;
   // the first CTA's segment is its last one unless its range starts with the item; every later one's is its first
   const int which = cut.begin(first) < u0 ? 1 : 0;
   auto part_of = [&](int cta) { return partial_of(k, HD, cta, cta == first ? which : 0); };
-  auto ml_of = [&](int cta) {
-    return __ldcg(reinterpret_cast<const float2*>(part_of(cta) + (size_t)k.row_cap * HD) + rr);
-  };
-  float m = -INFINITY;
-#pragma unroll 4
-  for (int i = first; i <= last; ++i) m = fmaxf(m, ml_of(i).x);
+  const bool valid = in_slot < k.slot_rows && r < s.rows;
+  // the segments' maxima and sums, eight segments at a time
+  if (valid)
+    for (int i = slice; i <= last - first; i += 8)
+      s_ml[i][rr & 31] = __ldcg(reinterpret_cast<const float2*>(part_of(first + i) + (size_t)k.row_cap * HD) + rr);
+  __syncthreads();
+  if (!valid) return;
+  const int n = last - first + 1;
   float l = 0.f;
   float4 o[NV];
 #pragma unroll
   for (int v = 0; v < NV; ++v) o[v] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-  for (int i = first; i <= last; ++i) {
-    const float2 x = ml_of(i);
-    const float4* p = reinterpret_cast<const float4*>(part_of(i));
-    float4 y[NV];
+  // Four segments' outputs are in flight at a time, the first four beside the maxima: two trips to memory in all for up to four.
+  auto load = [&](int i, float4* y) {
+    const float4* p = reinterpret_cast<const float4*>(part_of(first + (i < n ? i : n - 1)));
 #pragma unroll
     for (int v = 0; v < NV; ++v) y[v] = __ldcg(p + (size_t)(slice * NV + v) * k.row_cap + rr);
-    if (x.x == -INFINITY && x.y == 0.f) continue;         // has seen nothing
-    const float c = x.x == -INFINITY ? 1.f : ex2(x.x - m);
-    l = fmaf(x.y, c, l);
+  };
+  float4 y[4][NV];
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      o[v].x = fmaf(y[v].x, c, o[v].x); o[v].y = fmaf(y[v].y, c, o[v].y);
-      o[v].z = fmaf(y[v].z, c, o[v].z); o[v].w = fmaf(y[v].w, c, o[v].w);
+  for (int i = 0; i < 4; ++i) load(i, y[i]);
+  float m = -INFINITY;
+  for (int i = 0; i < n; ++i) m = fmaxf(m, s_ml[i][rr & 31].x);
+#pragma unroll 1
+  for (int i0 = 0; i0 < n; i0 += 4) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (i0 + i < n) {
+        const float2 x = s_ml[i0 + i][rr & 31];
+        // a segment that has seen nothing is left out (sum 0); one whose scores were all NaN is not
+        const float c = x.x == -INFINITY ? (x.y == 0.f ? 0.f : 1.f) : ex2(x.x - m);
+        if (c != 0.f) {                                   // (NaN too)
+          l = fmaf(x.y, c, l);
+#pragma unroll
+          for (int v = 0; v < NV; ++v) {
+            o[v].x = fmaf(y[i][v].x, c, o[v].x); o[v].y = fmaf(y[i][v].y, c, o[v].y);
+            o[v].z = fmaf(y[i][v].z, c, o[v].z); o[v].w = fmaf(y[i][v].w, c, o[v].w);
+          }
+        }
+      }
+      if (i0 + 4 + i < n) load(i0 + 4 + i, y[i]);
     }
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
@@ -929,7 +951,8 @@ void launch(Launcher& L, const TcArgs& k0, const CUtensorMap& map, const CUtenso
   const long long units = (long long)a.batch * a.g.Hkv * groups * tiles;
   const int sms = current_sm_count();
   if (units >= (1ll << 31)) { L.err = POSS_E_CAPACITY; return; }
-  const int ctas = units < sms ? (int)units : sms;
+  int ctas = units < sms ? (int)units : sms;
+  if (ctas > MAX_CTAS) ctas = MAX_CTAS;
   launch_pdl(L, k_paged_attn_tc<HD>, dim3(ctas), dim3(N_THREADS), smem, map, map_q, k);
   if (tiles > 1 && L.err == POSS_OK)                      // (an item of one tile is never cut)
     launch_pdl(L, k_paged_attn_tc_merge<HD>, dim3(k.row_cap / 32, a.g.Hkv * groups, a.batch), dim3(256), 0, k, ctas,
@@ -949,7 +972,8 @@ bool paged_attn_tc_supported(const poss_page_pool& p, int G, float scale) {
 size_t paged_attn_tc_workspace(const poss_page_pool& p, int batch, int rows, int Hq, int max_pages) {
   // two partials per CTA (its first and its last segment); the grid is at most the SM count
   (void)batch; (void)max_pages;
-  return (size_t)current_sm_count() * 2 * row_cap_of(rows, Hq / p.n_kv_heads) * (p.head_dim + 2) * 4;
+  const int sms = current_sm_count();
+  return (size_t)(sms < MAX_CTAS ? sms : MAX_CTAS) * 2 * row_cap_of(rows, Hq / p.n_kv_heads) * (p.head_dim + 2) * 4;
 }
 
 void launch_paged_attn_tc(Launcher& L, const PagedAttnArgs& a, const void* pool, const poss_page_pool& p) {

@@ -253,9 +253,7 @@ def test_captured_attention_replays_with_new_lengths_tables_and_contents(dtype, 
     for x in (a, c):
         x.t = {k: v for k, v in (("q", x.q.cuda()), ("pages", x.pages.cuda()), ("tables", cu(x.tables)),
                                  ("prefix", i32(x.prefix)), ("n", i32(x.n_rows)), ("mask", cu(x.mask)))}
-        from paper_2506_03566_b200.paged import _pool
-        sz = max(sz, L.load_library().poss_paged_attention_workspace_bytes(_pool(x.t["pages"])[0], 2, 9, 8,
-                                                                           x.tables.shape[1]))
+        sz = max(sz, L.poss_paged_attention_workspace_bytes(x.t["pages"], 2, 9, 8, x.tables.shape[1]))
     ws = torch.empty(sz, dtype=torch.uint8, device="cuda")
 
     def call(x):
@@ -659,7 +657,7 @@ def test_beam_selection_in_a_graph_with_a_shared_scratch_and_misaligned_rows():
     v, k = 10007, 4                                                  # odd: the rows start at every place of 16 bytes
     xs = [torch.randn(2, k, v, device="cuda") for _ in range(2)]
     s = torch.zeros(2, k, device="cuda")
-    ws = torch.empty(L.load_library().poss_beam_select_workspace_bytes(2, k, v), dtype=torch.uint8, device="cuda")
+    ws = torch.empty(L.poss_beam_select_workspace_bytes(2, k, v), dtype=torch.uint8, device="cuda")
     graphs, outs = [], []
     for x in xs:
         L.poss_beam_select(x, s, workspace=ws)
