@@ -1,9 +1,9 @@
 // Tree-masked attention over pages on the 5th-generation tensor cores (bf16, head dimension 64 or 128).
 //
 // The G = Hq / Hkv query heads of a KV head and a sequence's tree rows form one matrix of query rows (row * G + head), cut
-// into items of up to 256: (sequence, KV head, two slots of floor(128 / G) tree rows).  A unit of work is one item's product with 128 keys; the
-// units of the whole batch, in order of sequence, head, item and key, are cut into one contiguous range per CTA, one CTA
-// per SM, so that every SM streams the same number of keys however long the sequences are.  The part of an item that
+// into items of up to 256: (sequence, KV head, two slots of floor(128 / G) tree rows).  A unit of work is one item's product
+// with 64 keys; the units of the whole batch, in order of sequence, head, item and key, are cut into one contiguous range per
+// CTA, one CTA per SM, so that every SM streams the same number of keys however long the sequences are.  The part of an item that
 // falls into one CTA is a segment: one pass over its keys with the running maximum and sum of a softmax.  A segment that is
 // the whole item writes the output, any other leaves fp32 partials that a second kernel merges in key order.
 //
@@ -12,14 +12,15 @@
 //   * smaller items: both slots hold the same rows and take the even / the odd tiles; they are merged at the end.
 // Warps 0-3 / 4-7 do the softmax of slot 0 / 1 (one thread per query row), warps 8 and 11 issue the copies of keys and of
 // values, one lane each of warps 9 and 10 the products of slot 0 and 1:
-//   * copies: TMA, one box per page and 64 columns, keys and values of a tile in turn through a ring of stages.  A page that
-//     is missing or behind the last slot is read from behind the pool: zeros.  The next segment's queries come the same
-//     way while the last one ends;
+//   * copies: TMA, one box per page and 64 columns, through a ring of stages each for keys and values.  A page that is missing
+//     or behind the last slot is read from behind the pool: zeros.  The next segment's queries come the same way while the
+//     last one ends;
 //   * S = Q K^T (fp32, TMEM); the softmax thread masks its row of S in place where the tile reaches the tree, takes its
 //     maximum, writes P = 2^(s - m) as bf16 over S in TMEM; O += P V with P as the TMEM operand;
 //   * the reference maximum m moves only when a row's maximum has grown by more than 2^8 (P stays below 2^8, which bf16
 //     and the fp32 sums hold as well as 1): then the thread scales its row of O in TMEM.  Otherwise O is never touched;
-//   * while one slot's softmax runs, the other slot's products do.
+//   * a slot's scores have two buffers: while its softmax works on one tile, the products of the tile before and of the tile
+//     behind run.
 //
 // Unseen slots.  A score is replaced by -inf, so what a key holds is of no account.  A value is multiplied by an exact zero,
 // which is not enough for infinities and NaN: in tiles that reach behind the committed slots the values behind the last slot
@@ -29,8 +30,15 @@
 // The probabilities are rounded to bf16 (half a step, 2^-8): the second product's error stays near that of the output's
 // own rounding.  Sums, maxima and accumulators are fp32.
 //
-// What bounds it: with one token per sequence the read of keys and values; with 61 rows of 4 heads the products and the
-// exponentials come near to it.  DRAM traffic is the keys and values once.
+// What bounds it.  One token per sequence: the read of keys and values, once (16 sequences of up to 16384 slots, 834 MB: 137 us
+// with pages of 64, 6.1 TB/s; 155 us with pages of 16, whose boxes are 4 KB).  61 rows of 4 heads over the same slots: 246 us,
+// 830 TFLOP/s; a step of 64 keys and two slots takes 2050 cycles, of which the products alone need 1260 (M128 N64 K16 50
+// cycles, M128 N128 K16 64) and the exponentials 1024.  The rest is latency between the roles: a slot's product lane
+// spends 1000 cycles a step on barriers, commits and operand registers, the softmax 850 on its loads, maxima and barriers, and
+// both slots come to run in step, so that neither fills the other's gaps.  Measured beside it and not better: 16 softmax warps
+// of half a row each, 251 us; a lane for each kind of product in place of each slot, 257 us; three product lanes, 252 us; a late
+// start of slot 1, 247 us.  Short sequences: 18 us for 1 row over 1024 slots, 6 us of it before the first scores (lengths, pages,
+// the first copies), the rest two or three steps, partials and the merge's launch.
 //
 // Every wait is bounded; on expiry the CTA raises POSS_E_TIMEOUT, runs through its (bounded) walk without meaning, waits
 // (bounded) for its copies in flight, frees its TMEM and returns.
@@ -121,6 +129,8 @@ __device__ __forceinline__ SeqWork seq_work(const TcArgs& k, int b) {
   return s;
 }
 // CTAs that share `total` units (MIN_UNITS each at least), and the cut: the first total % grid of them take one unit more.
+// Two units and not one: partials and their merge cost more than a second step where few rows meet few keys (1 row over 1024 slots:
+// 18.0 against 19.5 us, over 100 slots 11.1 against 12.6); 61 rows over 100 slots would have 16.2 for 21.1, long ones are alike.
 constexpr uint32_t MIN_UNITS = 2;
 __device__ __forceinline__ int unit_grid(uint32_t total, uint32_t ctas) {
   const uint32_t n = (total + MIN_UNITS - 1) / MIN_UNITS;
@@ -244,6 +254,11 @@ __device__ __forceinline__ void tie32(uint32_t* r) {
   for (int i = 0; i < 32; i += 8)
     asm volatile("" : "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]), "+r"(r[i + 4]), "+r"(r[i + 5]),
                  "+r"(r[i + 6]), "+r"(r[i + 7]));
+}
+__device__ __forceinline__ uint64_t pack64(uint32_t lo, uint32_t hi) {
+  uint64_t d;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "r"(lo), "r"(hi));
+  return d;
 }
 // A from TMEM, B from shared memory
 __device__ __forceinline__ void umma_bf16_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc,
@@ -716,29 +731,28 @@ __global__ void __launch_bounds__(N_THREADS, 1) k_paged_attn_tc(const __grid_con
       }
     } else {
       // -------------------------------------------------------------- products
-      // The whole warp walks, one elected lane issues (operands stay warp-uniform).  The tensor core takes 512 cycles for the
-      // eight products of a step: what the warp does between two steps has to fit behind them, so stages and phases are
-      // counted along and a wait that has nothing to wait for costs one poll.
       const uint32_t slot = warp - WARP_MMA;
       const int steps = halves ? g.n : (g.n - (int)slot + 1) >> 1;
-      // One lane walks and issues.  The tensor core needs about 700 cycles for a step's products of one slot; what the lane does
-      // between them has to stay well below that, or the other slot's products alone cannot keep it busy.
+      // One lane walks and issues.  The tensor core needs 630 cycles for a step's products of one slot; what the lane does between
+      // them leaves it idle unless the other slot's products fill the gap.
       if (elected && ok) {
         const uint32_t bars = base + Z::CTL_OFF;
         auto at = [&](const void* b) { return bars + (uint32_t)(reinterpret_cast<const char*>(b) - reinterpret_cast<const char*>(&c)); };
-        auto pass = [&](uint32_t b, uint32_t phase) { if (!mbar_try_wait(b, phase)) ok = mbar_wait(b, phase, abort_flag); };
+        auto pass = [&](uint32_t b, uint32_t phase) { ok = mbar_wait(b, phase, abort_flag); };
         const uint32_t b_s = at(&c.s_full[0][0]) + slot * 16, b_p = at(&c.p_full[0][0]) + slot * 16, b_o = at(&c.pv_done[0][0]) + slot * 16;
         const uint32_t b_kf = at(&c.kv_full[0][0]), b_vf = at(&c.kv_full[1][0]), b_ke = at(&c.kv_empty[0][0]), b_ve = at(&c.kv_empty[1][0]);
         const uint32_t d_s = tm + slot * S_COLS, d_o = tm + 2 * S_COLS + slot * HD;
-        const uint64_t q = q_desc + (uint64_t)(slot * (Z::Q_TILE >> 4));
-        const int stride = halves ? 1 : 2;
-        // stage and phase of the slot's next keys and values
+        // (only a descriptor's lower word moves)
+        const uint32_t q_lo = (uint32_t)q_desc + slot * (Z::Q_TILE >> 4), k_lo = (uint32_t)k_desc, v_lo = (uint32_t)v_desc;
+        const uint32_t qk_hi = (uint32_t)(q_desc >> 32), v_hi = (uint32_t)(v_desc >> 32);
+        const uint32_t stride = halves ? 8 : 16;
+        // the slot's next keys and values: their stage's place among the barriers (8 times the stage), and phase
         const int skip = halves ? 0 : (int)slot, t0 = tiles_before + skip;
-        uint32_t k_st = t0 % Z::NK, k_ph = (t0 / Z::NK) & 1, v_st = t0 % Z::NV, v_ph = (t0 / Z::NV) & 1;
+        uint32_t k_at = t0 % Z::NK * 8, k_ph = (t0 / Z::NK) & 1, v_at = t0 % Z::NV * 8, v_ph = (t0 / Z::NV) & 1;
         int keys = g.s.total - (g.tile0 + skip) * KT;     // keys from the step's first one on
-        auto advance = [&](uint32_t& st, uint32_t& ph, uint32_t n) {
-          st += stride;
-          if (st >= n) { st -= n; ph ^= 1; }
+        auto advance = [&](uint32_t& x, uint32_t& ph, uint32_t n) {
+          x += stride;
+          if (x >= n * 8) { x -= n * 8; ph ^= 1; }
         };
         // a stage is free after two arrivals: one of each slot, or both of the one slot that uses the tile
         auto release = [&](uint32_t b) {
@@ -747,52 +761,64 @@ __global__ void __launch_bounds__(N_THREADS, 1) k_paged_attn_tc(const __grid_con
         };
         pass(at(&c.q_full), par);
         if (steps == 0) mbar_arrive(at(&c.q_empty));
+        // S = Q K^T of the slot's next tile, keys that have landed
+        auto scores = [&](uint32_t d, uint32_t bar_s) {
+          const uint32_t kd = k_lo + k_at * (Z::TILE >> 7);
+#pragma unroll
+          for (int cb = 0; cb < Z::CB; ++cb)
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk)
+              umma_bf16(d, pack64(q_lo + cb * (BLOCK >> 4) + ROW16 * kk, qk_hi), pack64(kd + cb * (KV_BLOCK >> 4) + ROW16 * kk, qk_hi),
+                        idesc_s, (cb | kk) ? 1u : 0u);
+          umma_commit(bar_s);
+          release(b_ke + k_at);
+          advance(k_at, k_ph, Z::NK);
+        };
+        // ---- the first two tiles' scores
 #pragma unroll 1
-        for (int y = -2; y < steps; ++y) {
-          // ---- O += P V of step y, then S = Q K^T of step y + 2 over the P that was read: one thread's products run in order.
-          // The slot's softmax works on step y + 1 meanwhile.  (Phases run on over the segments: n_own steps before this one.)
+        for (int y = 0; y < 2 && y < steps && ok; ++y) {
+          pass(b_kf + k_at, k_ph);
+          tc_fence_after();
           const uint32_t buf = (n_own + y) & 1;
-          if (y >= 0) {
-            if (y == 0) {
-              if (seg > 0) pass(at(&c.o_free), par ^ 1);
-              if (steps <= 2) umma_commit(at(&c.q_empty));   // (see Ctl; with more steps, behind the last first product)
-            }
-            pass(b_vf + v_st * 8, v_ph);
-            pass(b_p + buf * 8, ((n_own + y) >> 1) & 1);
-            if (!ok) break;
-            tc_fence_after();
-            const uint32_t p = d_s + buf * KT, acc = y > 0;
-            const uint64_t v = v_desc + (uint64_t)(v_st * (Z::TILE >> 4));
-            if (keys >= KT) {
-              umma_bf16_ts(d_o, p, v, idesc_o, acc);
-#pragma unroll
-              for (int ks = 1; ks < KT / 16; ++ks)        // 16 keys = 2048 bytes further each
-                umma_bf16_ts(d_o, p + ks * 8, v + (uint64_t)(ks * 128), idesc_o, 1u);
-            } else {
+          if (ok) scores(d_s + buf * KT, b_s + buf * 8);
+        }
+        if (seg > 0 && steps > 0) pass(at(&c.o_free), par ^ 1);
+        if (steps > 0 && steps <= 2) umma_commit(at(&c.q_empty));   // (see Ctl; with more steps, behind the last first product)
+        // ---- O += P V of step y, then S = Q K^T of step y + 2 over the P that was read: one thread's products run in order.
+        // The slot's softmax works on step y + 1 meanwhile.  (Phases run on over the segments: n_own steps before this one.)
 #pragma unroll 1
-              for (int ks = 0; ks * 16 < keys; ++ks) umma_bf16_ts(d_o, p + ks * 8, v + (uint64_t)(ks * 128), idesc_o, ks ? 1u : acc);
-            }
-            umma_commit(b_o + buf * 8);
-            release(b_ve + v_st * 8);
-            advance(v_st, v_ph, Z::NV);
-            keys -= stride * KT;
+        for (int y = 0; ok && y < steps; ++y) {
+          const uint32_t n = n_own + y, buf = n & 1, d = d_s + buf * KT;
+          const bool more = y + 2 < steps;
+          // the three barriers are asked one behind the other: an answer takes 80 cycles
+          const uint32_t v_here = mbar_try_wait(b_vf + v_at, v_ph), k_here = more ? mbar_try_wait(b_kf + k_at, k_ph) : 1u,
+                         p_here = mbar_try_wait(b_p + buf * 8, (n >> 1) & 1);
+          if (!v_here) pass(b_vf + v_at, v_ph);
+          if (!p_here && ok) pass(b_p + buf * 8, (n >> 1) & 1);
+          if (!ok) break;
+          tc_fence_after();
+          const uint32_t v = v_lo + v_at * (Z::TILE >> 7), acc = y > 0;
+          if (keys >= KT) {
+            umma_bf16_ts(d_o, d, pack64(v, v_hi), idesc_o, acc);
+#pragma unroll
+            for (int ks = 1; ks < KT / 16; ++ks)          // 16 keys = 2048 bytes further each
+              umma_bf16_ts(d_o, d + ks * 8, pack64(v + ks * 128, v_hi), idesc_o, 1u);
+          } else {
+#pragma unroll 1
+            for (int ks = 0; ks * 16 < keys; ++ks) umma_bf16_ts(d_o, d + ks * 8, pack64(v + ks * 128, v_hi), idesc_o, ks ? 1u : acc);
           }
-          if (y + 2 < steps) {
-            pass(b_kf + k_st * 8, k_ph);
-            if (!ok) break;
-            tc_fence_after();
-            const uint32_t d = d_s + buf * KT;
-            const uint64_t kd = k_desc + (uint64_t)(k_st * (Z::TILE >> 4));
-#pragma unroll
-            for (int cb = 0; cb < Z::CB; ++cb)
-#pragma unroll
-              for (int kk = 0; kk < 4; ++kk)
-                umma_bf16(d, q + (uint64_t)(cb * (BLOCK >> 4) + ROW16 * kk), kd + (uint64_t)(cb * (KV_BLOCK >> 4) + ROW16 * kk),
-                          idesc_s, (cb | kk) ? 1u : 0u);
-            umma_commit(b_s + buf * 8);
-            release(b_ke + k_st * 8);
-            advance(k_st, k_ph, Z::NK);
-            if (y >= 0 && y + 3 == steps) umma_commit(at(&c.q_empty));
+          umma_commit(b_o + buf * 8);
+          release(b_ve + v_at);
+          advance(v_at, v_ph, Z::NV);
+          keys -= (int)stride * (KT / 8);
+          if (more) {
+            if (!k_here) {
+              pass(b_kf + k_at, k_ph);
+              if (!ok) break;
+              tc_fence_after();
+            }
+            scores(d, b_s + buf * 8);
+            if (y + 3 == steps) umma_commit(at(&c.q_empty));
           }
         }
       }
