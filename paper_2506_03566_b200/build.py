@@ -1,13 +1,16 @@
-"""Builds libposs.so (the C-ABI CUDA library) in-tree with nvcc for sm_100a."""
+"""Builds libposs.so (the C-ABI CUDA library) in-tree with nvcc for sm_100a, and _paged_calls (its paged calls over torch
+tensors, a Python module of C++) beside it."""
 from __future__ import annotations
 
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libposs.so")
+CALLS = os.path.join(HERE, "_paged_calls" + sysconfig.get_config_var("EXT_SUFFIX"))
 SOURCES = ["kernels_basic.cu", "kernels_attention.cu", "kernels_attention_mma.cu", "kernels_tree.cu", "gemm_tc.cu", "attention_tc.cu", "poss_api.cu", "no_alloc.cu",
            "paged_pages.cu", "paged_attention.cu", "paged_attention_tc.cu", "beam_select.cu"]
 FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -57,6 +60,22 @@ def build(force: bool = False, verbose: bool = False) -> str:
         if r.returncode:
             sys.stderr.write(r.stdout)
             raise RuntimeError("link failed")
+    src = os.path.join(CSRC, "paged_calls.cpp")
+    if force or _stale(CALLS, [src] + headers):
+        import torch
+        root = os.path.dirname(torch.__file__)
+        cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-shared",
+               f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}", "-I" + sysconfig.get_paths()["include"],
+               "-isystem", os.path.join(root, "include"),
+               "-isystem", os.path.join(root, "include", "torch", "csrc", "api", "include"),
+               "-isystem", os.path.join(os.path.dirname(os.path.dirname(_nvcc())), "include"), src, "-o", CALLS,
+               "-L" + HERE, "-l:" + os.path.basename(OUT), "-L" + os.path.join(root, "lib"), "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda",
+               "-l:libstdc++.so.6",    # torch's own: a second copy linked in would have locales of its own
+               "-Wl,-rpath,$ORIGIN"]
+        r = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+        if r.returncode:
+            sys.stderr.write(r.stdout)
+            raise RuntimeError("g++ failed on paged_calls.cpp")
     return OUT
 
 

@@ -219,3 +219,27 @@ def test_plain_remap_keeps_its_own_promises():
                 names[i].append(step)
                 step += 1
             lens[i] += more
+
+
+def test_the_binding_names_what_is_wrong(lib):
+    """Refusals that need no device: what is no tensor, or none on the current device, and shapes that no call takes."""
+    from paper_2506_03566_b200 import (poss_beam_select, poss_paged_attention_workspace_bytes, poss_paged_tree_attention,
+                                       poss_pages_append, poss_pages_compact, poss_pages_remap)
+    pages, ints = torch.zeros(1, 3, 2, 2, 16, 64), torch.zeros(2, 3, dtype=torch.int32)
+    calls = (lambda x: poss_pages_append(x, x, x, 0, ints, ints[:, 0]),
+             lambda x: poss_paged_tree_attention(x, x, 0, ints, ints[:, 0], ints, 1.0),
+             lambda x: poss_pages_compact(x, ints, ints[:, 0], ints, ints[:, 0]),
+             lambda x: poss_pages_remap(x, ints, ints[:, 0], ints[:, 0]))
+    for f in calls:
+        for x, word in ((pages, "current device"), (pages[0], "six dimensions"), (pages[..., ::2], "six dimensions"),
+                        (pages[:, :, :1], "six dimensions"), (pages[:, :, :1].contiguous(), "kv heads"), (pages.half(), "bf16 or fp32"), ("pages", "got str"), (None, "got NoneType")):
+            with pytest.raises(ValueError, match="kv_pages.*" + word):
+                f(x)
+    for x, word in ((torch.zeros(1, 2, 5), "current device"), (torch.zeros(2, 5), "vocab"), (torch.zeros(1, 2, 5).half(), "fp32 or bf16"),
+                    (3, "got int"), (torch.zeros(1, 2, 5).to_sparse(), "dense")):
+        with pytest.raises(ValueError, match="logits.*" + word):
+            poss_beam_select(x, torch.zeros(1, 2))
+    with pytest.raises(TypeError):
+        poss_beam_select(torch.zeros(1, 2, 5))
+    with pytest.raises(ValueError, match="kv_pages"):
+        poss_paged_attention_workspace_bytes(pages.half(), 1, 1, 2, 1)
