@@ -207,6 +207,7 @@ __global__ void __launch_bounds__(128) k_paged_attn(SimtArgs s, const T* pool) {
   }
 }
 
+constexpr int MAX_SPLITS = 64;
 // merges the ns parts of a query row in key order: one warp per query row
 template <typename T, int D>
 __global__ void __launch_bounds__(128) k_paged_attn_merge(SimtArgs s) {
@@ -219,21 +220,49 @@ __global__ void __launch_bounds__(128) k_paged_attn_merge(SimtArgs s) {
   if (qi >= n.rows * a.G) return;
   const size_t step = (size_t)QB * (D + 2);
   const float* p = s.part + (((size_t)b * gridDim.y + blockIdx.y) * s.ns * QB + row) * (D + 2);
-  float mx = -INFINITY;
-  for (int i = 0; i < s.ns; ++i) mx = fmaxf(mx, p[i * step]);
+  // Lane i has the maximum and the sum of parts i and 32 + i, and their weights; a part that has seen nothing is left out (its sum is
+  // zero; one whose scores were all NaN is not).
+  static_assert(MAX_SPLITS == 64, "two parts per lane");
+  float m[2], w[2], mx = -INFINITY, l = 0.f;
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    const int i = lane + 32 * x;
+    m[x] = i < s.ns ? p[i * step] : -INFINITY;
+    w[x] = i < s.ns ? p[i * step + 1] : 0.f;
+    mx = fmaxf(mx, m[x]);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
   const float off = mx == -INFINITY ? 0.f : mx;
-  float l = 0.f, o[D / 32];
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    const bool nothing = m[x] == -INFINITY && w[x] == 0.f;
+    const float c = nothing ? 0.f : m[x] == -INFINITY ? 1.f : exp2f(m[x] - off);
+    l = nothing ? l : fmaf(w[x], c, l);
+    w[x] = nothing ? -1.f : c;                            // (a weight that no part has)
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+  float o[D / 32];
 #pragma unroll
   for (int e = 0; e < D / 32; ++e) o[e] = 0.f;
-  for (int i = 0; i < s.ns; ++i) {
-    const float mi = p[i * step];
-    const float li = p[i * step + 1];
-    // a part that has seen nothing is left out (its sum is zero; one whose scores were all NaN is not)
-    if (mi == -INFINITY && li == 0.f) continue;
-    const float c = mi == -INFINITY ? 1.f : exp2f(mi - off);
-    l = fmaf(li, c, l);
+  // eight parts' outputs are on their way at a time
+  for (int i0 = 0; i0 < s.ns; i0 += 8) {
+    float y[8][D / 32];
 #pragma unroll
-    for (int e = 0; e < D / 32; ++e) o[e] = fmaf(p[i * step + 2 + lane + 32 * e], c, o[e]);
+    for (int i = 0; i < 8; ++i) {
+      const float* part = p + (i0 + i < s.ns ? i0 + i : i0) * step + 2 + lane;
+#pragma unroll
+      for (int e = 0; e < D / 32; ++e) y[i][e] = part[32 * e];
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float c = __shfl_sync(0xffffffffu, i0 < 32 ? w[0] : w[1], (i0 + i) & 31);
+      if (i0 + i < s.ns && c >= 0.f) {
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e) o[e] = fmaf(y[i][e], c, o[e]);
+      }
+    }
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
   const int r = qi / a.G;
@@ -249,7 +278,7 @@ int simt_splits(long long blocks, long long slots) {
   long long ns = (SIMT_BLOCKS + blocks - 1) / blocks;
   const long long tiles = (slots + KB - 1) / KB;
   if (ns > tiles) ns = tiles;
-  if (ns > 64) ns = 64;
+  if (ns > MAX_SPLITS) ns = MAX_SPLITS;
   return ns < 1 ? 1 : (int)ns;
 }
 

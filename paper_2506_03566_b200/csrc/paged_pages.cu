@@ -82,11 +82,11 @@ __global__ void __launch_bounds__(256) k_pages_compact(PageGeo g, char* pool, co
   pdl_enter(POSS_K_PAGES_COMPACT);
   const int b = blockIdx.y, layer = blockIdx.x >> 1, kv = blockIdx.x & 1, t = threadIdx.x;
   const int prefix = prefix_len[b], a = n_accepted[b];
+  const int32_t* pb = path + (size_t)b * (POSS_MAX_DEPTH + 1);
+  const int from = t < POSS_MAX_DEPTH ? pb[t + 1] : 0, before = t && t < POSS_MAX_DEPTH ? pb[t] : 0;   // (one trip with the lengths)
   const long long slots = (long long)g.max_pages * g.page;
   bool ok = prefix >= 0 && a >= 0 && a <= POSS_MAX_DEPTH && (long long)prefix + a < slots;
   if (ok && t < a) {
-    const int32_t* pb = path + (size_t)b * (POSS_MAX_DEPTH + 1);
-    const int from = pb[t + 1], before = t ? pb[t] : 0;
     ok = from > before && (long long)prefix + from < slots;
     if (ok) {
       const int32_t* table = g.tables + (size_t)b * g.max_pages;
