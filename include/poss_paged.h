@@ -64,9 +64,9 @@ POSS_API size_t poss_paged_attention_workspace_bytes(const poss_page_pool* pool,
  * each).  Output rows behind n_rows[b] are left as they were; a row that sees nothing becomes zeros.  What is not seen
  * has no influence, whatever it holds (infinities and NaN too).  A missing page's slots count as unseen, a sequence
  * with lengths out of range has no rows (status).
- * rows <= POSS_MAX_ROWS; batch * n_kv_heads * ceil(rows * (query heads per KV head) / 256) * ceil(max_pages * page_slots
- * / 128) < 2^31.  bf16 with head dimension 64 or 128 and a page size of 16, 32, 64, 128 or 256 slots runs on
- * the tensor cores; the probabilities enter the second product rounded to bf16 there, sums and the output's
+ * out must not overlap q.  rows <= POSS_MAX_ROWS.  bf16 with head dimension 64 or 128, a page size of 16, 32, 64, 128 or
+ * 256 slots, at most 128 query heads per KV head (G) and a positive scale runs on the tensor cores, where batch * n_kv_heads *
+ * ceil(rows / (2 * floor(128 / G))) * ceil(max_pages * page_slots / 64) < 2^31; the probabilities enter the second product rounded to bf16 there, sums and the output's
  * accumulation are fp32.  How the keys are cut, and so the last bits of a result, depends on the whole batch's
  * lengths; equal calls give equal bits.  Errors: INVALID, SHAPE, CAPACITY, WORKSPACE (too small, not 256-byte
  * aligned), CUDA. */
@@ -80,7 +80,7 @@ POSS_API int poss_paged_tree_attention(const poss_page_pool* pool, int layer, co
  * path[b][k] moves to prefix_len[b] + k for k = 1 .. n_accepted[b]; out_len[b] (int32[batch]) = prefix_len[b] +
  * n_accepted[b] + 1, the slots committed then (the tree's root among them).  path int32[batch][POSS_MAX_DEPTH + 1],
  * n_accepted int32[batch]: the outputs of poss_verify_accept / poss_verify_sample, one row per sequence; path[b][k] is
- * increasing in k.  The slots must lie in pages that no other sequence holds.  A sequence with a length, an n_accepted
+ * increasing in k.  The slots must lie in pages that no other sequence holds; out_len must not overlap an input.  A sequence with a length, an n_accepted
  * (0 .. POSS_MAX_DEPTH) or a path out of order or range, or without a page that it needs, keeps its slots and gets
  * out_len = prefix_len (status).  Surplus pages stay in the table: poss_pages_remap gives them back. */
 POSS_API int poss_pages_compact(const poss_page_pool* pool, void* kv_pages, const int32_t* tables, int max_pages, int batch,
@@ -100,7 +100,8 @@ POSS_API size_t poss_pages_remap_workspace_bytes(const poss_page_pool* pool, int
  * take these in order, and one that meets a page with other holders left takes a fresh page instead, with the kept
  * slots copied in all layers; needed pages that the parent lacks are fresh too.  Fresh pages are the lowest-numbered
  * ones without a holder (those given up by this very call included), in order of sequence and place.
- * out_tables int32[n_after][max_pages] and out_refs int32[n_pages] must not overlap the inputs.  out_free int32[1] =
+ * out_tables int32[n_after][max_pages], out_refs int32[n_pages], out_len and out_free must not overlap the inputs nor each
+ * other.  out_free int32[1] =
  * pages without a holder afterwards.  If fewer pages are free than needed, out_free is minus the number that is
  * missing, out_refs equals refs, out_tables, out_len and the pool are left as they were.
  * A parent >= n_before, a length or room out of range or beyond max_pages, or a table entry >= n_pages: that sequence
@@ -126,6 +127,7 @@ POSS_API size_t poss_beam_select_workspace_bytes(int batch, int beams, int vocab
  * index group * beams + beam of the beam that it continues (parents for poss_pages_remap), whether it is finished now
  * (its beam was, or the token is eos; eos < 0: only the former), the new score.  With fewer continuations than beams the rest is token -1, parent
  * -1, score -inf, finished 1.  Scores are compared in 64 bits; the sum of exponentials is a sum of fp32 terms.
+ * out_scores may be scores and out_finished finished (in place); the outputs overlap no input and no other output else.
  * 1 <= beams <= POSS_MAX_TOPK, eos < vocab (with `finished` given, eos >= 0).  Errors: INVALID, CAPACITY, WORKSPACE. */
 POSS_API int poss_beam_select(const void* logits, int dtype, int batch, int beams, int vocab, const float* scores,
                      const int32_t* finished, int eos, int32_t* out_tokens, int32_t* out_parents, float* out_scores,

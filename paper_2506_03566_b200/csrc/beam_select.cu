@@ -448,6 +448,15 @@ int poss_beam_select(const void* logits, int dtype, int batch, int beams, int vo
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) ||
       workspace_bytes < poss_beam_select_workspace_bytes(batch, beams, vocab))
     return POSS_E_WORKSPACE;
+  // in place or apart: a group's scores are read before they are written, another group's may not have been
+  const size_t n = (size_t)batch * beams * 4;
+  auto crossed = [&](const void* o, const void* in, bool in_place) { return overlap(o, n, in, n) && !(in_place && o == in); };
+  const void* const outs[4] = {out_tokens, out_parents, out_scores, out_finished};
+  for (int i = 0; i < 4; ++i) {
+    if (crossed(outs[i], scores, i == 2) || crossed(outs[i], finished, i == 3)) return POSS_E_INVALID;
+    for (int j = 0; j < i; ++j)
+      if (overlap(outs[i], n, outs[j], n)) return POSS_E_INVALID;
+  }
   int64_t launches = 0;
   Launcher L{reinterpret_cast<cudaStream_t>(stream), &launches, POSS_OK};
   BeamArgs a;

@@ -63,6 +63,11 @@ inline PageGeo page_geo(const poss_page_pool* p, const int32_t* tables, int max_
   g.tables = tables; g.max_pages = max_pages;
   return g;
 }
+// do two arrays of na and nb bytes share some (a missing one shares none)
+inline bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return a && b && na && nb && x < y + nb && y < x + na;
+}
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 // SMs of the current device (148 when it cannot be asked: a grid size, nothing else depends on it)

@@ -350,6 +350,9 @@ int poss_paged_tree_attention(const poss_page_pool* pool, int layer, const void*
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) ||
       workspace_bytes < poss_paged_attention_workspace_bytes(pool, batch, rows, n_q_heads, max_pages))
     return POSS_E_WORKSPACE;
+  // one block's queries may be read while another's rows are written
+  const size_t row = (size_t)n_q_heads * pool->head_dim * es, n = (size_t)batch * rows;
+  if (overlap(out, n * row, q, (n - 1) * ld_q * es + row)) return POSS_E_INVALID;
   int64_t launches = 0;
   Launcher L{reinterpret_cast<cudaStream_t>(stream), &launches, POSS_OK};
   PagedAttnArgs a;

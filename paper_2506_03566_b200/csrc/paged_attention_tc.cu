@@ -956,7 +956,7 @@ std::atomic<int> g_lost_loads{0};
 int row_cap_of(int rows, int G) { return rows > QR / G ? 2 * QR : (rows * G + 31) / 32 * 32; }
 
 template <int HD>
-void launch(Launcher& L, const TcArgs& k0, const CUtensorMap& map, const CUtensorMap& map_q, int max_pages) {
+void launch(Launcher& L, const TcArgs& k0, const CUtensorMap& map, const CUtensorMap& map_q, long long units, long long tiles, int groups) {
   using Z = Shape<HD>;
   TcArgs k = k0;
   const PagedAttnArgs& a = k.a;
@@ -972,11 +972,7 @@ void launch(Launcher& L, const TcArgs& k0, const CUtensorMap& map, const CUtenso
     if (attr) *attr = true;
   }
   // one CTA per SM, as many as the fullest tables can give a unit
-  const long long tiles = ((long long)max_pages * a.g.page + KT - 1) / KT;
-  const int groups = (a.rows + 2 * k.slot_rows - 1) / (2 * k.slot_rows);
-  const long long units = (long long)a.batch * a.g.Hkv * groups * tiles;
   const int sms = current_sm_count();
-  if (units >= (1ll << 31)) { L.err = POSS_E_CAPACITY; return; }
   int ctas = units < sms ? (int)units : sms;
   if (ctas > MAX_CTAS) ctas = MAX_CTAS;
   launch_pdl(L, k_paged_attn_tc<HD>, dim3(ctas), dim3(N_THREADS), smem, map, map_q, k);
@@ -1003,6 +999,10 @@ size_t paged_attn_tc_workspace(const poss_page_pool& p, int batch, int rows, int
 }
 
 void launch_paged_attn_tc(Launcher& L, const PagedAttnArgs& a, const void* pool, const poss_page_pool& p) {
+  const long long tiles = ((long long)a.g.max_pages * a.g.page + KT - 1) / KT;
+  const int groups = (a.rows + 2 * (QR / a.G) - 1) / (2 * (QR / a.G));
+  const long long units = (long long)a.batch * a.g.Hkv * groups * tiles;
+  if (units >= (1ll << 31)) { L.err = POSS_E_CAPACITY; return; }
   EncodeTiledFn encode = encode_fn();
   if (!encode) { L.err = POSS_E_CUDA; return; }
   TcArgs k;
@@ -1045,8 +1045,8 @@ void launch_paged_attn_tc(Launcher& L, const PagedAttnArgs& a, const void* pool,
       return;
     }
   }
-  if (a.g.d == 128) launch<128>(L, k, map, map_q, a.g.max_pages);
-  else launch<64>(L, k, map, map_q, a.g.max_pages);
+  if (a.g.d == 128) launch<128>(L, k, map, map_q, units, tiles, groups);
+  else launch<64>(L, k, map, map_q, units, tiles, groups);
 }
 
 extern "C" int poss_debug_paged_lose_load(int launches) {

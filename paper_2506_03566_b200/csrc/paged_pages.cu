@@ -394,6 +394,11 @@ int poss_pages_compact(const poss_page_pool* pool, void* kv_pages, const int32_t
   if (rc != POSS_OK) return rc;
   if (!kv_pages || !tables || !prefix_len || !path || !n_accepted || !out_len || !aligned16(kv_pages))
     return POSS_E_INVALID;
+  // every block reads the lengths, one of each sequence writes the new one
+  const size_t n = (size_t)batch * 4;
+  if (overlap(out_len, n, prefix_len, n) || overlap(out_len, n, n_accepted, n) ||
+      overlap(out_len, n, path, n * (POSS_MAX_DEPTH + 1)) || overlap(out_len, n, tables, n * max_pages))
+    return POSS_E_INVALID;
   int64_t launches = 0;
   Launcher L{reinterpret_cast<cudaStream_t>(stream), &launches, POSS_OK};
   const PageGeo g = page_geo(pool, tables, max_pages);
@@ -432,6 +437,14 @@ int poss_pages_remap(const poss_page_pool* pool, void* kv_pages, const int32_t* 
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) ||
       workspace_bytes < poss_pages_remap_workspace_bytes(pool, n_before, n_after, max_pages))
     return POSS_E_WORKSPACE;
+  // the inputs are read while the outputs are written
+  const size_t pages = (size_t)pool->n_pages * 4, place = (size_t)max_pages * 4, n0 = (size_t)n_before * 4, n1 = (size_t)n_after * 4;
+  const struct { const void* at; size_t bytes; } arrays[] = {
+      {out_tables, n1 * max_pages}, {out_refs, pages}, {out_len, n1}, {out_free, 4},      // written
+      {tables, place * n_before}, {refs, pages}, {seq_len, n0}, {parents, n1}, {room, n1}};
+  for (int i = 0; i < 4; ++i)
+    for (int j = i + 1; j < 9; ++j)
+      if (overlap(arrays[i].at, arrays[i].bytes, arrays[j].at, arrays[j].bytes)) return POSS_E_INVALID;
   int64_t launches = 0;
   Launcher L{reinterpret_cast<cudaStream_t>(stream), &launches, POSS_OK};
   RemapArgs a;

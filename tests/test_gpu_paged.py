@@ -772,3 +772,139 @@ def test_rounds_of_drafted_trees_over_pages():
             for s in range(n):
                 assert torch.equal(pages[0, int(tables[b][s // page]), :, :, s % page], flat[b][0, :, :, s])
     assert int(status) == 0 and int(refs.sum()) == sum(-(-int(n) // page) for n in lens.tolist())
+
+
+# ------------------------------------------------------------------ what the cut of the work over the SMs can meet
+@pytest.mark.parametrize("dtype,hq,hkv,d,page,prefix,rows,n_rows", [
+    (BF, 3, 1, 128, 16, [3000, 0], 5, [5, 4]),                    # three heads to a key head, one item over many SMs
+    (BF, 7, 1, 64, 64, [1500, 2], 40, [40, 11]),                  # seven: slots of 18 rows, three items
+    (BF, 130, 1, 64, 16, [70], 2, None),                          # more heads to a key head than a slot has rows
+    (BF, 128, 1, 128, 16, [333], 3, None),                        # a slot per row
+    (BF, 4, 2, 64, 128, [190, 64, 63, 0], 70, [70, 1, 65, 70]),   # trees over page and tile ends
+    (BF, 4, 2, 128, 256, [250, 511], 128, [128, 100]),
+    (BF, 8, 2, 128, 16, [64 * i + j for i in range(8) for j in (-1 + (i == 0), 0, 1)], 2, None),   # all around the tiles
+])
+def test_attention_over_uneven_cuts(dtype, hq, hkv, d, page, prefix, rows, n_rows):
+    c = Case(60, dtype, hq, hkv, d, page, prefix, rows, n_rows)
+    got = c.run()
+    assert int(c.gpu_status) == 0
+    c.check(got)
+    for _ in range(20):
+        assert torch.equal(c.run()[:, :1], got[:, :1])
+
+
+@pytest.mark.parametrize("d,batch,rows", [(64, 200, 3), (128, 33, 5), (64, 1024, 1)])
+def test_attention_of_many_short_sequences(d, batch, rows):
+    """More sequences than a warp has lanes, most with a tile or less, some without rows; a long one in their middle."""
+    rng = np.random.default_rng(61)
+    prefix = rng.integers(0, 70, batch).tolist()
+    prefix[batch // 2] = 900
+    n_rows = rng.integers(0, rows + 1, batch).tolist()
+    n_rows[batch // 2] = rows
+    c = Case(62, BF, 2, 1, d, 16, prefix, rows, n_rows)
+    fill = torch.full((batch, rows, 2, d), -3.0, dtype=BF, device="cuda")
+    got = c.run(out=fill.clone())
+    assert int(c.gpu_status) == 0
+    c.check(got)
+    for b in range(batch):
+        assert torch.equal(got[b, n_rows[b]:], fill[b, n_rows[b]:])
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_a_batch_without_rows_or_slots_writes_nothing(d):
+    c = Case(63, BF, 4, 2, d, 16, [30, 0, 7], 3, [0, 0, 0])
+    fill = torch.full((3, 3, 4, d), 2.0, dtype=BF, device="cuda")
+    assert torch.equal(c.run(out=fill.clone()), fill) and int(c.gpu_status) == 0
+
+
+@pytest.mark.parametrize("dtype,d,page", [(F32, 64, 24), (BF, 64, 16), (BF, 128, 16)])
+def test_two_attention_calls_at_once(dtype, d, page):
+    """Two streams, each with scratch of its own, many calls in flight."""
+    cases = [Case(64 + i, dtype, 8, 2, d, page, [700 - 300 * i, 33, 5], 9 + 20 * i) for i in range(2)]
+    wants = [c.want() for c in cases]
+    streams = [torch.cuda.Stream() for _ in cases]
+    args = [(c.q.cuda(), c.pages.cuda(), 0, cu(c.tables), i32(c.prefix), cu(c.mask), c.scale) for c in cases]
+    torch.cuda.synchronize()
+    outs = [[], []]
+    for _ in range(12):
+        for s, a, o in zip(streams, args, outs):
+            with torch.cuda.stream(s):
+                o.append(lib().poss_paged_tree_attention(*a))
+    torch.cuda.synchronize()
+    for c, w, o in zip(cases, wants, outs):
+        c.check(o[0], w)
+        assert all(torch.equal(x, o[0]) for x in o)
+
+
+def test_two_captured_graphs_share_scratch_in_turn():
+    """Scratch needs no initial value: graphs that use the same, replayed one behind the other, leave each other alone."""
+    cases = [Case(66 + i, BF, 8, 2, 128, 16, [900 - 500 * i, 64], 3 + 30 * i) for i in range(2)]
+    L = lib()
+    ws = torch.empty(max(L.poss_paged_attention_workspace_bytes(c.pages.cuda(), 2, c.rows, 8, c.tables.shape[1])
+                         for c in cases), dtype=torch.uint8, device="cuda")
+    graphs, outs = [], []
+    for c in cases:
+        a = (c.q.cuda(), c.pages.cuda(), 0, cu(c.tables), i32(c.prefix), cu(c.mask), c.scale)
+        out = torch.empty(2, c.rows, 8, 128, dtype=BF, device="cuda")
+        L.poss_paged_tree_attention(*a, out=out, workspace=ws)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            L.poss_paged_tree_attention(*a, out=out, workspace=ws)
+        graphs.append((g, a))
+        outs.append(out)
+    wants = [c.want() for c in cases]
+    for _ in range(3):
+        for o in outs:
+            o.fill_(9.0)
+        ws.fill_(255)                                             # (NaN wherever it is read before it is written)
+        for g, _ in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        for c, o, w in zip(cases, outs, wants):
+            c.check(o, w)
+
+
+# ------------------------------------------------------------------ beams: the selection's rare paths, and in place
+def test_beam_selection_with_more_entries_than_the_merge_ranks():
+    """One part of the merge's lists holds nothing but poor heads, so the bound keeps out none of the others' entries."""
+    torch.manual_seed(70)
+    k, v = 16, 32 * 8192 - 7
+    x = torch.randn(1, k, v, device="cuda")
+    for chunk in (15, 31):
+        x[:, :, chunk * 8192 - 8:(chunk + 1) * 8192 + 8] = -60.0
+    check_beams(x, -np.random.default_rng(71).random((1, k)).astype(np.float32))
+    x[0, 3] = 0.0                                                 # (and equal logits in one of the beams)
+    check_beams(x, np.zeros((1, k), np.float32))
+
+
+@pytest.mark.parametrize("k,v", [(4, 32003), (16, 9000), (1, 40000)])
+def test_beam_selection_in_place(k, v):
+    torch.manual_seed(72)
+    L = lib()
+    x = torch.randn(3, k, v, device="cuda")
+    s = -torch.rand(3, k, device="cuda")
+    f = (torch.rand(3, k, device="cuda") < 0.3).to(torch.int32)
+    want = L.poss_beam_select(x, s, finished=f, eos=1)
+    out = {"tokens": torch.empty_like(f), "parents": torch.empty_like(f), "scores": s, "finished": f}
+    got = L.poss_beam_select(x, s, finished=f, eos=1, out=out)
+    assert all(torch.equal(got[n], want[n]) for n in want) and got["scores"] is s
+    with pytest.raises(L.PossError):
+        L.poss_beam_select(x, s, out={**out, "tokens": out["parents"]})
+
+
+def test_outputs_over_inputs_are_refused():
+    L = lib()
+    pages = torch.zeros(1, 4, 2, 2, 16, 64, dtype=BF, device="cuda")
+    t, n = i32([[0, 1], [2, -1]]), i32([20, 3])
+    path, acc = torch.zeros(2, L.POSS_MAX_DEPTH + 1, dtype=torch.int32, device="cuda"), i32([0, 0])
+    with pytest.raises(L.PossError):
+        L.poss_pages_compact(pages, t, n, path, acc, out_len=n)
+    refs = i32([1, 1, 1, 0])
+    out = {"tables": torch.empty_like(t), "refs": torch.empty_like(refs), "seq_len": n, "n_free": i32([0])}
+    with pytest.raises(L.PossError):
+        L.poss_pages_remap(pages, t, n, refs, out=out)
+    q = torch.zeros(2, 1, 4, 64, dtype=BF, device="cuda")
+    with pytest.raises(L.PossError):
+        L.poss_paged_tree_attention(q, pages, 0, t, n, torch.ones(2, 1, 1, dtype=torch.int64, device="cuda"), 0.1, out=q)
+    assert L.poss_pages_compact(pages, t, n, path, acc).tolist() == [21, 4]

@@ -243,3 +243,33 @@ def test_the_binding_names_what_is_wrong(lib):
         poss_beam_select(torch.zeros(1, 2, 5))
     with pytest.raises(ValueError, match="kv_pages"):
         poss_paged_attention_workspace_bytes(pages.half(), 1, 1, 2, 1)
+
+
+def test_outputs_that_overlap_inputs_are_refused(lib):
+    """Everything else is in order: only the addresses meet.  (Distinct ones are used for all the others.)"""
+    at = lambda i: P + (i << 24)
+    for kw in (dict(out=at(1)), dict(out=at(1) + 4), dict(out=at(2) + 40), dict(out=at(3) - 4), dict(out=at(4))):
+        args = dict(pages=at(0), prefix=at(1), path=at(2), acc=at(3), tables=at(4), out=at(5))
+        assert compact(lib, **{**args, **kw}) == INVALID, kw
+    outs, ins = ("out_tables", "out_refs", "out_len", "free"), ("tables", "refs", "lens", "parents")
+    names = outs + ins
+    args = dict(pages=at(0), ws=at(20), **{x: at(i + 1) for i, x in enumerate(names)})
+    for o in outs:
+        for x in names:
+            if x != o:
+                assert remap(lib, **{**args, o: args[x]}) == INVALID, (o, x)
+    assert attend(lib, q=at(1), out=at(1), pages=at(0), ws=at(5), ld=512) == INVALID
+    assert attend(lib, q=at(1), out=at(1) + 5 * 1024 + 496, pages=at(0), ws=at(5), ld=512) == INVALID      # the last row's end
+    assert attend(lib, q=at(1), out=at(1) - 6 * 512 + 16, pages=at(0), ws=at(5), ld=512) == INVALID
+    b = dict(x=at(0), scores=at(1), fin=at(2), tok=at(3), par=at(4), sc=at(5), of=at(6), ws=at(7))
+    for kw in (dict(tok=at(1)), dict(par=at(2)), dict(sc=at(1) + 4), dict(sc=at(2)), dict(of=at(2) - 4), dict(of=at(1)),
+               dict(par=at(3)), dict(of=at(5) + 28)):
+        assert beam(lib, **{**b, **kw}) == INVALID, kw
+
+
+def test_attention_refuses_more_units_than_it_can_count(lib):
+    p = pool(n_pages=1 << 20, page_slots=128, head_dim=128)
+    at = lambda i: P + (i << 24)
+    args = dict(pages=at(0), tables=at(1), q=at(2), prefix=at(3), mask=at(4), out=at(40), ws=at(80), ws_bytes=1 << 40)
+    # 1024 sequences x 2 heads x 1 item x 2^20 tiles of 64 slots = 2^31
+    assert attend(lib, p, batch=1024, rows=3, hq=4, ld=512, mp=1 << 19, **args) == CAPACITY
