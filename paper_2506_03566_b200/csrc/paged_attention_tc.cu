@@ -77,28 +77,6 @@ template <int HD> struct Shape {
   static constexpr int Q_OFF = 0, K_OFF = 2 * Q_TILE, V_OFF = K_OFF + NK * TILE, CTL_OFF = V_OFF + NV * TILE;
 };
 
-// Barriers are waited for by parity, so no role may be able to fall, or run, two phases behind another on one barrier:
-//   s_full / p_full / pv_done [slot][step & 1]: S of step y + 2 is issued behind the second product of step y, which waits for
-//     P of step y -- a softmax that has seen S of step y knows that the products of step y - 2 are complete;
-//   kv_full / kv_empty [keys, values][stage]: filled in order by one warp, but copies land in any order.  A slot that uses every
-//     tile sees every phase; one that uses every other tile must meet the same stages again and no others, so that it has seen
-//     a stage's last phase itself: the rings have even lengths.  (At a segment's start all earlier phases are over: q_full
-//     follows q_empty, which follows all of the last segment's first products, and o_free all of its second ones.)
-//   q_full, q_empty, o_free: one phase per segment.  A slot without steps in a segment waits for no o_free there, but a slot
-//     with steps gives q_empty up only behind its wait for the o_free before: whoever has seen q_full of segment s + 1 knows
-//     that o_free of segment s - 1 is complete.
-struct Ctl {
-  uint64_t kv_full[2][MAX_STAGES], kv_empty[2][MAX_STAGES], q_full, q_empty, s_full[2][2], p_full[2][2], pv_done[2][2], o_free, drain[2];
-  uint32_t tmem;
-  int abort;
-  uint8_t gone[GONE_RING];              // by tile: a page of it is missing
-  unsigned long long nonfinite[2][N_SOFTMAX / 32][2];   // by parity and warp: tree slots whose values hold infinities or NaN
-  uint32_t total, offset0;              // units of the batch; the CTA's first unit inside its first sequence
-  int seq0, grid;                       // that sequence; CTAs that share the units
-  float2 ml[2][QR];                     // a slot's maximum and sum, for the merge of two slots with the same rows
-};
-static_assert(sizeof(Ctl) <= 3072, "the control block lies behind the tiles");
-
 struct TcArgs {
   PagedAttnArgs a;
   float scale_log2;                     // scale times log2 e, positive
@@ -128,6 +106,30 @@ __device__ __forceinline__ SeqWork seq_work(const TcArgs& k, int b) {
   s.units = (uint32_t)s.groups * a.g.Hkv * s.tiles;       // no rows: no groups
   return s;
 }
+// Barriers are waited for by parity, so no role may be able to fall, or run, two phases behind another on one barrier:
+//   s_full / p_full / pv_done [slot][step & 1]: S of step y + 2 is issued behind the second product of step y, which waits for
+//     P of step y -- a softmax that has seen S of step y knows that the products of step y - 2 are complete;
+//   kv_full / kv_empty [keys, values][stage]: filled in order by one warp, but copies land in any order.  A slot that uses every
+//     tile sees every phase; one that uses every other tile must meet the same stages again and no others, so that it has seen
+//     a stage's last phase itself: the rings have even lengths.  (At a segment's start all earlier phases are over: q_full
+//     follows q_empty, which follows all of the last segment's first products, and o_free all of its second ones.)
+//   q_full, q_empty, o_free: one phase per segment.  A slot without steps in a segment waits for no o_free there, but a slot
+//     with steps gives q_empty up only behind its wait for the o_free before: whoever has seen q_full of segment s + 1 knows
+//     that o_free of segment s - 1 is complete.
+struct Ctl {
+  uint64_t kv_full[2][MAX_STAGES], kv_empty[2][MAX_STAGES], q_full, q_empty, s_full[2][2], p_full[2][2], pv_done[2][2], o_free, drain[2];
+  uint32_t tmem;
+  int abort;
+  uint8_t gone[GONE_RING];              // by tile: a page of it is missing
+  unsigned long long nonfinite[2][N_SOFTMAX / 32][2];   // by parity and warp: tree slots whose values hold infinities or NaN
+  uint32_t total, offset0, skipped;     // units of the batch; the CTA's first unit inside its first sequence; units of its
+                                        // range that another CTA takes
+  int seq0, grid, whole;                // that sequence; see Plan
+  SeqWork work0;                        // its work
+  float2 ml[2][QR];                     // a slot's maximum and sum, for the merge of two slots with the same rows
+};
+static_assert(sizeof(Ctl) <= 3072, "the control block lies behind the tiles");
+
 // CTAs that share `total` units (MIN_UNITS each at least), and the cut: the first total % grid of them take one unit more.
 // Two units and not one: partials and their merge cost more than a second step where few rows meet few keys (1 row over 1024 slots:
 // 18.0 against 19.5 us, over 100 slots 11.1 against 12.6); 61 rows over 100 slots would have 16.2 for 21.1, long ones are alike.
@@ -145,17 +147,46 @@ struct Cut {
     return u < longer ? u / (each + 1) : more + (u - longer) / each;
   }
 };
-// One warp: the units of all sequences.  For up to 32 sequences every lane keeps its own one's in *mine.
-__device__ __forceinline__ uint32_t count_units(const TcArgs& k, uint32_t* mine) {
+// One warp: the units of all sequences, and how they are cut.  For up to 32 sequences every lane keeps its own one's in *mine;
+// *before: the units of the sequences before b.
+struct Plan {
+  uint32_t total;
+  int grid;                             // CTAs that share them
+  bool whole;                           // items are not cut: a CTA takes those that begin in its range
+};
+// Cutting costs the partials' way through L2 and the merge, the more the more rows there are: units that whole items may make the
+// longest range longer.  Measured cut / whole: 61 rows of 4 heads over 100 slots (2 and 3 units) 21.4 / 18.7 us, 7 ragged trees of 25
+// rows over up to 300 slots (2 and 6) 14.1 / 12.0, 16 x 61 rows over up to 500 (8 and 9) 44 / 43; 4 x 61 rows over up to 1000 (4 and 17)
+// 28 / 34, 1 row over 400 (2 and 6) 12.3 / 15.0.
+__device__ __forceinline__ uint32_t whole_extra(int row_cap) { return 2 + row_cap / 32; }
+__device__ __forceinline__ Plan make_plan(const TcArgs& k, uint32_t ctas, int b, SeqWork* mine, uint32_t* before) {
   const int lane = threadIdx.x & 31;
-  uint32_t t = 0;
-  *mine = 0;
-  for (int b = lane; b < k.a.batch; b += 32) {
-    const uint32_t u = seq_work(k, b).units;
-    if (b < 32) *mine = u;
-    t += u;
+  uint32_t t = 0, first = 0, longest = 0, shortest = 0xffffffffu;
+  mine->units = 0;
+  for (int x = lane; x < k.a.batch; x += 32) {
+    const SeqWork s = seq_work(k, x);
+    if (x < 32) *mine = s;
+    t += s.units;
+    if (x < b) first += s.units;
+    if (s.units) {
+      longest = max(longest, (uint32_t)s.tiles);
+      shortest = min(shortest, (uint32_t)s.tiles);
+    }
   }
-  return __reduce_add_sync(0xffffffffu, t);
+  Plan p;
+  p.total = __reduce_add_sync(0xffffffffu, t);
+  *before = __reduce_add_sync(0xffffffffu, first);
+  longest = __reduce_max_sync(0xffffffffu, longest);
+  shortest = __reduce_min_sync(0xffffffffu, shortest);
+  p.grid = unit_grid(p.total, ctas);
+  p.whole = false;
+  if (p.total) {
+    // the longest range if items stay whole: a share and the rest of an item; known better where all are equal
+    const uint32_t share = (p.total + p.grid - 1) / p.grid;
+    const uint32_t worst = longest == shortest ? (share + longest - 1) / longest * longest : share + longest - 1;
+    p.whole = worst <= share + whole_extra(k.row_cap);
+  }
+  return p;
 }
 
 struct Segment {
@@ -165,20 +196,21 @@ struct Segment {
 // A CTA's segments in order; every role walks them by itself.
 struct Walk {
   uint32_t u, u_end, offset;
-  int b;
-  __device__ __forceinline__ void start(const Ctl& c) {
+  int b, whole;
+  __device__ __forceinline__ void start(const Ctl& c, Segment* g) {
     u = u_end = 0;
     if ((int)blockIdx.x < c.grid) {
       const Cut cut(c.total, c.grid);
-      u = cut.begin(blockIdx.x);
+      u = cut.begin(blockIdx.x) + c.skipped;
       u_end = cut.begin(blockIdx.x + 1);
     }
     b = c.seq0;
     offset = c.offset0;
+    whole = c.whole;
+    g->s = c.work0;
   }
   __device__ __forceinline__ bool next(const TcArgs& k, Segment* g) {
-    if (u >= u_end) return false;
-    g->s = seq_work(k, b);
+    if (u >= u_end) return false;                           // (g still holds its sequence's work)
     while (offset >= g->s.units) {
       offset -= g->s.units;
       if (++b >= k.a.batch) return false;                   // (not reached: the range lies inside the batch's units)
@@ -193,7 +225,8 @@ struct Walk {
       g->head = (int)(item / (uint32_t)g->s.groups);
       g->group = (int)item - g->head * g->s.groups;
     }
-    g->n = min(g->s.tiles - g->tile0, (int)(u_end - u));
+    g->n = g->s.tiles - g->tile0;
+    if (!whole) g->n = min(g->n, (int)(u_end - u));
     u += g->n;
     offset += g->n;
     return true;
@@ -407,14 +440,17 @@ __global__ void __launch_bounds__(N_THREADS, 1) k_paged_attn_tc(const __grid_con
 
   if (warp == 0) {
     // the batch's units, and the sequence that the CTA's first one lies in
-    uint32_t u;
-    const uint32_t total = count_units(k, &u);
-    const int grid = unit_grid(total, gridDim.x);
-    if ((int)blockIdx.x < grid) {
-      uint32_t at = Cut(total, grid).begin(blockIdx.x);
+    SeqWork own;
+    uint32_t unused;
+    const Plan plan = make_plan(k, gridDim.x, 0, &own, &unused);
+    if ((int)blockIdx.x < plan.grid) {
+      uint32_t at = Cut(plan.total, plan.grid).begin(blockIdx.x);
       for (int b0 = 0; b0 < a.batch; b0 += 32) {
-        if (b0 > 0) u = b0 + lane < a.batch ? seq_work(k, b0 + lane).units : 0;
-        uint32_t x = u;
+        if (b0 > 0) {
+          own.units = 0;
+          if (b0 + lane < a.batch) own = seq_work(k, b0 + lane);
+        }
+        uint32_t x = own.units;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
           const uint32_t y = __shfl_up_sync(0xffffffffu, x, o);
@@ -424,8 +460,11 @@ __global__ void __launch_bounds__(N_THREADS, 1) k_paged_attn_tc(const __grid_con
         if (here) {
           const int first = __ffs(here) - 1;
           if (lane == first) {
+            const uint32_t off = at - (x - own.units), into = plan.whole ? off % (uint32_t)own.tiles : 0u;
             c.seq0 = b0 + first;
-            c.offset0 = at - (x - u);
+            c.work0 = own;
+            c.skipped = into ? (uint32_t)own.tiles - into : 0u;   // the item that began before
+            c.offset0 = off + c.skipped;
           }
           break;
         }
@@ -433,16 +472,17 @@ __global__ void __launch_bounds__(N_THREADS, 1) k_paged_attn_tc(const __grid_con
       }
     }
     if (lane == 0) {
-      c.total = total;
-      c.grid = grid;
+      c.total = plan.total;
+      c.grid = plan.grid;
+      c.whole = plan.whole;
     }
   }
   __syncthreads();
 
-  Walk walk;
-  walk.start(c);
-  const uint32_t u_first = walk.u;
   Segment g;
+  Walk walk;
+  walk.start(c, &g);
+  const uint32_t u_first = walk.u;
   // what a role carries from segment to segment
   bool ok = __all_sync(0xffffffffu, *abort_flag == 0);
   int tiles_before = 0;                                   // tiles of the segments before
@@ -488,28 +528,39 @@ __global__ void __launch_bounds__(N_THREADS, 1) k_paged_attn_tc(const __grid_con
         const int t = halves ? i : 2 * i + wg, key0 = (g.tile0 + t) * KT;
         const bool partly = key0 + KT > g.s.prefix;       // the tile reaches the tree
         if (partly && (!halves || wg == 0)) {
-          // values behind the last slot, and infinities and NaN of tree slots, become zeros; one thread per key
+          // values behind the last slot, and infinities and NaN of tree slots, become zeros; two threads per key
           // (once the scores are there, the slot's last values but one have been used: the stage is in this tile's turn)
           const int st = (tiles_before + t) % Z::NV;
           wait(c.s_full[wg][n_own & 1], n_own >> 1);
           wait(c.kv_full[1][st], (tiles_before + t) / Z::NV);
-          const int key = key0 + row, n16 = min(KT, (g.s.total - key0 + 15) & ~15);
-          if (ok && row < n16 && key >= g.s.prefix) {
-            uint8_t* v = smem + Z::V_OFF + st * Z::TILE + row * 128;
-            bool found = false;
-#pragma unroll 4
-            for (int j = 0; j < HD / 8; ++j) {
-              uint4* p = reinterpret_cast<uint4*>(v + (j >> 3) * KV_BLOCK + (((j & 7) ^ (row & 7)) << 4));
-              uint4 x = *p;
-              if (key >= g.s.total) {
-                *p = make_uint4(0, 0, 0, 0);
-              } else if (nonfinite2(x.x) || nonfinite2(x.y) || nonfinite2(x.z) || nonfinite2(x.w)) {
-                found = true;
-                *p = make_uint4(finite2(x.x), finite2(x.y), finite2(x.z), finite2(x.w));
+          const int kr = row % KT, key = key0 + kr, n16 = min(KT, (g.s.total - key0 + 15) & ~15);
+          if (ok && kr < n16 && key >= g.s.prefix) {
+            constexpr int N = HD / 16;                    // pieces of 16 bytes per thread
+            uint8_t* v = smem + Z::V_OFF + st * Z::TILE + kr * 128;
+            auto piece = [&](int x) {
+              const int i = (row / KT) * N + x;
+              return reinterpret_cast<uint4*>(v + (i >> 3) * KV_BLOCK + (((i & 7) ^ (kr & 7)) << 4));
+            };
+            if (key >= g.s.total) {
+#pragma unroll
+              for (int x = 0; x < N; ++x) *piece(x) = make_uint4(0, 0, 0, 0);
+            } else {
+              uint4 x[N];
+              bool found = false;
+#pragma unroll
+              for (int i = 0; i < N; ++i) x[i] = *piece(i);
+#pragma unroll
+              for (int i = 0; i < N; ++i) found |= nonfinite2(x[i].x) | nonfinite2(x[i].y) | nonfinite2(x[i].z) | nonfinite2(x[i].w);
+              if (found) {
+#pragma unroll 1
+                for (int i = 0; i < N; ++i) {
+                  const uint4 y = *piece(i);
+                  *piece(i) = make_uint4(finite2(y.x), finite2(y.y), finite2(y.z), finite2(y.w));
+                }
+                const int j = key - g.s.prefix;
+                atomicOr(&c.nonfinite[par][warp][j >> 6], 1ull << (j & 63));
               }
             }
-            const int j = key - g.s.prefix;
-            if (found) atomicOr(&c.nonfinite[par][warp][j >> 6], 1ull << (j & 63));
           }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         }
@@ -598,7 +649,7 @@ __global__ void __launch_bounds__(N_THREADS, 1) k_paged_attn_tc(const __grid_con
         const int rr = halves ? wg * QR + row : row;      // row inside the item
         const float inv = l == 0.f ? 0.f : 1.f / l;       // a row that sees nothing: zeros
         uint64_t nf_lo = 0, nf_hi = 0;
-#pragma unroll 1
+#pragma unroll
         for (int w = 0; w < N_SOFTMAX / 32; ++w) {
           nf_lo |= c.nonfinite[par][w][0];
           nf_hi |= c.nonfinite[par][w][1];
@@ -615,22 +666,18 @@ __global__ void __launch_bounds__(N_THREADS, 1) k_paged_attn_tc(const __grid_con
         bf16* const out = reinterpret_cast<bf16*>(a.out) +
                           (((size_t)g.b * a.rows + r) * a.Hq + g.head * a.G + head) * HD;
         const int col0 = halves ? 0 : wg * (HD / 2), cols = halves ? HD : HD / 2;
+        // (16 columns at a time: the code is met for the first time here, and less of it comes sooner)
 #pragma unroll 1
-        for (int j = col0; j < col0 + cols; j += 32) {
-          uint32_t o[32];
+        for (int j = col0; j < col0 + cols; j += 16) {
+          uint32_t o[16];
           if (halves) {
-            tmem_ld32(t_o + j, o);
-            tmem_wait_ld();
-            tie32(o);
+            tmem_ld16(t_o + j, reinterpret_cast<float*>(o));
           } else {
-            uint32_t o1[32];
-            tmem_ld32(t_lane + 2 * S_COLS + j, o);
-            tmem_ld32(t_lane + 2 * S_COLS + HD + j, o1);
-            tmem_wait_ld();
-            tie32(o);
-            tie32(o1);
+            uint32_t o1[16];
+            tmem_ld16(t_lane + 2 * S_COLS + j, reinterpret_cast<float*>(o));
+            tmem_ld16(t_lane + 2 * S_COLS + HD + j, reinterpret_cast<float*>(o1));
 #pragma unroll
-            for (int x = 0; x < 32; ++x) {                // (a slot left out: its accumulator may never have been written)
+            for (int x = 0; x < 16; ++x) {                // (a slot left out: its accumulator may never have been written)
               const float y0 = c0 == 0.f ? 0.f : __uint_as_float(o[x]) * c0;
               const float y1 = c1 == 0.f ? 0.f : __uint_as_float(o1[x]) * c1;
               o[x] = __float_as_uint(y0 + y1);
@@ -646,7 +693,7 @@ __global__ void __launch_bounds__(N_THREADS, 1) k_paged_attn_tc(const __grid_con
                 if (p < 0) continue;
                 const bf16* v = k.layer + page_offset(a.g, 0, p, 1, g.head) + (size_t)(slot % a.g.page) * HD + j;
 #pragma unroll
-                for (int x = 0; x < 32; ++x) {
+                for (int x = 0; x < 16; ++x) {
                   const float y = to_f(v[x]);
                   if (!(fabsf(y) < INFINITY)) o[x] = __float_as_uint(__uint_as_float(o[x]) + y);
                 }
@@ -656,7 +703,7 @@ __global__ void __launch_bounds__(N_THREADS, 1) k_paged_attn_tc(const __grid_con
           if (valid) {
             if (whole) {
 #pragma unroll
-              for (int x = 0; x < 32; x += 8) {
+              for (int x = 0; x < 16; x += 8) {
                 uint32_t w[4];
 #pragma unroll
                 for (int y = 0; y < 4; ++y)
@@ -666,7 +713,7 @@ __global__ void __launch_bounds__(N_THREADS, 1) k_paged_attn_tc(const __grid_con
             } else {
               uint4* dst = reinterpret_cast<uint4*>(part) + (size_t)(j >> 2) * k.row_cap + rr;
 #pragma unroll
-              for (int x = 0; x < 32; x += 4, dst += k.row_cap) __stcg(dst, make_uint4(o[x], o[x + 1], o[x + 2], o[x + 3]));
+              for (int x = 0; x < 16; x += 4, dst += k.row_cap) __stcg(dst, make_uint4(o[x], o[x + 1], o[x + 2], o[x + 3]));
             }
           }
         }
@@ -855,7 +902,8 @@ __global__ void __launch_bounds__(N_THREADS, 1) k_paged_attn_tc(const __grid_con
 template <int HD>
 __global__ void __launch_bounds__(256) k_paged_attn_tc_merge(const TcArgs k, int ctas, int max_groups) {
   constexpr int NV = HD / 32;                             // float4 per thread
-  __shared__ uint32_t s_total, s_before;
+  __shared__ Plan s_plan;
+  __shared__ uint32_t s_before;
   __shared__ float2 s_ml[MAX_CTAS][32];
   pdl_enter(POSS_K_PAGED_ATTN_COMBINE);
   const PagedAttnArgs& a = k.a;
@@ -866,18 +914,14 @@ __global__ void __launch_bounds__(256) k_paged_attn_tc_merge(const TcArgs k, int
   const int in_slot = line / a.G, r = (2 * group + rr / QR) * k.slot_rows + in_slot, qh = line - in_slot * a.G;
   if (group >= s.groups) return;
   if (threadIdx.x < 32) {
-    uint32_t total = 0, before = 0;
-    for (int x = threadIdx.x; x < a.batch; x += 32) {
-      const uint32_t u = seq_work(k, x).units;
-      total += u;
-      if (x < b) before += u;
-    }
-    total = __reduce_add_sync(0xffffffffu, total);
-    before = __reduce_add_sync(0xffffffffu, before);
-    if (threadIdx.x == 0) { s_total = total; s_before = before; }
+    SeqWork mine;
+    uint32_t before;
+    const Plan plan = make_plan(k, ctas, b, &mine, &before);
+    if (threadIdx.x == 0) { s_plan = plan; s_before = before; }
   }
   __syncthreads();
-  const Cut cut(s_total, unit_grid(s_total, ctas));
+  if (s_plan.whole) return;                               // nothing was cut
+  const Cut cut(s_plan.total, s_plan.grid);
   const uint32_t u0 = s_before + ((uint32_t)head * s.groups + group) * s.tiles;
   const int first = cut.cta_of(u0), last = cut.cta_of(u0 + s.tiles - 1);
   if (first == last) return;                              // written by its CTA
