@@ -86,6 +86,7 @@ struct TcArgs {
   int inject_lost_load;
   uint32_t smem_bytes;
   const bf16* layer;                    // the layer's first element
+  struct PlanOut* plan;                 // what the merge needs to know, left by the first CTA
 };
 
 // ---- the units of a sequence
@@ -147,27 +148,38 @@ struct Cut {
     return u < longer ? u / (each + 1) : more + (u - longer) / each;
   }
 };
-// One warp: the units of all sequences, and how they are cut.  For up to 32 sequences every lane keeps its own one's in *mine;
-// *before: the units of the sequences before b.
+// One warp: the units of all sequences, and how they are cut.  For up to 32 sequences every lane keeps its own one's work in *mine.
 struct Plan {
   uint32_t total;
   int grid;                             // CTAs that share them
   bool whole;                           // items are not cut: a CTA takes those that begin in its range
 };
+struct PlanOut {
+  uint32_t total;
+  int grid, whole, unused;
+  uint32_t before[POSS_MAX_PAGED_BATCH];   // units of the sequences before
+};
+__device__ __forceinline__ uint32_t inclusive_scan(uint32_t x) {
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t y = __shfl_up_sync(0xffffffffu, x, o);
+    if ((int)(threadIdx.x & 31) >= o) x += y;
+  }
+  return x;
+}
 // Cutting costs the partials' way through L2 and the merge, the more the more rows there are: units that whole items may make the
 // longest range longer.  Measured cut / whole: 61 rows of 4 heads over 100 slots (2 and 3 units) 21.4 / 18.7 us, 7 ragged trees of 25
 // rows over up to 300 slots (2 and 6) 14.1 / 12.0, 16 x 61 rows over up to 500 (8 and 9) 44 / 43; 4 x 61 rows over up to 1000 (4 and 17)
 // 28 / 34, 1 row over 400 (2 and 6) 12.3 / 15.0.
 __device__ __forceinline__ uint32_t whole_extra(int row_cap) { return 2 + row_cap / 32; }
-__device__ __forceinline__ Plan make_plan(const TcArgs& k, uint32_t ctas, int b, SeqWork* mine, uint32_t* before) {
+__device__ __forceinline__ Plan make_plan(const TcArgs& k, uint32_t ctas, SeqWork* mine) {
   const int lane = threadIdx.x & 31;
-  uint32_t t = 0, first = 0, longest = 0, shortest = 0xffffffffu;
+  uint32_t t = 0, longest = 0, shortest = 0xffffffffu;
   mine->units = 0;
   for (int x = lane; x < k.a.batch; x += 32) {
     const SeqWork s = seq_work(k, x);
     if (x < 32) *mine = s;
     t += s.units;
-    if (x < b) first += s.units;
     if (s.units) {
       longest = max(longest, (uint32_t)s.tiles);
       shortest = min(shortest, (uint32_t)s.tiles);
@@ -175,7 +187,6 @@ __device__ __forceinline__ Plan make_plan(const TcArgs& k, uint32_t ctas, int b,
   }
   Plan p;
   p.total = __reduce_add_sync(0xffffffffu, t);
-  *before = __reduce_add_sync(0xffffffffu, first);
   longest = __reduce_max_sync(0xffffffffu, longest);
   shortest = __reduce_min_sync(0xffffffffu, shortest);
   p.grid = unit_grid(p.total, ctas);
@@ -441,8 +452,7 @@ __global__ void __launch_bounds__(N_THREADS, 1) k_paged_attn_tc(const __grid_con
   if (warp == 0) {
     // the batch's units, and the sequence that the CTA's first one lies in
     SeqWork own;
-    uint32_t unused;
-    const Plan plan = make_plan(k, gridDim.x, 0, &own, &unused);
+    const Plan plan = make_plan(k, gridDim.x, &own);
     if ((int)blockIdx.x < plan.grid) {
       uint32_t at = Cut(plan.total, plan.grid).begin(blockIdx.x);
       for (int b0 = 0; b0 < a.batch; b0 += 32) {
@@ -450,12 +460,7 @@ __global__ void __launch_bounds__(N_THREADS, 1) k_paged_attn_tc(const __grid_con
           own.units = 0;
           if (b0 + lane < a.batch) own = seq_work(k, b0 + lane);
         }
-        uint32_t x = own.units;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const uint32_t y = __shfl_up_sync(0xffffffffu, x, o);
-          if (lane >= o) x += y;
-        }
+        const uint32_t x = inclusive_scan(own.units);
         const unsigned here = __ballot_sync(0xffffffffu, at < x);
         if (here) {
           const int first = __ffs(here) - 1;
@@ -475,6 +480,7 @@ __global__ void __launch_bounds__(N_THREADS, 1) k_paged_attn_tc(const __grid_con
       c.total = plan.total;
       c.grid = plan.grid;
       c.whole = plan.whole;
+      if (blockIdx.x == 0) { k.plan->total = plan.total; k.plan->grid = plan.grid; k.plan->whole = plan.whole; }
     }
   }
   __syncthreads();
@@ -888,9 +894,21 @@ __global__ void __launch_bounds__(N_THREADS, 1) k_paged_attn_tc(const __grid_con
       while (!mbar_try_wait(bar(c.drain[warp - WARP_MMA]), 0) && global_ns() - t0 < WAIT_LIMIT_NS / 2) __nanosleep(64);
     }
   }
-  if (blockIdx.x == 0 && warp == WARP_KEYS)
-    for (int b = lane; b < a.batch; b += 32)
-      if (seq_work(k, b).bad) raise_status(a.status, POSS_E_INVALID);
+  if (blockIdx.x == 0 && warp == WARP_KEYS) {
+    uint32_t before = 0;
+    for (int b0 = 0; b0 < a.batch; b0 += 32) {
+      const int b = b0 + lane;
+      uint32_t u = 0;
+      if (b < a.batch) {
+        const SeqWork s = seq_work(k, b);
+        if (s.bad) raise_status(a.status, POSS_E_INVALID);
+        u = s.units;
+      }
+      const uint32_t x = inclusive_scan(u);
+      if (b < a.batch) k.plan->before[b] = before + x - u;
+      before += __shfl_sync(0xffffffffu, x, 31);
+    }
+  }
   tc_fence_before();
   __syncthreads();
   if (warp == WARP_MMA) tmem_dealloc(tm, TMEM_COLS);
@@ -900,29 +918,22 @@ __global__ void __launch_bounds__(N_THREADS, 1) k_paged_attn_tc(const __grid_con
 // ---------------------------------------------------------------------------------------------------- merge
 // A block: 32 query rows of one item, eight threads per row.  The item's segments lie in consecutive CTAs, in key order.
 template <int HD>
-__global__ void __launch_bounds__(256) k_paged_attn_tc_merge(const TcArgs k, int ctas, int max_groups) {
+__global__ void __launch_bounds__(256) k_paged_attn_tc_merge(const TcArgs k, int max_groups) {
   constexpr int NV = HD / 32;                             // float4 per thread
-  __shared__ Plan s_plan;
-  __shared__ uint32_t s_before;
   __shared__ float2 s_ml[MAX_CTAS][32];
   pdl_enter(POSS_K_PAGED_ATTN_COMBINE);
   const PagedAttnArgs& a = k.a;
   const int b = blockIdx.z, head = blockIdx.y / max_groups, group = blockIdx.y - head * max_groups;
+  const PlanOut* const plan = k.plan;
+  const uint32_t total = __ldcg(&plan->total), before = __ldcg(&plan->before[b]);
+  const int whole = __ldcg(&plan->whole), cut_grid = __ldcg(&plan->grid);
   const SeqWork s = seq_work(k, b);
+  if (whole || group >= s.groups) return;                 // (whole: nothing was cut)
   // line rr of the item: slot, tree row and head
   const int rr = blockIdx.x * 32 + (threadIdx.x & 31), slice = threadIdx.x >> 5, line = rr % QR;
   const int in_slot = line / a.G, r = (2 * group + rr / QR) * k.slot_rows + in_slot, qh = line - in_slot * a.G;
-  if (group >= s.groups) return;
-  if (threadIdx.x < 32) {
-    SeqWork mine;
-    uint32_t before;
-    const Plan plan = make_plan(k, ctas, b, &mine, &before);
-    if (threadIdx.x == 0) { s_plan = plan; s_before = before; }
-  }
-  __syncthreads();
-  if (s_plan.whole) return;                               // nothing was cut
-  const Cut cut(s_plan.total, s_plan.grid);
-  const uint32_t u0 = s_before + ((uint32_t)head * s.groups + group) * s.tiles;
+  const Cut cut(total, cut_grid);
+  const uint32_t u0 = before + ((uint32_t)head * s.groups + group) * s.tiles;
   const int first = cut.cta_of(u0), last = cut.cta_of(u0 + s.tiles - 1);
   if (first == last) return;                              // written by its CTA
   // the first CTA's segment is its last one unless its range starts with the item; every later one's is its first
@@ -996,6 +1007,7 @@ EncodeTiledFn encode_fn() {
 
 std::atomic<int> g_lost_loads{0};
 
+constexpr size_t PLAN_BYTES = (sizeof(PlanOut) + 255) / 256 * 256;
 // lines of an item that can hold query rows: one slot's, or both
 int row_cap_of(int rows, int G) { return rows > QR / G ? 2 * QR : (rows * G + 31) / 32 * 32; }
 
@@ -1021,8 +1033,7 @@ void launch(Launcher& L, const TcArgs& k0, const CUtensorMap& map, const CUtenso
   if (ctas > MAX_CTAS) ctas = MAX_CTAS;
   launch_pdl(L, k_paged_attn_tc<HD>, dim3(ctas), dim3(N_THREADS), smem, map, map_q, k);
   if (tiles > 1 && L.err == POSS_OK)                      // (an item of one tile is never cut)
-    launch_pdl(L, k_paged_attn_tc_merge<HD>, dim3(k.row_cap / 32, a.g.Hkv * groups, a.batch), dim3(256), 0, k, ctas,
-               groups);
+    launch_pdl(L, k_paged_attn_tc_merge<HD>, dim3(k.row_cap / 32, a.g.Hkv * groups, a.batch), dim3(256), 0, k, groups);
 }
 
 }  // namespace
@@ -1036,10 +1047,10 @@ bool paged_attn_tc_supported(const poss_page_pool& p, int G, float scale) {
 }
 
 size_t paged_attn_tc_workspace(const poss_page_pool& p, int batch, int rows, int Hq, int max_pages) {
-  // two partials per CTA (its first and its last segment); the grid is at most the SM count
+  // the plan; two partials per CTA (its first and its last segment); the grid is at most the SM count
   (void)batch; (void)max_pages;
   const int sms = current_sm_count();
-  return (size_t)(sms < MAX_CTAS ? sms : MAX_CTAS) * 2 * row_cap_of(rows, Hq / p.n_kv_heads) * (p.head_dim + 2) * 4;
+  return PLAN_BYTES + (size_t)(sms < MAX_CTAS ? sms : MAX_CTAS) * 2 * row_cap_of(rows, Hq / p.n_kv_heads) * (p.head_dim + 2) * 4;
 }
 
 void launch_paged_attn_tc(Launcher& L, const PagedAttnArgs& a, const void* pool, const poss_page_pool& p) {
@@ -1052,6 +1063,8 @@ void launch_paged_attn_tc(Launcher& L, const PagedAttnArgs& a, const void* pool,
   TcArgs k;
   memset(&k, 0, sizeof(k));
   k.a = a;
+  k.plan = reinterpret_cast<PlanOut*>(a.ws);
+  k.a.ws = reinterpret_cast<char*>(a.ws) + PLAN_BYTES;
   k.layer = reinterpret_cast<const bf16*>(pool) + page_offset(a.g, a.layer, 0, 0, 0);
   k.scale_log2 = a.scale * 1.4426950408889634f;
   k.slot_rows = QR / a.G;
