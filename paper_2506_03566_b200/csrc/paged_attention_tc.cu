@@ -5,7 +5,8 @@
 // with 64 keys; the units of the whole batch, in order of sequence, head, item and key, are cut into one contiguous range per
 // CTA, one CTA per SM, so that every SM streams the same number of keys however long the sequences are.  The part of an item that
 // falls into one CTA is a segment: one pass over its keys with the running maximum and sum of a softmax.  A segment that is
-// the whole item writes the output, any other leaves fp32 partials that a second kernel merges in key order.
+// the whole item writes the output, any other leaves fp32 partials that a second kernel merges in key order.  Where items are
+// short the ranges end at items instead (Plan).
 //
 // Inside a CTA two "slots" of 128 query rows share the key tiles:
 //   * items with rows for both slots: each has its own, both use every tile (each key is read once);
@@ -31,13 +32,13 @@
 // own rounding.  Sums, maxima and accumulators are fp32.
 //
 // What bounds it.  One token per sequence: the read of keys and values, once (16 sequences of up to 16384 slots, 834 MB: 137 us
-// with pages of 64, 6.1 TB/s; 155 us with pages of 16, whose boxes are 4 KB).  61 rows of 4 heads over the same slots: 246 us,
+// with pages of 64, 6.1 TB/s; 153 us with pages of 16, whose boxes are 4 KB).  61 rows of 4 heads over the same slots: 244 us,
 // 830 TFLOP/s; a step of 64 keys and two slots takes 2050 cycles, of which the products alone need 1260 (M128 N64 K16 50
 // cycles, M128 N128 K16 64) and the exponentials 1024.  The rest is latency between the roles: a slot's product lane
 // spends 1000 cycles a step on barriers, commits and operand registers, the softmax 850 on its loads, maxima and barriers, and
-// both slots come to run in step, so that neither fills the other's gaps.  Measured beside it and not better: 16 softmax warps
+// both slots come to run in step, so that neither fills the other's gaps.  Measured against 246 us and not better: 16 softmax warps
 // of half a row each, 251 us; a lane for each kind of product in place of each slot, 257 us; three product lanes, 252 us; a late
-// start of slot 1, 247 us.  Short sequences: 18 us for 1 row over 1024 slots, 6 us of it before the first scores (lengths, pages,
+// start of slot 1, 247 us.  Short sequences: 17 us for 1 row over 1024 slots, 6 us of it before the first scores (lengths, pages,
 // the first copies), the rest two or three steps, partials and the merge's launch.
 //
 // Every wait is bounded; on expiry the CTA raises POSS_E_TIMEOUT, runs through its (bounded) walk without meaning, waits
