@@ -273,6 +273,8 @@ __global__ void __launch_bounds__(THREADS) k_beam_merge(BeamArgs a) {
   __shared__ Cand s_head[16];
   __shared__ int s_n;
   __shared__ Cand s_entry[MAX_ENTRIES];
+  __shared__ int s_pre_tok[PRE][THREADS];
+  __shared__ float s_pre_val[PRE][THREADS];
   pdl_enter(POSS_K_BEAM_MERGE);
   const int g = blockIdx.x, t = threadIdx.x, lane = t & 31, warp = t >> 5, K = a.K;
   Cand none;
@@ -281,14 +283,18 @@ __global__ void __launch_bounds__(THREADS) k_beam_merge(BeamArgs a) {
   // their way while the sums are worked on: a group of few chunks is a chain of trips to memory and little else.
   const int lists = K * a.n_chunks, parts = K <= WARPS ? WARPS : 2 * WARPS;
   const int part = t / (THREADS / parts), l0 = (t % (THREADS / parts)) * parts + part;
-  int pre_tok[PRE];
-  float pre_val[PRE];
+  {
+    int tok[PRE];
+    float val[PRE];
 #pragma unroll
-  for (int i = 0; i < PRE; ++i) {
-    const bool there = l0 < lists && i < K;
-    const size_t at = ((size_t)g * lists + (there ? l0 : 0)) * K + (there ? i : 0);
-    pre_tok[i] = there ? a.ctok[at] : -1;
-    pre_val[i] = there ? a.cval[at] : 0.f;
+    for (int i = 0; i < PRE; ++i) {
+      const bool there = l0 < lists && i < K;
+      const size_t at = ((size_t)g * lists + (there ? l0 : 0)) * K + (there ? i : 0);
+      tok[i] = there ? a.ctok[at] : -1;
+      val[i] = there ? a.cval[at] : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < PRE; ++i) { s_pre_tok[i][t] = tok[i]; s_pre_val[i][t] = val[i]; }
   }
   for (int b = warp; b < K; b += WARPS) {
     const int row = g * K + b;
@@ -342,7 +348,7 @@ __global__ void __launch_bounds__(THREADS) k_beam_merge(BeamArgs a) {
     return make(l, i, a.ctok[at], a.cval[at]);            // (a beam without lists: whatever lies there is not looked at)
   };
   // ---- 1
-  Cand head = l0 < lists ? make(l0, 0, pre_tok[0], pre_val[0]) : none;
+  Cand head = l0 < lists ? make(l0, 0, s_pre_tok[0][t], s_pre_val[0][t]) : none;
   for (int l = l0 + THREADS; l < lists; l += THREADS) {
     const Cand e = entry(l, 0);
     if (better(e, head)) head = e;
@@ -366,12 +372,15 @@ __global__ void __launch_bounds__(THREADS) k_beam_merge(BeamArgs a) {
     return true;
   };
   if (l0 < lists) {
-    bool more = true;
-#pragma unroll
-    for (int i = 0; i < PRE; ++i) more = more && i < K && take(make(l0, i, pre_tok[i], pre_val[i]));
-    for (int i = PRE; more && i < K; ++i) more = take(entry(l0, i));
+#pragma unroll 1
+    for (int i = 0; i < K; ++i) {
+      const size_t at = ((size_t)g * lists + l0) * K + i;
+      if (!take(make(l0, i, i < PRE ? s_pre_tok[i][t] : a.ctok[at], i < PRE ? s_pre_val[i][t] : a.cval[at]))) break;
+    }
   }
+#pragma unroll 1
   for (int l = l0 + THREADS; l < lists; l += THREADS)
+#pragma unroll 1
     for (int i = 0; i < K && take(entry(l, i)); ++i) {}
   __syncthreads();
   const int n = s_n;

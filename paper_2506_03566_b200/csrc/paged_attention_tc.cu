@@ -130,7 +130,8 @@ struct Ctl {
   SeqWork work0;                        // its work
   float2 ml[2][QR];                     // a slot's maximum and sum, for the merge of two slots with the same rows
 };
-static_assert(sizeof(Ctl) <= 3072, "the control block lies behind the tiles");
+constexpr int CTL_BYTES = 3 * 1024;
+static_assert(sizeof(Ctl) <= CTL_BYTES, "the control block lies behind the tiles");
 
 // CTAs that share `total` units (MIN_UNITS each at least), and the cut: the first total % grid of them take one unit more.
 // Two units and not one: partials and their merge cost more than a second step where few rows meet few keys (1 row over 1024 slots:
@@ -1017,7 +1018,7 @@ void launch(Launcher& L, const TcArgs& k0, const CUtensorMap& map, const CUtenso
   using Z = Shape<HD>;
   TcArgs k = k0;
   const PagedAttnArgs& a = k.a;
-  const size_t smem = Z::CTL_OFF + 3072;
+  const size_t smem = Z::CTL_OFF + CTL_BYTES;
   k.smem_bytes = (uint32_t)smem;
   static PerDeviceFlags attr_done;
   bool* attr = attr_done.current();
