@@ -9,8 +9,8 @@
 //   of 8192 for logits in no order) are ever compared with one another.
 // Measured (fp32, in a captured graph): 32 groups of 8 beams over 128256 tokens, 131 MB, 40 us: 29 the first kernel (4.5 TB/s; the
 // registers of a chunk allow 4 blocks per SM, whose reductions and compares leave the memory idle a third of the time), 11 the
-// second, a chain of trips to memory and barriers in 32 blocks.  4 beams over 32000 tokens: 10.6 us, 4.3 and 6.3; the chunks stay
-// at 8192 there too, since smaller ones make the second kernel's lists longer.
+// second, a chain of trips to memory and barriers in 32 blocks.  4 beams over 32000 tokens: 10.0 us, 4.2 and 5.8; the chunks stay
+// at 8192 there too: with 2048 it takes 8.4, but 8 beams over 128256 take 12.2 for 9.8, since the second kernel's lists grow.
 #include "paged.cuh"
 #include <float.h>
 
@@ -81,21 +81,28 @@ template <> struct Vec<bf16> {
   }
 };
 
+// Place in its chunk of a thread's j-th logit.  A whole chunk is read in pieces of 16 bytes; one that the row does not fill in
+// single logits, dealt to all threads: parts of the block that get none would leave the selection without a bound (4 beams over
+// 1000 bf16 tokens 16.5 us, in pieces, against 8.5).
+template <typename T> __device__ __forceinline__ int place(bool filled, int j) {
+  constexpr int N = Vec<T>::N;
+  return filled ? ((j / N) * THREADS + (int)threadIdx.x) * N + j % N : j * THREADS + (int)threadIdx.x;
+}
 // the thread's logits of a chunk; places outside the row count as banned
 template <typename T>
-__device__ __forceinline__ void load_chunk(const T* base, int V, int first, float (&x)[PER]) {
+__device__ __forceinline__ void load_chunk(const T* base, int V, int first, bool filled, float (&x)[PER]) {
   constexpr int N = Vec<T>::N;
-  const int t0 = first + (int)threadIdx.x * N;
-  if (first >= 0 && first + CHUNK <= V) {
+  if (filled) {
 #pragma unroll
     for (int j = 0; j < PER / N; ++j)
-      Vec<T>::get(__ldcs(reinterpret_cast<const uint4*>(base + t0 + j * THREADS * N)), x + j * N);
+      Vec<T>::get(__ldcs(reinterpret_cast<const uint4*>(base + first + (j * THREADS + (int)threadIdx.x) * N)), x + j * N);
   } else {
+    const int at = first + (int)threadIdx.x;
+    const T* const p = base + at;                         // (place<T>(false, j) = j * THREADS + threadIdx.x)
 #pragma unroll
-    for (int j = 0; j < PER / N; ++j) {
-      const int i = t0 + j * THREADS * N;
-#pragma unroll
-      for (int e = 0; e < N; ++e) x[j * N + e] = i + e >= 0 && i + e < V ? to_f(base[i + e]) : -INFINITY;
+    for (int j = 0; j < PER; ++j) {
+      x[j] = -INFINITY;
+      if ((unsigned)(at + j * THREADS) < (unsigned)V) x[j] = to_f(p[j * THREADS]);
     }
   }
 }
@@ -103,7 +110,6 @@ __device__ __forceinline__ void load_chunk(const T* base, int V, int first, floa
 // Block (chunk, row).
 template <typename T>
 __global__ void __launch_bounds__(THREADS, 4) k_beam_lists(BeamArgs a, const T* logits) {
-  constexpr int N = Vec<T>::N;                            // values per load
   __shared__ float s_max[16], s_sum[WARPS];
   __shared__ int s_count;
   __shared__ float s_val[MAX_CAND];
@@ -118,7 +124,8 @@ __global__ void __launch_bounds__(THREADS, 4) k_beam_lists(BeamArgs a, const T* 
   const int shift = (int)((reinterpret_cast<uintptr_t>(base) & 15) / sizeof(T));
   const int chunk = blockIdx.x, first = chunk * CHUNK - shift;
   float x[PER];
-  load_chunk<T>(base, a.V, first, x);
+  const bool filled = first >= 0 && first + CHUNK <= a.V;
+  load_chunk<T>(base, a.V, first, filled, x);
   // Maxima of fours and of the thread.  (-inf needs no care, +inf and NaN are rare: they show in the maximum.)
   float q[PER / 4], m = -INFINITY;
   auto maxima = [&] {
@@ -159,7 +166,7 @@ __global__ void __launch_bounds__(THREADS, 4) k_beam_lists(BeamArgs a, const T* 
             const int at = atomicAdd(&s_count, 1);
             if (at < MAX_CAND) {
               s_val[at] = x[j];
-              s_tok[at] = first + ((j / N) * THREADS + t) * N + j % N;
+              s_tok[at] = first + place<T>(filled, j);
             }
           }
         }
@@ -215,10 +222,11 @@ __global__ void __launch_bounds__(THREADS, 4) k_beam_lists(BeamArgs a, const T* 
     int li = -1;
     for (int r = 0; r < K; ++r) {
       float bv = -INFINITY;
-      int bi = 0x7fffffff;
+      int bi = 0x7fffffff, f = filled;
+      asm volatile("" : "+r"(f));                         // (the places are worked out in each round, not kept for all)
 #pragma unroll
       for (int j = 0; j < PER; ++j) {
-        const int i = first + ((j / N) * THREADS + t) * N + j % N;
+        const int i = first + place<T>(f != 0, j);
         if (x[j] > -INFINITY && before(lv, li, x[j], i) && before(x[j], i, bv, bi)) { bv = x[j]; bi = i; }
       }
 #pragma unroll

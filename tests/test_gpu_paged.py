@@ -908,3 +908,14 @@ def test_outputs_over_inputs_are_refused():
     with pytest.raises(L.PossError):
         L.poss_paged_tree_attention(q, pages, 0, t, n, torch.ones(2, 1, 1, dtype=torch.int64, device="cuda"), 0.1, out=q)
     assert L.poss_pages_compact(pages, t, n, path, acc).tolist() == [21, 4]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("v", [255, 256, 257, 1000, 2047, 8192 + 3, 8192 + 700, 16384 + 2049])
+def test_beam_selection_over_chunks_that_the_vocabulary_does_not_fill(dtype, v):
+    torch.manual_seed(73)
+    for k in (1, 5, 16):
+        x = (torch.randn(2, k, v, device="cuda") * 2).to(dtype)
+        x[0, 0, -1] = 30.0                                        # the row's last logit is the best
+        x[1, :, 0] = 25.0
+        check_beams(x, -np.random.default_rng(74).random((2, k)).astype(np.float32))
