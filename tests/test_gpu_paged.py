@@ -919,3 +919,29 @@ def test_beam_selection_over_chunks_that_the_vocabulary_does_not_fill(dtype, v):
         x[0, 0, -1] = 30.0                                        # the row's last logit is the best
         x[1, :, 0] = 25.0
         check_beams(x, -np.random.default_rng(74).random((2, k)).astype(np.float32))
+
+
+@pytest.mark.parametrize("n_pages", [12 * 1024, 12 * 1024 + 1, 20000])
+def test_remap_of_a_pool_larger_than_shared_memory_counts(n_pages):
+    """Either side of the pool size up to which the counts lie in shared memory; most pages pinned, so that the free ones lie far up."""
+    rng = np.random.default_rng(75)
+    n, mp, page = 40, 12, 4
+    pages = torch.randn(1, n_pages, 2, 1, page, 32, device="cuda")
+    refs = (rng.random(n_pages) < 0.98).astype(np.int32)
+    refs[-50:] = 0
+    tables, lens = np.full((n, mp), -1, np.int32), np.zeros(n, np.int32)
+    fits = 0
+    for step in range(8):
+        parents = rng.integers(-1, n, n)
+        kept = np.where(parents >= 0, lens[np.maximum(parents, 0)], 0)
+        room = np.minimum(rng.integers(0, 2 * page + 2, n), mp * page - kept)
+        state = check_remap(pages, tables, lens, refs, parents.tolist(), room.tolist())
+        if state is None:
+            for p in tables[tables >= 0]:
+                refs[p] -= 1
+            tables, lens = np.full((n, mp), -1, np.int32), np.zeros(n, np.int32)
+            continue
+        fits += 1
+        tables, refs, lens, _ = state
+        lens = (lens + room).astype(np.int32)
+    assert fits > 3
