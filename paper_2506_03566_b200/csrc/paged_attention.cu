@@ -8,7 +8,7 @@
 // columns of the output.  With ns > 1 the parts are left in scratch and a second kernel merges them in key order.
 // What bounds it: fp32 multiply-adds and the shared-memory reads that feed them for trees over long contexts (16 trees of 61
 // rows over up to 8191 slots in bf16: 4.6 ms, the tensor-core kernel 0.14), the trips to memory of a 32-key step and of the merge for
-// short ones (3 trees of 15 rows over up to 517 slots, fp32: 13.3 us).
+// short ones (3 trees of 15 rows over up to 517 slots, fp32: 12.9 us).
 #include "paged_attention.cuh"
 #include <math.h>
 
@@ -83,33 +83,48 @@ __global__ void __launch_bounds__(128) k_paged_attn(SimtArgs s, const T* pool) {
 #pragma unroll
     for (int v = 0; v < NV; ++v) o[i][v] = make_float4(0.f, 0.f, 0.f, 0.f);
 
+  // where a key's row lies: thread `t`'s key of a tile, asked for one tile ahead
+  auto find = [&](int tile) {
+    const int key = tile * KB + t;
+    long long at = -1;
+    if (t < KB && tile < tile1 && key < total) {
+      const int p = page_at(table, a.g.max_pages, a.g.n_pages, key / a.g.page);
+      if (p >= 0) at = (long long)(page_offset(a.g, a.layer, p, 0, kvh) + (size_t)(key % a.g.page) * D);
+      else raise_status(a.status, POSS_E_INVALID);
+    }
+    return at;
+  };
+  constexpr int PER = KB * (D / 4) / 128;                 // pieces of four of a tile's keys, or values, per thread
+  const size_t to_values = (size_t)a.g.Hkv * a.g.page * D;
+  long long next_at = find(tile0);
   for (int tile = tile0; tile < tile1; ++tile) {
     const int key0 = tile * KB;
     __syncthreads();                                      // the last tile's values and probabilities have been read
-    if (t < KB) {
-      const int key = key0 + t;
-      long long at = -1;
-      if (key < total) {
-        const int p = page_at(table, a.g.max_pages, a.g.n_pages, key / a.g.page);
-        if (p >= 0) at = (long long)(page_offset(a.g, a.layer, p, 0, kvh) + (size_t)(key % a.g.page) * D);
-        else raise_status(a.status, POSS_E_INVALID);
-      }
-      s_at[t] = at;
-    }
+    if (t < KB) s_at[t] = next_at;
     __syncthreads();
-    auto load_rows = [&](size_t shift) {
-      for (int i = t; i < KB * (D / 4); i += 128) {
-        const int row = i / (D / 4), c = (i - row * (D / 4)) * 4;
-        const long long at = s_at[row];
-        *reinterpret_cast<float4*>(&skv[row][c]) =
-            at >= 0 ? load4<T>(pool + at + shift + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+    next_at = find(tile + 1);
+    // keys and values are on their way together; the values wait in registers for the keys' place
+    float4 keys[PER], values[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int e = t + 128 * i, row = e / (D / 4), c = (e - row * (D / 4)) * 4;
+      const long long at = s_at[row];
+      keys[i] = values[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (at >= 0) {
+        keys[i] = load4<T>(pool + at + c);
+        values[i] = load4<T>(pool + at + to_values + c);
+      }
+    }
+    auto store_rows = [&](const float4* v) {
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        const int e = t + 128 * i, row = e / (D / 4), c = (e - row * (D / 4)) * 4;
+        *reinterpret_cast<float4*>(&skv[row][c]) = v[i];
       }
     };
-    load_rows(0);
+    store_rows(keys);
     const bool partly = key0 + KB > n.prefix;             // some row may not see some key
-    uint32_t have = 0xffffffffu;
-    for (int i = 0; i < KB; ++i)
-      if (s_at[i] < 0) have &= ~(1u << i);
+    const uint32_t have = __ballot_sync(0xffffffffu, s_at[t & 31] >= 0);
     __syncthreads();
     float x[2][4];
 #pragma unroll
@@ -165,26 +180,30 @@ __global__ void __launch_bounds__(128) k_paged_attn(SimtArgs s, const T* pool) {
       for (int v = 0; v < NV; ++v) { o[i][v].x *= c; o[i][v].y *= c; o[i][v].z *= c; o[i][v].w *= c; }
     }
     __syncthreads();                                      // the keys have been read
-    load_rows((size_t)a.g.Hkv * a.g.page * D);
+    store_rows(values);
     __syncthreads();
-    for (int j = 0; j < KB; ++j) {
-      float p[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) p[i] = sp[2 * ty + i][j];
-      // an unseen value takes no part, whatever it holds: 0 x inf would
-      const bool on0 = (seen_any[0] >> j) & 1u, on1 = (seen_any[1] >> j) & 1u;
+    // an unseen value takes no part, whatever it holds: 0 x inf would
+    auto add = [&](int j, bool on0, bool on1) {
+      const float p0 = sp[2 * ty][j], p1 = sp[2 * ty + 1][j];
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
         const float4 w = *reinterpret_cast<const float4*>(&skv[j][tx * 4 + 32 * v]);
         if (on0) {
-          o[0][v].x = fmaf(p[0], w.x, o[0][v].x); o[0][v].y = fmaf(p[0], w.y, o[0][v].y);
-          o[0][v].z = fmaf(p[0], w.z, o[0][v].z); o[0][v].w = fmaf(p[0], w.w, o[0][v].w);
+          o[0][v].x = fmaf(p0, w.x, o[0][v].x); o[0][v].y = fmaf(p0, w.y, o[0][v].y);
+          o[0][v].z = fmaf(p0, w.z, o[0][v].z); o[0][v].w = fmaf(p0, w.w, o[0][v].w);
         }
         if (on1) {
-          o[1][v].x = fmaf(p[1], w.x, o[1][v].x); o[1][v].y = fmaf(p[1], w.y, o[1][v].y);
-          o[1][v].z = fmaf(p[1], w.z, o[1][v].z); o[1][v].w = fmaf(p[1], w.w, o[1][v].w);
+          o[1][v].x = fmaf(p1, w.x, o[1][v].x); o[1][v].y = fmaf(p1, w.y, o[1][v].y);
+          o[1][v].z = fmaf(p1, w.z, o[1][v].z); o[1][v].w = fmaf(p1, w.w, o[1][v].w);
         }
       }
+    };
+    if (__all_sync(0xffffffffu, (seen_any[0] & seen_any[1]) == 0xffffffffu)) {
+#pragma unroll 8
+      for (int j = 0; j < KB; ++j) add(j, true, true);
+    } else {
+#pragma unroll 1
+      for (int j = 0; j < KB; ++j) add(j, (seen_any[0] >> j) & 1u, (seen_any[1] >> j) & 1u);
     }
   }
 #pragma unroll
