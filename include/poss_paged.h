@@ -66,8 +66,8 @@ POSS_API size_t poss_paged_attention_workspace_bytes(const poss_page_pool* pool,
  * with lengths out of range has no rows (status).
  * out must not overlap q.  rows <= POSS_MAX_ROWS.  bf16 with head dimension 64 or 128, a page size of 16, 32, 64, 128 or
  * 256 slots, at most 128 query heads per KV head (G) and a positive scale runs on the tensor cores, where batch * n_kv_heads *
- * ceil(rows / (2 * floor(128 / G))) * ceil(max_pages * page_slots / 64) < 2^31; the probabilities enter the second product rounded to bf16 there, sums and the output's
- * accumulation are fp32.  How the keys are cut, and so the last bits of a result, depends on the whole batch's
+ * ceil(rows / (2 * floor(128 / G))) * ceil(max_pages * page_slots / 64) < 2^31; the probabilities enter the second
+ * product rounded to bf16 there, sums and the output's accumulation are fp32.  How the keys are cut, and so the last bits of a result, depends on the whole batch's
  * lengths; equal calls give equal bits.  Errors: INVALID, SHAPE, CAPACITY, WORKSPACE (too small, not 256-byte
  * aligned), CUDA. */
 POSS_API int poss_paged_tree_attention(const poss_page_pool* pool, int layer, const void* kv_pages, const int32_t* tables,
@@ -80,8 +80,8 @@ POSS_API int poss_paged_tree_attention(const poss_page_pool* pool, int layer, co
  * path[b][k] moves to prefix_len[b] + k for k = 1 .. n_accepted[b]; out_len[b] (int32[batch]) = prefix_len[b] +
  * n_accepted[b] + 1, the slots committed then (the tree's root among them).  path int32[batch][POSS_MAX_DEPTH + 1],
  * n_accepted int32[batch]: the outputs of poss_verify_accept / poss_verify_sample, one row per sequence; path[b][k] is
- * increasing in k.  The slots must lie in pages that no other sequence holds; out_len must not overlap an input.  A sequence with a length, an n_accepted
- * (0 .. POSS_MAX_DEPTH) or a path out of order or range, or without a page that it needs, keeps its slots and gets
+ * increasing in k.  The slots must lie in pages that no other sequence holds; out_len must not overlap an input.
+ * A sequence with a length, an n_accepted (0 .. POSS_MAX_DEPTH) or a path out of order or range, or without a page that it needs, keeps its slots and gets
  * out_len = prefix_len (status).  Surplus pages stay in the table: poss_pages_remap gives them back. */
 POSS_API int poss_pages_compact(const poss_page_pool* pool, void* kv_pages, const int32_t* tables, int max_pages, int batch,
                        const int32_t* prefix_len, const int32_t* path, const int32_t* n_accepted, int32_t* out_len,
@@ -125,8 +125,8 @@ POSS_API size_t poss_beam_select_workspace_bytes(int batch, int beams, int vocab
  * its token; a beam whose score is not finite has no continuation (a search starts with scores 0, -inf, -inf, ...).
  * out_tokens, out_parents, out_finished int32[batch][beams], out_scores float[batch][beams]: the token, the global
  * index group * beams + beam of the beam that it continues (parents for poss_pages_remap), whether it is finished now
- * (its beam was, or the token is eos; eos < 0: only the former), the new score.  With fewer continuations than beams the rest is token -1, parent
- * -1, score -inf, finished 1.  Scores are compared in 64 bits; the sum of exponentials is a sum of fp32 terms.
+ * (its beam was, or the token is eos; eos < 0: only the former), the new score.  With fewer continuations than beams the
+ * rest is token -1, parent -1, score -inf, finished 1.  Scores are compared in 64 bits; the sum of exponentials is a sum of fp32 terms.
  * out_scores may be scores and out_finished finished (in place); the outputs overlap no input and no other output else.
  * 1 <= beams <= POSS_MAX_TOPK, eos < vocab (with `finished` given, eos >= 0).  Errors: INVALID, CAPACITY, WORKSPACE. */
 POSS_API int poss_beam_select(const void* logits, int dtype, int batch, int beams, int vocab, const float* scores,

@@ -3,6 +3,7 @@ tensors, a Python module of C++) beside it."""
 from __future__ import annotations
 
 import os
+import shutil
 import subprocess
 import sys
 import sysconfig
@@ -64,12 +65,13 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if force or _stale(CALLS, [src] + headers):
         import torch
         root = os.path.dirname(torch.__file__)
+        cuda = os.path.dirname(os.path.dirname(os.path.realpath(shutil.which(_nvcc()) or "/usr/local/cuda/bin/nvcc")))
         cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-shared",
                f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}", "-I" + sysconfig.get_paths()["include"],
                "-isystem", os.path.join(root, "include"),
                "-isystem", os.path.join(root, "include", "torch", "csrc", "api", "include"),
-               "-isystem", os.path.join(os.path.dirname(os.path.dirname(_nvcc())), "include"), src, "-o", CALLS,
-               "-L" + HERE, "-l:" + os.path.basename(OUT), "-L" + os.path.join(root, "lib"), "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda",
+               "-isystem", os.path.join(cuda, "include"), src, "-o", CALLS, "-L" + HERE, "-l:" + os.path.basename(OUT),
+               "-L" + os.path.join(root, "lib"), "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda",
                "-l:libstdc++.so.6",    # torch's own: a second copy linked in would have locales of its own
                "-Wl,-rpath,$ORIGIN"]
         r = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
