@@ -174,10 +174,13 @@ __global__ void __launch_bounds__(THREADS, 4) k_beam_lists(BeamArgs a, const T* 
     }
   }
   // Sum of exponentials below the chunk's maximum (an all-banned chunk: maximum -inf, sum 0): 2^(x log2 e - c) with c the
-  // rounded mx log2 e; what c leaves over is put right once for the sum.
+  // rounded mx log2 e; what c leaves over is put right once for the sum.  It is 2^-4 at the most below 2^20, but grows with mx:
+  // behind 2^31 or so the power of it leaves fp32.  So larger maxima (finite masks: -1e10, the type's lowest value) take the
+  // differences first; those that count are exact there, and what overflows goes to -inf, whose power is 0.
   float sum = 0.f;
-  if (mx > -INFINITY) {
-    const float L2E = 1.4426950408889634f, c = mx * L2E;
+  const float L2E = 1.4426950408889634f;
+  if (fabsf(mx) < 0x1p20f) {
+    const float c = mx * L2E;
     float2 s0 = make_float2(0.f, 0.f), s1 = s0;
 #pragma unroll
     for (int j = 0; j < PER; j += 4) {
@@ -187,6 +190,9 @@ __global__ void __launch_bounds__(THREADS, 4) k_beam_lists(BeamArgs a, const T* 
       s1 = add2(s1, make_float2(ex2(v.x), ex2(v.y)));
     }
     sum = ((s0.x + s0.y) + (s1.x + s1.y)) * ex2(-fmaf(mx, L2E, -c));
+  } else if (mx > -INFINITY) {
+#pragma unroll
+    for (int j = 0; j < PER; ++j) sum += ex2((x[j] - mx) * L2E);
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -329,7 +335,8 @@ __global__ void __launch_bounds__(THREADS) k_beam_merge(BeamArgs a) {
     if (lane == 0) {
       s_lse[b] = lse;
       s_score[b] = (double)score;
-      s_kind[b] = !alive ? 0 : done ? 2 : 1;
+      // (an open beam whose tokens are all banned has no finite sum)
+      s_kind[b] = !alive ? 0 : done ? 2 : fabs(lse) < (double)INFINITY ? 1 : 0;
     }
   }
   if (t == 0) s_n = 0;

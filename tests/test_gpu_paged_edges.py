@@ -1,0 +1,69 @@
+"""GPU tests of the paged-cache and beam calls at the edges of what they document: logits of any finite size, beams that are
+alike, outputs of a call that did not fit, items of one key tile behind longer ones."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from tests import paged_util as pg
+from tests.test_gpu_paged import BF, F32, i32, lib
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------ beams
+def check_selection(x, scores, finished=None, eos=-1):
+    """The definition in 64 bits.  A score is off by half a step of fp32 (2^-24 of it), by 2^-20 for the sum of exponentials (fp32
+    terms and chunk sums), and by what 64 bits leave of maximum + log(sum) and of the logit minus it: two roundings, 2^-53 of the
+    row's largest finite logit each, on either side."""
+    s = np.asarray(scores, np.float32)
+    out = {"tokens": torch.full(s.shape, 77, dtype=torch.int32, device="cuda"), "parents": torch.full(s.shape, 77, dtype=torch.int32, device="cuda"),
+           "scores": torch.full(s.shape, 77.0, device="cuda"), "finished": torch.full(s.shape, 77, dtype=torch.int32, device="cuda")}
+    r = lib().poss_beam_select(x, torch.as_tensor(s).cuda(), finished=None if finished is None else i32(finished), eos=eos, out=out)
+    torch.cuda.synchronize()
+    rows = x.double().cpu().numpy()
+    tok, par, sc, fin = pg.beam_select(rows, s, finished, eos)
+    assert np.array_equal(r["tokens"].cpu().numpy(), tok)
+    assert np.array_equal(r["parents"].cpu().numpy(), par)
+    assert np.array_equal(r["finished"].cpu().numpy(), fin)
+    got = r["scores"].double().cpu().numpy()
+    on = np.isfinite(sc)
+    assert np.array_equal(np.isneginf(got), ~on)
+    top = np.where(np.isfinite(rows), np.abs(rows), 0.0).max(-1).reshape(-1)[np.maximum(par, 0)]
+    assert (np.abs(got[on] - sc[on]) <= np.abs(sc[on]) * 2.0 ** -24 + 2.0 ** -20 + top[on] * 2.0 ** -51).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("low", ["lowest", -1e30, -1e10, -3e9, -1e9, -1e4])
+def test_finite_masks_of_any_size_leave_the_other_logits_alone(dtype, low):
+    """Tokens masked with the type's lowest value, or another very negative number: whole chunks of 8192, a last chunk that the
+    vocabulary does not fill, whole rows, and all but a few tokens."""
+    low = torch.finfo(dtype).min if low == "lowest" else low
+    torch.manual_seed(80)
+    k, v = 4, 30000
+    x = (torch.randn(7, k, v, device="cuda") * 2).to(dtype)
+    x[0, :, 8192:] = low
+    x[1, :, :29000] = low
+    x[2] = low                                                  # a row of equal logits, however low
+    x[3, 1:3] = low
+    x[4, :, 3:] = low                                           # fewer tokens left than beams
+    x[5, :, 8192:16384] = low
+    x[5, :, 9000] = -math.inf
+    x[6, :, 16384:] = low
+    x[6, :, 16384:24576] = -math.inf
+    x[6, :, 29999] = math.nan
+    check_selection(x, -np.random.default_rng(81).random((7, k)).astype(np.float32))
+    check_selection(x, np.zeros((7, k), np.float32), np.eye(7, k, dtype=np.int32), eos=3)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("high", [1e4, 1e9, 1e10, 1e30, 3e38])
+def test_logits_of_any_finite_size(dtype, high):
+    torch.manual_seed(82)
+    k, v = 5, 20011
+    x = (torch.randn(3, k, v, device="cuda") * 2).to(dtype)
+    x[0, :, 100:117] = high
+    x[1, 2] = high
+    x[2] *= high / 16                                           # logits spread over the whole size, both signs
+    check_selection(x, -np.random.default_rng(83).random((3, k)).astype(np.float32))
