@@ -67,3 +67,17 @@ def test_logits_of_any_finite_size(dtype, high):
     x[1, 2] = high
     x[2] *= high / 16                                           # logits spread over the whole size, both signs
     check_selection(x, -np.random.default_rng(83).random((3, k)).astype(np.float32))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("k,v", [(4, 10007), (16, 8193), (7, 32003), (8, 50257), (3, 24578), (5, 32000)])
+def test_beams_that_are_alike_tie_wherever_their_rows_start(dtype, k, v):
+    """Equal logits and scores are equal continuations: the lower beam comes first.  Rows of these lengths start at every place of
+    16 bytes."""
+    torch.manual_seed(84)
+    x = torch.randn(3, 1, v, device="cuda").to(dtype).expand(3, k, v).contiguous()
+    check_selection(x, np.zeros((3, k), np.float32))
+    check_selection(x, np.full((3, k), -2.3, np.float32))
+    y = torch.randn(1, 1, v, device="cuda").to(dtype)
+    x[2, 1::2] = y[0]                                             # two kinds in turn
+    check_selection(x, np.full((3, k), 0.7, np.float32))
