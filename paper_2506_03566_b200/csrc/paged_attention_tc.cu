@@ -118,6 +118,8 @@ __device__ __forceinline__ SeqWork seq_work(const TcArgs& k, int b) {
 //   q_full, q_empty, o_free: one phase per segment.  A slot without steps in a segment waits for no o_free there, but a slot
 //     with steps gives q_empty up only behind its wait for the o_free before: whoever has seen q_full of segment s + 1 knows
 //     that o_free of segment s - 1 is complete.
+// ml has no second copy: a slot writes its own for a segment only when the other one has read it for the segment before.  A slot with
+// steps has waited for second products, which follow that segment's o_free; one without steps waits for o_free itself.
 struct Ctl {
   uint64_t kv_full[2][MAX_STAGES], kv_empty[2][MAX_STAGES], q_full, q_empty, s_full[2][2], p_full[2][2], pv_done[2][2], o_free, drain[2];
   uint32_t tmem;
@@ -641,6 +643,7 @@ __global__ void __launch_bounds__(N_THREADS, 1) k_paged_attn_tc(const __grid_con
       if (steps > 0) wait(c.pv_done[wg][(n_own - 1) & 1], (n_own - 1) >> 1);
       float c0 = 1.f, c1 = 0.f;                           // weights of slot 0's and slot 1's outputs (same rows)
       if (!halves) {
+        if (steps == 0 && seg > 0) wait(c.o_free, seg - 1);   // (slot 0's next outputs wait for it as well: no time is lost)
         c.ml[wg][row] = make_float2(m, l);
         tc_fence_before();
         softmax_sync();                                   // both slots' outputs are complete

@@ -7,7 +7,7 @@ import pytest
 import torch
 
 from tests import paged_util as pg
-from tests.test_gpu_paged import BF, F32, i32, lib
+from tests.test_gpu_paged import BF, F32, Case, i32, lib
 
 pytestmark = pytest.mark.gpu
 
@@ -81,3 +81,20 @@ def test_beams_that_are_alike_tie_wherever_their_rows_start(dtype, k, v):
     y = torch.randn(1, 1, v, device="cuda").to(dtype)
     x[2, 1::2] = y[0]                                             # two kinds in turn
     check_selection(x, np.full((3, k), 0.7, np.float32))
+
+
+# ------------------------------------------------------------------ attention
+@pytest.mark.parametrize("d,lens", [(128, (150, 20, 40)), (64, (150, 20, 40)), (128, (700, 3, 60, 1, 64))])
+def test_items_of_one_tile_behind_longer_ones(d, lens):
+    """Few rows, so the two slots of a CTA share them and take the key tiles in turn: over a short sequence the second slot has
+    nothing to do and is at the next item at once, while the first still joins both slots' sums of the one before."""
+    batch, rows = 600, 2
+    prefix = [lens[i % len(lens)] - rows for i in range(batch)]
+    c = Case(90, BF, 2, 1, d, 16, [max(0, p) for p in prefix], rows)
+    got = c.run()
+    assert int(c.gpu_status) == 0
+    c.check(got)
+    args = (c.q.cuda(), c.pages.cuda(), 0, torch.as_tensor(c.tables).cuda(), i32(c.prefix), torch.as_tensor(c.mask).cuda(), c.scale)
+    outs = [lib().poss_paged_tree_attention(*args) for _ in range(100)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, got) for o in outs)
