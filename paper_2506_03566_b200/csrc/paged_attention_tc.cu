@@ -120,7 +120,12 @@ __device__ __forceinline__ SeqWork seq_work(const TcArgs& k, int b) {
 //     that o_free of segment s - 1 is complete.
 // ml has no second copy: a slot writes its own for a segment only when the other one has read it for the segment before.  A slot with
 // steps has waited for second products, which follow that segment's o_free; one without steps waits for o_free itself.
+//   clean, in turn: one phase per tile that slot 0 puts right for both slots.  A segment has at most three; slot 0 can be past those
+//     of one segment and two of the next (its second products there wait for o_free of this one) while slot 1 waits for this one's
+//     first, five ahead: with six barriers none is a phase ahead of a wait.
+constexpr int N_CLEAN = 6;
 struct Ctl {
+  uint64_t clean[N_CLEAN];
   uint64_t kv_full[2][MAX_STAGES], kv_empty[2][MAX_STAGES], q_full, q_empty, s_full[2][2], p_full[2][2], pv_done[2][2], o_free, drain[2];
   uint32_t tmem;
   int abort;
@@ -427,6 +432,7 @@ __global__ void __launch_bounds__(N_THREADS, 1) k_paged_attn_tc(const __grid_con
       mbar_init(bar(c.q_full), 1);
       mbar_init(bar(c.q_empty), 2);
       mbar_init(bar(c.o_free), N_SOFTMAX);
+      for (int i = 0; i < N_CLEAN; ++i) mbar_init(bar(c.clean[i]), QR);
       for (int i = 0; i < 2; ++i) {
         mbar_init(bar(c.drain[i]), 1);
         for (int j = 0; j < 2; ++j) {
@@ -575,11 +581,10 @@ __global__ void __launch_bounds__(N_THREADS, 1) k_paged_attn_tc(const __grid_con
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         }
         if (partly && halves) {
-          // slot 1's product reads what slot 0's warps have put right.  (A segment has at most three such tiles; of the next
-          // one's, slot 0 can reach two while slot 1 has two of this one's before it: six barriers in turn.)
-          const int id = 2 + n_partly % 6;
-          if (wg == 0) asm volatile("bar.arrive %0, 256;" ::"r"(id) : "memory");
-          else asm volatile("bar.sync %0, 256;" ::"r"(id) : "memory");
+          // slot 1's product reads what slot 0's warps have put right
+          uint64_t& b = c.clean[n_partly % N_CLEAN];
+          if (wg == 0) mbar_arrive(bar(b));
+          else wait(b, n_partly / N_CLEAN);
           ++n_partly;
         }
         const int buf = n_own & 1;

@@ -98,3 +98,17 @@ def test_items_of_one_tile_behind_longer_ones(d, lens):
     outs = [lib().poss_paged_tree_attention(*args) for _ in range(100)]
     torch.cuda.synchronize()
     assert all(torch.equal(o, got) for o in outs)
+
+
+@pytest.mark.parametrize("d,hq,hkv,rows", [(128, 32, 8, 61), (64, 8, 8, 128), (128, 4, 1, 2)])
+def test_a_wait_that_runs_out_with_many_items_in_a_cta(d, hq, hkv, rows):
+    """The value tiles of one launch are withheld from CTAs that hold several items of few tiles, with rows for both slots or for
+    one: every role comes to the end of its walk, the status word says so, and the next call is sound."""
+    batch = 64 if rows > 2 else 600
+    c = Case(91, BF, hq, hkv, d, 16, [100 - rows // 2] * batch, rows)
+    first = c.run()
+    assert int(c.gpu_status) == 0
+    assert lib().load_library().poss_debug_paged_lose_load(1) == 0
+    c.run()
+    assert int(c.gpu_status) == 6
+    assert torch.equal(c.run(), first) and int(c.gpu_status) == 0
