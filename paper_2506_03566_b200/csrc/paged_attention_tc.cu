@@ -503,6 +503,7 @@ __global__ void __launch_bounds__(N_THREADS, 1) k_paged_attn_tc(const __grid_con
   bool ok = __all_sync(0xffffffffu, *abort_flag == 0);
   int tiles_before = 0;                                   // tiles of the segments before
   int n_own = 0, n_partly = 0;                            // softmax and products: steps of the slot; copies: tiles
+  int n_queries = 0;                                      // copies: segments whose queries are on their way or here
   // copies: stage and phase of the next keys or values
   uint32_t c_ph = 0, elected = 0;
   int c_st = 0;
@@ -760,6 +761,7 @@ __global__ void __launch_bounds__(N_THREADS, 1) k_paged_attn_tc(const __grid_con
                         (2 * g.group + (halves ? slot : 0)) * k.slot_rows, g.b);
           }
         }
+        n_queries += ok;
         __syncwarp();
       };
 #pragma unroll 1
@@ -896,6 +898,8 @@ __global__ void __launch_bounds__(N_THREADS, 1) k_paged_attn_tc(const __grid_con
     const uint64_t t0 = global_ns();
     if (warp == WARP_KEYS || warp == WARP_VALUES) {
       const int kv = warp == WARP_VALUES, n = kv ? Z::NV : Z::NK;
+      while (n_queries > 0 && !mbar_try_wait(bar(c.q_full), (uint32_t)((n_queries - 1) & 1)) && global_ns() - t0 < WAIT_LIMIT_NS / 2)
+        __nanosleep(64);
       for (int i = n_own > n ? n_own - n : 0; i < n_own; ++i)
         while (!mbar_try_wait(bar(c.kv_full[kv][i % n]), (uint32_t)((i / n) & 1)) && global_ns() - t0 < WAIT_LIMIT_NS / 2)
           __nanosleep(64);

@@ -112,3 +112,27 @@ def test_a_wait_that_runs_out_with_many_items_in_a_cta(d, hq, hkv, rows):
     c.run()
     assert int(c.gpu_status) == 6
     assert torch.equal(c.run(), first) and int(c.gpu_status) == 0
+
+
+def test_waits_that_run_out_at_once_in_many_launches():
+    """Launches without their value tiles one behind the other, on two streams: each ends with its queries and tiles landed, and its
+    TMEM given back, so that the launches behind it and beside it are sound."""
+    cases = [Case(92 + i, BF, 8, 2, 128, 16, [300 - 200 * i, 40, 5], 9 + 50 * i) for i in range(2)]
+    wants = [c.want() for c in cases]
+    streams = [torch.cuda.Stream() for _ in cases]
+    args = [(c.q.cuda(), c.pages.cuda(), 0, torch.as_tensor(c.tables).cuda(), i32(c.prefix), torch.as_tensor(c.mask).cuda(), c.scale)
+            for c in cases]
+    torch.cuda.synchronize()
+    assert lib().load_library().poss_debug_paged_lose_load(2) == 0
+    status = [[torch.zeros(1, dtype=torch.int32, device="cuda") for _ in range(3)] for _ in cases]
+    torch.cuda.synchronize()
+    outs = [[], []]
+    for i in range(3):
+        for s, a, o, st in zip(streams, args, outs, status):
+            with torch.cuda.stream(s):
+                o.append(lib().poss_paged_tree_attention(*a, status=st[i]))
+    torch.cuda.synchronize()
+    assert [[int(x) for x in st] for st in status] == [[6, 0, 0], [6, 0, 0]]
+    for c, w, o in zip(cases, wants, outs):
+        c.check(o[1], w)
+        assert torch.equal(o[2], o[1])
