@@ -87,7 +87,7 @@ POSS_API int poss_pages_compact(const poss_page_pool* pool, void* kv_pages, cons
                        const int32_t* prefix_len, const int32_t* path, const int32_t* n_accepted, int32_t* out_len,
                        int32_t* status, poss_stream stream);
 
-/* Scratch of poss_pages_remap, in bytes (0: arguments out of range). */
+/* Scratch of poss_pages_remap and poss_pages_remap_fresh, in bytes (0: arguments out of range). */
 POSS_API size_t poss_pages_remap_workspace_bytes(const poss_page_pool* pool, int n_before, int n_after, int max_pages);
 
 /* Replaces the n_before sequences of a table by n_after new ones: reordering and forking (several sequences with one
@@ -112,6 +112,15 @@ POSS_API int poss_pages_remap(const poss_page_pool* pool, void* kv_pages, const 
                      int max_pages, int n_before, int n_after, const int32_t* seq_len, const int32_t* refs,
                      int32_t* out_refs, const int32_t* parents, const int32_t* room, int32_t* out_len,
                      int32_t* out_free, void* workspace, size_t workspace_bytes, int32_t* status,
+                     poss_stream stream);
+
+/* poss_pages_remap into outputs that hold nothing yet: if fewer pages are free than needed, every entry of out_tables
+ * becomes -1 and every length 0 instead of being left, so that what follows before out_free has been read finds no page
+ * to write to.  (The old tables go on with refs, which out_refs equals then.)  All else, errors too, is the same. */
+POSS_API int poss_pages_remap_fresh(const poss_page_pool* pool, void* kv_pages, const int32_t* tables,
+                     int32_t* out_tables, int max_pages, int n_before, int n_after, const int32_t* seq_len,
+                     const int32_t* refs, int32_t* out_refs, const int32_t* parents, const int32_t* room,
+                     int32_t* out_len, int32_t* out_free, void* workspace, size_t workspace_bytes, int32_t* status,
                      poss_stream stream);
 
 /* Scratch of poss_beam_select, in bytes (0: arguments out of range). */

@@ -113,6 +113,8 @@ EXPORTS = {
     "poss_pages_remap_workspace_bytes": (C.c_size_t, [C.POINTER(poss_page_pool)] + [C.c_int] * 3),
     "poss_pages_remap": (C.c_int, [C.POINTER(poss_page_pool)] + [C.c_void_p] * 3 + [C.c_int] * 3 + [C.c_void_p] * 8 +
                          [C.c_size_t, C.c_void_p, C.c_void_p]),
+    "poss_pages_remap_fresh": (C.c_int, [C.POINTER(poss_page_pool)] + [C.c_void_p] * 3 + [C.c_int] * 3 + [C.c_void_p] * 8 +
+                               [C.c_size_t, C.c_void_p, C.c_void_p]),
     "poss_beam_select_workspace_bytes": (C.c_size_t, [C.c_int] * 3),
     "poss_beam_select": (C.c_int, [C.c_void_p] + [C.c_int] * 4 + [C.c_void_p, C.c_void_p, C.c_int] + [C.c_void_p] * 5 +
                          [C.c_size_t, C.c_void_p]),

@@ -330,9 +330,11 @@ POSS_CALL(remap, 9) {  // kv_pages, tables, seq_len, refs, parents, room, out, w
   int32_t* out_len = get("seq_len", {n1}, "out seq_len");
   int32_t* n_free = get("n_free", {1}, "n_free");
   const Scratch ws(x[7], poss_pages_remap_workspace_bytes(&pool.p, n0, n1, t.max_pages), dev);
+  // (tables made here hold whatever their memory held: never pages that somebody might write to)
+  const auto remap = out.made ? poss_pages_remap_fresh : poss_pages_remap;
   call("poss_pages_remap", dev, [&](poss_stream stream) {
-    return poss_pages_remap(&pool.p, pool.pages, t.at, out_tables, t.max_pages, n0, n1, len, refs, out_refs, parents, room, out_len,
-                            n_free, ws.at, ws.bytes, status, stream);
+    return remap(&pool.p, pool.pages, t.at, out_tables, t.max_pages, n0, n1, len, refs, out_refs, parents, room, out_len, n_free, ws.at,
+                 ws.bytes, status, stream);
   });
   return out.release();
 }

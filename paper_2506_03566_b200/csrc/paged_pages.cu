@@ -157,6 +157,7 @@ struct RemapArgs {
   int32_t *writers, *last;     // [n_pages]
   int32_t* free_list;          // [n_pages]
   int32_t* copies;             // [n_after][3]: source page, target page, slots (0: none)
+  int fresh;                   // outputs that hold nothing yet: tables and lengths are emptied where it does not fit
 };
 
 struct RemapSeq { int parent, kept, room, needed; };
@@ -290,9 +291,13 @@ __global__ void __launch_bounds__(REMAP_THREADS, 1) k_pages_remap(RemapArgs a) {
   }
   __syncthreads();
   if (n_free < n_fresh) {
-    // does not fit: nothing changes
+    // does not fit: nothing changes, or the outputs become those of sequences without slots
     for (int p = t; p < g.n_pages; p += REMAP_THREADS) a.out_refs[p] = a.refs[p];
     for (int i = t; i < a.n_after; i += REMAP_THREADS) a.copies[3 * i + 2] = 0;
+    if (a.fresh) {
+      for (size_t i = t; i < (size_t)a.n_after * g.max_pages; i += REMAP_THREADS) a.out_tables[i] = -1;
+      for (int i = t; i < a.n_after; i += REMAP_THREADS) a.out_len[i] = 0;
+    }
     if (t == 0) a.out_free[0] = n_free - n_fresh;
     return;
   }
@@ -367,6 +372,66 @@ __global__ void __launch_bounds__(256) k_pages_copy(PageGeo g, char* pool, const
 
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 
+int remap(const poss_page_pool* pool, void* kv_pages, const int32_t* tables, int32_t* out_tables, int max_pages,
+          int n_before, int n_after, const int32_t* seq_len, const int32_t* refs, int32_t* out_refs,
+          const int32_t* parents, const int32_t* room, int32_t* out_len, int32_t* out_free, void* workspace,
+          size_t workspace_bytes, int32_t* status, poss_stream stream, bool fresh) {
+  int rc = page_pool_check(pool);
+  if (rc != POSS_OK) return rc;
+  if (n_before < 0 || n_after < 0) return POSS_E_INVALID;
+  rc = page_table_check(pool, max_pages, 1);
+  if (rc != POSS_OK) return rc;
+  if (n_before > POSS_MAX_PAGED_BATCH || n_after > POSS_MAX_PAGED_BATCH) return POSS_E_CAPACITY;
+  if (!parents && n_after > 0 && n_before != n_after) return POSS_E_INVALID;
+  if (!kv_pages || !refs || !out_refs || !out_free || refs == out_refs || !aligned16(kv_pages)) return POSS_E_INVALID;
+  if (n_before > 0 && (!tables || !seq_len)) return POSS_E_INVALID;
+  if (n_after > 0 && (!out_tables || !out_len || out_tables == tables)) return POSS_E_INVALID;
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) ||
+      workspace_bytes < poss_pages_remap_workspace_bytes(pool, n_before, n_after, max_pages))
+    return POSS_E_WORKSPACE;
+  // the inputs are read while the outputs are written
+  const size_t pages = (size_t)pool->n_pages * 4, place = (size_t)max_pages * 4, n0 = (size_t)n_before * 4, n1 = (size_t)n_after * 4;
+  const struct { const void* at; size_t bytes; } arrays[] = {
+      {out_tables, n1 * max_pages}, {out_refs, pages}, {out_len, n1}, {out_free, 4},      // written
+      {tables, place * n_before}, {refs, pages}, {seq_len, n0}, {parents, n1}, {room, n1}};
+  for (int i = 0; i < 4; ++i)
+    for (int j = i + 1; j < 9; ++j)
+      if (overlap(arrays[i].at, arrays[i].bytes, arrays[j].at, arrays[j].bytes)) return POSS_E_INVALID;
+  int64_t launches = 0;
+  Launcher L{reinterpret_cast<cudaStream_t>(stream), &launches, POSS_OK};
+  RemapArgs a;
+  a.g = page_geo(pool, tables, max_pages);
+  a.out_tables = out_tables; a.n_before = n_before; a.n_after = n_after;
+  a.seq_len = seq_len; a.refs = refs; a.parents = parents; a.room = room;
+  a.out_refs = out_refs; a.out_len = out_len; a.out_free = out_free; a.status = status; a.fresh = fresh;
+  char* w = reinterpret_cast<char*>(workspace);
+  const size_t per_page = round256((size_t)pool->n_pages * 4);
+  a.writers = reinterpret_cast<int32_t*>(w);
+  a.last = reinterpret_cast<int32_t*>(w + per_page);
+  a.free_list = reinterpret_cast<int32_t*>(w + 2 * per_page);
+  a.copies = reinterpret_cast<int32_t*>(w + 3 * per_page);
+  if (pool->n_pages <= SMEM_PAGES) {
+    static PerDeviceFlags attr_done;
+    bool* attr = attr_done.current();
+    if (!attr || !*attr) {
+      if (cudaFuncSetAttribute(k_pages_remap<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_PAGES * 16) != cudaSuccess)
+        return POSS_E_CUDA;
+      if (attr) *attr = true;
+    }
+    launch_pdl(L, k_pages_remap<true>, dim3(1), dim3(REMAP_THREADS), (size_t)pool->n_pages * 16, a);
+  } else {
+    launch_pdl(L, k_pages_remap<false>, dim3(1), dim3(REMAP_THREADS), 0, a);
+  }
+  if (n_after > 0) {
+    const dim3 grid(pool->n_layers * 2, n_after);
+    if (pool->dtype == POSS_BF16)
+      launch_pdl(L, k_pages_copy<2>, grid, dim3(256), 0, a.g, (char*)kv_pages, (const int32_t*)a.copies);
+    else
+      launch_pdl(L, k_pages_copy<4>, grid, dim3(256), 0, a.g, (char*)kv_pages, (const int32_t*)a.copies);
+  }
+  return L.err;
+}
+
 }  // namespace
 
 extern "C" {
@@ -440,60 +505,17 @@ int poss_pages_remap(const poss_page_pool* pool, void* kv_pages, const int32_t* 
                      int32_t* out_refs, const int32_t* parents, const int32_t* room, int32_t* out_len,
                      int32_t* out_free, void* workspace, size_t workspace_bytes, int32_t* status,
                      poss_stream stream) {
-  int rc = page_pool_check(pool);
-  if (rc != POSS_OK) return rc;
-  if (n_before < 0 || n_after < 0) return POSS_E_INVALID;
-  rc = page_table_check(pool, max_pages, 1);
-  if (rc != POSS_OK) return rc;
-  if (n_before > POSS_MAX_PAGED_BATCH || n_after > POSS_MAX_PAGED_BATCH) return POSS_E_CAPACITY;
-  if (!parents && n_after > 0 && n_before != n_after) return POSS_E_INVALID;
-  if (!kv_pages || !refs || !out_refs || !out_free || refs == out_refs || !aligned16(kv_pages)) return POSS_E_INVALID;
-  if (n_before > 0 && (!tables || !seq_len)) return POSS_E_INVALID;
-  if (n_after > 0 && (!out_tables || !out_len || out_tables == tables)) return POSS_E_INVALID;
-  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) ||
-      workspace_bytes < poss_pages_remap_workspace_bytes(pool, n_before, n_after, max_pages))
-    return POSS_E_WORKSPACE;
-  // the inputs are read while the outputs are written
-  const size_t pages = (size_t)pool->n_pages * 4, place = (size_t)max_pages * 4, n0 = (size_t)n_before * 4, n1 = (size_t)n_after * 4;
-  const struct { const void* at; size_t bytes; } arrays[] = {
-      {out_tables, n1 * max_pages}, {out_refs, pages}, {out_len, n1}, {out_free, 4},      // written
-      {tables, place * n_before}, {refs, pages}, {seq_len, n0}, {parents, n1}, {room, n1}};
-  for (int i = 0; i < 4; ++i)
-    for (int j = i + 1; j < 9; ++j)
-      if (overlap(arrays[i].at, arrays[i].bytes, arrays[j].at, arrays[j].bytes)) return POSS_E_INVALID;
-  int64_t launches = 0;
-  Launcher L{reinterpret_cast<cudaStream_t>(stream), &launches, POSS_OK};
-  RemapArgs a;
-  a.g = page_geo(pool, tables, max_pages);
-  a.out_tables = out_tables; a.n_before = n_before; a.n_after = n_after;
-  a.seq_len = seq_len; a.refs = refs; a.parents = parents; a.room = room;
-  a.out_refs = out_refs; a.out_len = out_len; a.out_free = out_free; a.status = status;
-  char* w = reinterpret_cast<char*>(workspace);
-  const size_t per_page = round256((size_t)pool->n_pages * 4);
-  a.writers = reinterpret_cast<int32_t*>(w);
-  a.last = reinterpret_cast<int32_t*>(w + per_page);
-  a.free_list = reinterpret_cast<int32_t*>(w + 2 * per_page);
-  a.copies = reinterpret_cast<int32_t*>(w + 3 * per_page);
-  if (pool->n_pages <= SMEM_PAGES) {
-    static PerDeviceFlags attr_done;
-    bool* attr = attr_done.current();
-    if (!attr || !*attr) {
-      if (cudaFuncSetAttribute(k_pages_remap<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_PAGES * 16) != cudaSuccess)
-        return POSS_E_CUDA;
-      if (attr) *attr = true;
-    }
-    launch_pdl(L, k_pages_remap<true>, dim3(1), dim3(REMAP_THREADS), (size_t)pool->n_pages * 16, a);
-  } else {
-    launch_pdl(L, k_pages_remap<false>, dim3(1), dim3(REMAP_THREADS), 0, a);
-  }
-  if (n_after > 0) {
-    const dim3 grid(pool->n_layers * 2, n_after);
-    if (pool->dtype == POSS_BF16)
-      launch_pdl(L, k_pages_copy<2>, grid, dim3(256), 0, a.g, (char*)kv_pages, (const int32_t*)a.copies);
-    else
-      launch_pdl(L, k_pages_copy<4>, grid, dim3(256), 0, a.g, (char*)kv_pages, (const int32_t*)a.copies);
-  }
-  return L.err;
+  return remap(pool, kv_pages, tables, out_tables, max_pages, n_before, n_after, seq_len, refs, out_refs, parents, room,
+               out_len, out_free, workspace, workspace_bytes, status, stream, false);
+}
+
+int poss_pages_remap_fresh(const poss_page_pool* pool, void* kv_pages, const int32_t* tables, int32_t* out_tables,
+                           int max_pages, int n_before, int n_after, const int32_t* seq_len, const int32_t* refs,
+                           int32_t* out_refs, const int32_t* parents, const int32_t* room, int32_t* out_len,
+                           int32_t* out_free, void* workspace, size_t workspace_bytes, int32_t* status,
+                           poss_stream stream) {
+  return remap(pool, kv_pages, tables, out_tables, max_pages, n_before, n_after, seq_len, refs, out_refs, parents, room,
+               out_len, out_free, workspace, workspace_bytes, status, stream, true);
 }
 
 int poss_debug_page_of_slot(const int32_t* h_table, int max_pages, int page_slots, int n_pages, int64_t slot,

@@ -77,7 +77,8 @@ def poss_pages_compact(kv_pages, tables, prefix_len, path, n_accepted, out_len=N
 
 def poss_pages_remap(kv_pages, tables, seq_len, refs, parents=None, room=None, out=None, workspace=None, status=None):
     """Replaces the sequences of `tables` by parents.numel() new ones (poss_paged.h).  Returns a dict of int32 tensors:
-    tables, refs, seq_len, n_free (one element; negative: that many pages were missing and nothing changed)."""
+    tables, refs, seq_len, n_free (one element).  A negative n_free: that many pages were missing, the pool is unchanged and
+    refs as before; tables and seq_len are then as they were in a caller's `out`, else without pages and slots (-1 and 0)."""
     return _calls().remap(kv_pages, tables, seq_len, refs, parents, room, out, workspace, status)
 
 

@@ -136,3 +136,41 @@ def test_waits_that_run_out_at_once_in_many_launches():
     for c, w, o in zip(cases, wants, outs):
         c.check(o[1], w)
         assert torch.equal(o[2], o[1])
+
+
+# ------------------------------------------------------------------ remap
+def test_a_remap_that_does_not_fit_returns_empty_tables_of_its_own():
+    """Too few free pages, and no outputs given: the tables that the call made name no page, its lengths are zero, so that a step
+    that runs before n_free has been read writes nothing and is reported."""
+    L = lib()
+    for n_pages in (4, 13000):                                    # counts in shared memory, and in scratch
+        pages = torch.randn(1, n_pages, 2, 2, 16, 64, device="cuda").to(BF)
+        tables, lens = i32([[0, 1, -1], [2, -1, -1]]), i32([20, 9])
+        refs = torch.ones(n_pages, dtype=torch.int32, device="cuda")
+        parents, room = i32([0, 0, 1]), i32([12, 12, 30])
+        for filler in (1, 2):                                     # whatever torch's allocator hands out next held these
+            junk = [torch.full((3, 3), filler, dtype=torch.int32, device="cuda"), torch.full((3,), 5, dtype=torch.int32, device="cuda")]
+            del junk
+            before = pages.clone()
+            r = L.poss_pages_remap(pages, tables, lens, refs, parents, room)
+            assert int(r["n_free"]) < 0 and torch.equal(r["refs"], refs) and torch.equal(pages, before)
+            assert (r["tables"] == -1).all() and (r["seq_len"] == 0).all()
+            status = torch.zeros(1, dtype=torch.int32, device="cuda")
+            k = torch.ones(3, 1, 2, 64, dtype=BF, device="cuda")
+            L.poss_pages_append(k, k, pages, 0, r["tables"], r["seq_len"], status=status)
+            assert int(status) == 1 and torch.equal(pages, before)
+        # the same in a graph, replayed when it fits and when it does not
+        refs[-3:] = 0
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            r = L.poss_pages_remap(pages, tables, lens, refs, parents, room)
+        for fits in (n_pages > 4, False, n_pages > 4):
+            refs.fill_(1)
+            if fits:
+                refs[-3:] = 0
+            g.replay()
+            torch.cuda.synchronize()
+            assert (int(r["n_free"]) >= 0) == fits
+            assert r["seq_len"].tolist() == ([20, 20, 9] if fits else [0, 0, 0])
+            assert fits or ((r["tables"] == -1).all() and torch.equal(r["refs"], refs))
