@@ -294,7 +294,8 @@ __global__ void __launch_bounds__(128) k_paged_attn_merge(SimtArgs s) {
 }
 
 // Parts per (sequence, KV head, query tile): enough blocks for four per SM of a 148-SM device, at least one 32-key tile
-// each where the table is full.  blocks * ns <= SIMT_BLOCKS + blocks bounds the scratch.
+// each where the table is full.  Scratch: SIMT_BLOCKS blocks and more make one part each, which goes straight to the output;
+// with fewer, blocks * ns < SIMT_BLOCKS + blocks.
 constexpr int SIMT_BLOCKS = 592;
 int simt_splits(long long blocks, long long slots) {
   long long ns = (SIMT_BLOCKS + blocks - 1) / blocks;
@@ -317,7 +318,7 @@ void launch_simt(Launcher& L, const SimtArgs& s, const void* pool) {
 
 size_t paged_attn_simt_workspace(int batch, int rows, int Hq, int Hkv, int d) {
   const long long blocks = (long long)batch * Hkv * ((rows * (Hq / Hkv) + QB - 1) / QB);
-  return (size_t)(SIMT_BLOCKS + blocks) * QB * (d + 2) * 4;
+  return (size_t)(SIMT_BLOCKS + (blocks < SIMT_BLOCKS ? blocks : SIMT_BLOCKS - 1)) * QB * (d + 2) * 4;
 }
 
 void launch_paged_attn_simt(Launcher& L, const PagedAttnArgs& a, const void* pool, int dtype) {

@@ -174,3 +174,16 @@ def test_a_remap_that_does_not_fit_returns_empty_tables_of_its_own():
             assert (int(r["n_free"]) >= 0) == fits
             assert r["seq_len"].tolist() == ([20, 20, 9] if fits else [0, 0, 0])
             assert fits or ((r["tables"] == -1).all() and torch.equal(r["refs"], refs))
+
+
+@pytest.mark.parametrize("dtype,d,batch,scale", [(F32, 32, 295, 0.2), (F32, 32, 296, 0.2), (F32, 32, 297, 0.2), (F32, 128, 7, 0.1),
+                                                 (BF, 64, 295, -0.2), (BF, 64, 297, -0.2), (BF, 64, 297, 0.2), (BF, 128, 3, 0.1)])
+def test_attention_stays_inside_its_scratch(dtype, d, batch, scale):
+    """Either side of the 592 blocks from which on the SIMT kernel leaves no parts; what lies behind the scratch is as it was."""
+    c = Case(95, dtype, 2, 2, d, 16, [70] * (batch - 1) + [300], 2)
+    c.scale = scale
+    need = lib().poss_paged_attention_workspace_bytes(c.pages.cuda(), batch, 2, 2, c.tables.shape[1])
+    buf = torch.full((need + 65536,), 0xA5, dtype=torch.uint8, device="cuda")
+    got = c.run(workspace=buf[:need])
+    assert int(c.gpu_status) == 0 and (buf[need:] == 0xA5).all()
+    c.check(got) if scale > 0 else pg.check_attention(got, *c.want(), dtype, False)

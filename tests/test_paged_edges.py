@@ -23,3 +23,22 @@ def test_a_remap_into_new_outputs_refuses_what_the_other_refuses(lib, kw, code):
         code = WORKSPACE
     for f in (lib.poss_pages_remap, lib.poss_pages_remap_fresh):
         assert f(C.byref(p), *list(a.values()), None, None) == code
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(dtype=0), dict(page_slots=24), dict(head_dim=128), dict(head_dim=32)])
+def test_attention_scratch_holds_the_parts_that_are_made_and_stays_small(lib, kw):  # noqa: F811
+    """Parts are made where less than 592 blocks of 32 query rows would run: at most 64 for each, at most 592 + blocks in all.  Calls
+    of more blocks make none, so that scratch is bounded however large the call is: by those 1183 parts of 32 rows, or by the
+    tensor-core kernel's two partials of 256 rows for each of 160 CTAs and its plan."""
+    p = pool(**kw)
+    size = lambda b, r, hq, mp: lib.poss_paged_attention_workspace_bytes(C.byref(p), b, r, hq, mp)
+    row = (p.head_dim + 2) * 4
+    for hq in (2, 6, 16, 80):
+        for batch in (1, 2, 5, 37, 150, 293, 294, 600, 1024):
+            for rows in (1, 3, 33, 128):
+                for mp in (1, 2, 9, 4000):
+                    blocks = batch * 2 * -(-rows * (hq // 2) // 32)
+                    parts = min(-(-592 // blocks), -(-mp * p.page_slots // 32), 64)
+                    n = size(batch, rows, hq, mp)
+                    assert n >= (blocks * parts * 32 * row if parts > 1 else 1)
+                    assert n <= max(1183 * 32 * row, 160 * 2 * 256 * row + 8192) + 256
