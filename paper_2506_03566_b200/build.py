@@ -12,6 +12,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libposs.so")
 CALLS = os.path.join(HERE, "_paged_calls" + sysconfig.get_config_var("EXT_SUFFIX"))
+CALLS_TORCH = os.path.join(HERE, "_build", "_paged_calls.torch")   # the torch that it was built with
 SOURCES = ["kernels_basic.cu", "kernels_attention.cu", "kernels_attention_mma.cu", "kernels_tree.cu", "gemm_tc.cu", "attention_tc.cu", "poss_api.cu", "no_alloc.cu",
            "paged_pages.cu", "paged_attention.cu", "paged_attention_tc.cu", "beam_select.cu"]
 FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -30,6 +31,21 @@ def _stale(target: str, deps) -> bool:
         return True
     t = os.path.getmtime(target)
     return any(os.path.getmtime(d) > t for d in deps)
+
+
+def _torch_version() -> str:
+    import torch
+    return f"{torch.__version__} C++11 ABI {int(torch.compiled_with_cxx11_abi())}"
+
+
+def _calls_stale(deps) -> bool:
+    """_paged_calls reaches into torch's C++ by layout: it is as old as its sources, or as the torch that it was built with."""
+    try:
+        with open(CALLS_TORCH) as f:
+            built_with = f.read()
+    except OSError:
+        return True
+    return built_with != _torch_version() or _stale(CALLS, deps)
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
@@ -62,12 +78,13 @@ def build(force: bool = False, verbose: bool = False) -> str:
             sys.stderr.write(r.stdout)
             raise RuntimeError("link failed")
     src = os.path.join(CSRC, "paged_calls.cpp")
-    if force or _stale(CALLS, [src] + headers):
+    if force or _calls_stale([src] + headers):
         import torch
         root = os.path.dirname(torch.__file__)
         cuda = os.path.dirname(os.path.dirname(os.path.realpath(shutil.which(_nvcc()) or "/usr/local/cuda/bin/nvcc")))
         cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-shared",
-               f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}", "-I" + sysconfig.get_paths()["include"],
+               f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
+               f'-DPOSS_BUILT_WITH_TORCH="{_torch_version()}"', "-I" + sysconfig.get_paths()["include"],
                "-isystem", os.path.join(root, "include"),
                "-isystem", os.path.join(root, "include", "torch", "csrc", "api", "include"),
                "-isystem", os.path.join(cuda, "include"), src, "-o", CALLS, "-L" + HERE, "-l:" + os.path.basename(OUT),
@@ -78,6 +95,8 @@ def build(force: bool = False, verbose: bool = False) -> str:
         if r.returncode:
             sys.stderr.write(r.stdout)
             raise RuntimeError("g++ failed on paged_calls.cpp")
+        with open(CALLS_TORCH, "w") as f:
+            f.write(_torch_version())
     return OUT
 
 

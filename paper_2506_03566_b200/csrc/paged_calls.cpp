@@ -378,4 +378,8 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_paged_calls", nullptr, -1, method
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__paged_calls() { return PyModule_Create(&module); }
+PyMODINIT_FUNC PyInit__paged_calls() {
+  PyObject* m = PyModule_Create(&module);
+  if (m && PyModule_AddStringConstant(m, "built_with_torch", POSS_BUILT_WITH_TORCH)) Py_CLEAR(m);
+  return m;
+}

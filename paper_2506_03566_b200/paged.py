@@ -20,7 +20,7 @@ _module = None
 
 
 def _calls():
-    """The module of csrc/paged_calls.cpp.  Raises if it is missing."""
+    """The module of csrc/paged_calls.cpp.  Raises if it is missing, or was built with another torch."""
     global _module
     if _module is None:
         load_library()
@@ -28,6 +28,10 @@ def _calls():
             from . import _paged_calls as module
         except ImportError as e:
             raise ImportError(f"_paged_calls not built ({e}); run python -m paper_2506_03566_b200.build") from e
+        from .build import _torch_version
+        if module.built_with_torch != _torch_version():
+            raise ImportError(f"_paged_calls was built with torch {module.built_with_torch}, this is {_torch_version()}; run "
+                              "python -m paper_2506_03566_b200.build")
         module.bind(PossError)
         _module = module
     return _module

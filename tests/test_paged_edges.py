@@ -42,3 +42,16 @@ def test_attention_scratch_holds_the_parts_that_are_made_and_stays_small(lib, kw
                     n = size(batch, rows, hq, mp)
                     assert n >= (blocks * parts * 32 * row if parts > 1 else 1)
                     assert n <= max(1183 * 32 * row, 160 * 2 * 256 * row + 8192) + 256
+
+
+def test_the_module_of_the_calls_is_built_anew_for_another_torch(lib, monkeypatch):  # noqa: F811
+    """It reaches into torch's C++ by layout: neither the build nor the package goes on with one built for another version."""
+    import torch
+    from paper_2506_03566_b200 import build, paged
+    assert not build._calls_stale([])
+    assert paged._calls().built_with_torch == build._torch_version()
+    monkeypatch.setattr(torch, "__version__", "1.2.3")
+    assert build._calls_stale([])
+    monkeypatch.setattr(paged, "_module", None)
+    with pytest.raises(ImportError, match="1.2.3.*build"):
+        paged._calls()
