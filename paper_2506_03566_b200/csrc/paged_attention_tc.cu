@@ -17,8 +17,9 @@
 //     or behind the last slot is read from behind the pool: zeros.  The next segment's queries come the same way while the
 //     last one ends;
 //   * S = Q K^T (fp32, TMEM); the softmax thread masks its row of S in place where the tile reaches the tree, takes its
-//     maximum, writes P = 2^(s - m) as bf16 over S in TMEM; O += P V with P as the TMEM operand;
-//   * the reference maximum m moves only when a row's maximum has grown by more than 2^8 (P stays below 2^8, which bf16
+//     maximum, writes P = 2^(s - m) over S in TMEM as the sum of two bf16; O += P V with P as the TMEM operand, two products
+//     per 16 keys;
+//   * the reference maximum m moves only when a row's maximum has grown by more than 2^8 (P stays below 2^8, which two bf16
 //     and the fp32 sums hold as well as 1): then the thread scales its row of O in TMEM.  Otherwise O is never touched;
 //   * a slot's scores have two buffers: while its softmax works on one tile, the products of the tile before and of the tile
 //     behind run.
@@ -28,8 +29,9 @@
 // are set to zero, and infinities and NaN of tree slots too, in shared memory; the rows that do see such a slot get them
 // added at the end.
 //
-// The probabilities are rounded to bf16 (half a step, 2^-8): the second product's error stays near that of the output's
-// own rounding.  Sums, maxima and accumulators are fp32.
+// A probability is cut to bf16 and what that leaves over rounded to bf16, 2^-15 of it in all; the kernel of the contiguous caches
+// splits it as well.  With one bf16 (2^-8) the output's error is 1.4 times that of its own rounding and up to 3.3 times the bound
+// that holds there; 16 trees of 61 rows over up to 8191 slots would take 126 us for 148.  Sums, maxima and accumulators are fp32.
 //
 // What bounds it.  One token per sequence: the read of keys and values, once (16 sequences of up to 16384 slots, 834 MB: 137 us
 // with pages of 64, 6.1 TB/s; 153 us with pages of 16, whose boxes are 4 KB).  61 rows of 4 heads over the same slots: 244 us,
@@ -67,6 +69,7 @@ constexpr int MAX_STAGES = 8;
 constexpr float RESCALE_LOG2 = 8.f;
 constexpr uint32_t TMEM_COLS = 512;
 constexpr int S_COLS = 2 * KT;          // a slot's scores: two buffers, in turn (P lies over its scores)
+constexpr int P_COLS = KT / 2;          // a tile's probabilities as bf16; what they leave over lies behind them
 
 template <int HD> struct Shape {
   static constexpr int CB = HD / 64;                      // 64-column blocks
@@ -378,16 +381,22 @@ __device__ __forceinline__ float max32(const uint32_t* s, float m) {
   a = max3(a, __uint_as_float(s[30]), __uint_as_float(s[31]));
   return max3(a, b, m);
 }
-// p = 2^(s * scale + off) for 32 scores, packed to bf16; their sum goes to l0, l1.  (A part of the 2^x as a polynomial on the
+// p = 2^(s * scale + off) for 32 scores as bf16, and what that leaves over in `rest`; their sum goes to l0, l1.  (A part of the 2^x as a polynomial on the
 // multiply-add pipe was measured too: it loses, 261 against 249 us for 16 trees of 61 rows over 16383 slots.)
-__device__ __forceinline__ void exp32(const uint32_t* s, float2 scale, float2 off, uint32_t* p, float2& l0, float2& l1) {
+__device__ __forceinline__ void exp32(const uint32_t* s, float2 scale, float2 off, uint32_t* p, uint32_t* rest, float2& l0, float2& l1) {
 #pragma unroll
   for (int x = 0; x < 32; x += 2) {
     const float2 a = fma2(make_float2(__uint_as_float(s[x]), __uint_as_float(s[x + 1])), scale, off);
     const float2 e = make_float2(ex2(a.x), ex2(a.y));
     if (x & 2) l1 = add2(l1, e);
     else l0 = add2(l0, e);
-    p[x >> 1] = pack_bf16(e.x, e.y);
+    // cut, not rounded, and a little short, so that the rest of what is above 0 is too: an infinite value that is seen would
+    // otherwise meet a rest of 0 or below and come out as NaN
+    const float2 t = fma2(e, make_float2(1.f - 0x1p-20f, 1.f - 0x1p-20f), make_float2(0.f, 0.f));
+    const uint32_t tx = __float_as_uint(t.x), ty = __float_as_uint(t.y);
+    p[x >> 1] = __byte_perm(tx, ty, 0x7632);
+    const float2 d = add2(e, make_float2(__uint_as_float((tx & 0xffff0000u) ^ 0x80000000u), __uint_as_float((ty & 0xffff0000u) ^ 0x80000000u)));
+    rest[x >> 1] = pack_bf16(d.x, d.y);                 // (d is exact)
   }
 }
 __device__ __forceinline__ void softmax_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
@@ -593,7 +602,7 @@ __global__ void __launch_bounds__(N_THREADS, 1) k_paged_attn_tc(const __grid_con
         tc_fence_after();
         const bool missing = *(volatile uint8_t*)&c.gone[(tiles_before + t) % GONE_RING] != 0;   // (written before the keys' copies)
         if (live) {
-          uint32_t sa[32], sb[32], p[32];
+          uint32_t sa[32], sb[32], p[32], rest[32];
           tmem_ld32(t_s + buf * KT, sa);
           tmem_ld32(t_s + buf * KT + 32, sb);
           tmem_wait_ld();
@@ -636,9 +645,10 @@ __global__ void __launch_bounds__(N_THREADS, 1) k_paged_attn_tc(const __grid_con
           const float off = m == -INFINITY ? 0.f : -m;  // nothing seen so far: 2^(-inf) = 0
           const float2 of = make_float2(off, off);
           float2 l0 = make_float2(0.f, 0.f), l1 = l0;
-          exp32(sa, sc, of, p, l0, l1);
-          exp32(sb, sc, of, p + 16, l0, l1);
+          exp32(sa, sc, of, p, rest, l0, l1);
+          exp32(sb, sc, of, p + 16, rest + 16, l0, l1);
           tmem_st32(t_s + buf * KT, p);                 // (over the scores)
+          tmem_st32(t_s + buf * KT + P_COLS, rest);
           l += (l0.x + l0.y) + (l1.x + l1.y);
           tmem_wait_st();
         }
@@ -865,12 +875,18 @@ __global__ void __launch_bounds__(N_THREADS, 1) k_paged_attn_tc(const __grid_con
           const uint32_t v = v_lo + v_at * (Z::TILE >> 7), acc = y > 0;
           if (keys >= KT) {
             umma_bf16_ts(d_o, d, pack64(v, v_hi), idesc_o, acc);
+            umma_bf16_ts(d_o, d + P_COLS, pack64(v, v_hi), idesc_o, 1u);
 #pragma unroll
-            for (int ks = 1; ks < KT / 16; ++ks)          // 16 keys = 2048 bytes further each
+            for (int ks = 1; ks < KT / 16; ++ks) {        // 16 keys = 2048 bytes further each
               umma_bf16_ts(d_o, d + ks * 8, pack64(v + ks * 128, v_hi), idesc_o, 1u);
+              umma_bf16_ts(d_o, d + P_COLS + ks * 8, pack64(v + ks * 128, v_hi), idesc_o, 1u);
+            }
           } else {
 #pragma unroll 1
-            for (int ks = 0; ks * 16 < keys; ++ks) umma_bf16_ts(d_o, d + ks * 8, pack64(v + ks * 128, v_hi), idesc_o, ks ? 1u : acc);
+            for (int ks = 0; ks * 16 < keys; ++ks) {
+              umma_bf16_ts(d_o, d + ks * 8, pack64(v + ks * 128, v_hi), idesc_o, ks ? 1u : acc);
+              umma_bf16_ts(d_o, d + P_COLS + ks * 8, pack64(v + ks * 128, v_hi), idesc_o, 1u);
+            }
           }
           umma_commit(b_o + buf * 8);
           release(b_ve + v_at);

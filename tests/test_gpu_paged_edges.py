@@ -187,3 +187,35 @@ def test_attention_stays_inside_its_scratch(dtype, d, batch, scale):
     got = c.run(workspace=buf[:need])
     assert int(c.gpu_status) == 0 and (buf[need:] == 0xA5).all()
     c.check(got) if scale > 0 else pg.check_attention(got, *c.want(), dtype, False)
+
+
+@pytest.mark.parametrize("hq,hkv,d,page,prefix,rows,n_rows", [
+    (32, 8, 128, 16, [1024], 1, None), (8, 2, 128, 64, [700, 31, 2000], 61, [61, 60, 7]), (8, 2, 64, 32, [300, 0, 17, 129], 25, [25, 1, 24, 13]),
+    (4, 1, 64, 256, [257], 128, None), (4, 4, 128, 16, [5000, 63], 3, None), (128, 1, 128, 16, [333], 3, None),
+])
+def test_tensor_core_attention_keeps_sixteen_bits_of_a_probability(hq, hkv, d, page, prefix, rows, n_rows):
+    """The bounds of the plain form without the 2^-8 that a probability in one bf16 would need: 2^-15 of A instead, the cut and the
+    rounding of its two parts.  And the bound of the contiguous call: 2^-8 of the element, 2e-3 of the output's RMS."""
+    c = Case(96, BF, hq, hkv, d, page, prefix, rows, n_rows)
+    got = c.run(out=torch.zeros(c.b, rows, hq, d, dtype=BF, device="cuda"))
+    want, tol, big = c.want()
+    pg.check_attention(got, want, tol + big * 2.0 ** -15, big, BF, False)
+    live = ~torch.isnan(want)
+    err, w = (got.double().cpu() - want).abs()[live], want[live]
+    assert (err <= 2.0 ** -8 * w.abs() + 2e-3 * w.pow(2).mean().sqrt()).all()
+
+
+@pytest.mark.parametrize("d,page", [(64, 16), (128, 64)])
+@pytest.mark.parametrize("rows", [1, 9, 61])
+def test_an_infinite_value_of_a_committed_slot_comes_out_as_infinity(d, page, rows):
+    """Every row sees it: +inf or -inf in its column whatever the slot's score, the greatest one among them; all else as without it."""
+    c = Case(97, BF, 8, 2, d, page, [200, 77], rows)
+    want, tol, big = c.want()
+    c.q[1] = 0.0                                                  # every slot's score is the row's greatest
+    c.pages[0, int(c.tables[0][0]), 1, :, 3, 5] = math.inf
+    c.pages[0, int(c.tables[1][0]), 1, :, 7, 9] = -math.inf
+    got = c.run().cpu().float()
+    assert (got[0, :, :, 5] == math.inf).all() and (got[1, :, :, 9] == -math.inf).all()
+    keep = [i for i in range(d) if i != 5]
+    pg.check_attention(got[:1, ..., keep], want[:1, ..., keep], tol[:1, ..., keep], big[:1, ..., keep], BF, True)
+    assert torch.isfinite(got[1, ..., [i for i in range(d) if i != 9]]).all()
