@@ -65,11 +65,12 @@ POSS_API size_t poss_paged_attention_workspace_bytes(const poss_page_pool* pool,
  * has no influence, whatever it holds (infinities and NaN too).  A missing page's slots count as unseen, a sequence
  * with lengths out of range has no rows (status).
  * out must not overlap q.  rows <= POSS_MAX_ROWS.  bf16 with head dimension 64 or 128, a page size of 16, 32, 64, 128 or
- * 256 slots, at most 128 query heads per KV head (G) and a positive scale runs on the tensor cores, where batch * n_kv_heads *
- * ceil(rows / (2 * floor(128 / G))) * ceil(max_pages * page_slots / 64) < 2^31; the probabilities enter the second
- * product as the sum of two bf16 there (2^-15 relative), sums and the output's accumulation are fp32.  How the keys are
- * cut, and so the last bits of a result, depends on the whole batch's lengths; equal calls give equal bits.  Errors: INVALID, SHAPE, CAPACITY, WORKSPACE (too small, not 256-byte
- * aligned), CUDA. */
+ * 256 slots, at most 128 query heads per KV head (G) and a positive scale runs on the tensor cores.  There the
+ * probabilities enter the second product as the sum of two bf16 (2^-15 relative), sums and the output's accumulation are
+ * fp32, scores times scale must stay below 2^29 in size (else the row is not finite), and batch * n_kv_heads *
+ * ceil(rows / (2 * floor(128 / G))) * ceil(max_pages * page_slots / 64) must be below 2^31 (else CAPACITY).  How the keys
+ * are cut, and so the last bits of a result, depends on the whole batch's lengths; equal calls give equal bits.
+ * Errors: INVALID, SHAPE, CAPACITY, WORKSPACE (too small, not 256-byte aligned), CUDA. */
 POSS_API int poss_paged_tree_attention(const poss_page_pool* pool, int layer, const void* kv_pages, const int32_t* tables,
                               int max_pages, int batch, int rows, int n_q_heads, const void* q, int64_t ld_q,
                               const int32_t* prefix_len, const int32_t* n_rows, const uint64_t* anc_mask, float scale,

@@ -219,3 +219,23 @@ def test_an_infinite_value_of_a_committed_slot_comes_out_as_infinity(d, page, ro
     keep = [i for i in range(d) if i != 5]
     pg.check_attention(got[:1, ..., keep], want[:1, ..., keep], tol[:1, ..., keep], big[:1, ..., keep], BF, True)
     assert torch.isfinite(got[1, ..., [i for i in range(d) if i != 9]]).all()
+
+
+@pytest.mark.parametrize("dtype,d,page", [(BF, 128, 16), (BF, 64, 64), (F32, 64, 24)])
+@pytest.mark.parametrize("size", [1e3, 1e6, 2.0 ** 28])
+def test_scores_of_any_size_up_to_the_documented_one(dtype, d, page, size):
+    """Queries and keys of one column each, so that scores are single products; the greatest one takes all where they lie apart."""
+    c = Case(98, dtype, 4, 2, d, page, [150, 3], 9)
+    c.q[..., 1:] = 0
+    c.pages[:, :, 0, :, :, 1:] = 0
+    c.scale = 0.25
+    top = max(float(c.q.float().abs().max()) * float(c.pages[:, :, 0].float().abs().max()) * 0.25, 1.0)
+    for x in (c.q, c.pages[:, :, 0]):
+        x *= 2.0 ** math.floor(0.5 * math.log2(size / top))       # (exact)
+    want, tol, big = c.want()
+    # the plain bound holds a score error e in exp(e) ~ 1 + e; where e is not small the row's greatest score and the others lie a
+    # whole score step apart or tie, and the output is within the sum of both weights' reach: 2 A
+    tol = torch.minimum(tol, 2 * big)
+    got = c.run()
+    assert int(c.gpu_status) == 0
+    pg.check_attention(got, want, tol, big, dtype, dtype == BF)
