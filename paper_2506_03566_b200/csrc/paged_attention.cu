@@ -317,7 +317,7 @@ void launch_simt(Launcher& L, const SimtArgs& s, const void* pool) {
 }  // namespace
 
 size_t paged_attn_simt_workspace(int batch, int rows, int Hq, int Hkv, int d) {
-  const long long blocks = (long long)batch * Hkv * ((rows * (Hq / Hkv) + QB - 1) / QB);
+  const long long blocks = (long long)batch * Hkv * (((long long)rows * (Hq / Hkv) + QB - 1) / QB);
   return (size_t)(SIMT_BLOCKS + (blocks < SIMT_BLOCKS ? blocks : SIMT_BLOCKS - 1)) * QB * (d + 2) * 4;
 }
 
@@ -365,7 +365,7 @@ int poss_paged_tree_attention(const poss_page_pool* pool, int layer, const void*
   if (rc != POSS_OK) return rc;
   if (rows > POSS_MAX_ROWS) return POSS_E_CAPACITY;
   // a launch's grid: query tiles of 32 rows times KV heads
-  if ((long long)pool->n_kv_heads * ((rows * (n_q_heads / pool->n_kv_heads) + 31) / 32) > 65535) return POSS_E_CAPACITY;
+  if (pool->n_kv_heads * (((long long)rows * (n_q_heads / pool->n_kv_heads) + 31) / 32) > 65535) return POSS_E_CAPACITY;
   if (!kv_pages || !tables || !q || !prefix_len || !anc_mask || !out) return POSS_E_INVALID;
   const int es = pool->dtype == POSS_BF16 ? 2 : 4;
   if (ld_q < (int64_t)n_q_heads * pool->head_dim || (ld_q * es) % 16) return POSS_E_INVALID;

@@ -55,3 +55,12 @@ def test_the_module_of_the_calls_is_built_anew_for_another_torch(lib, monkeypatc
     monkeypatch.setattr(paged, "_module", None)
     with pytest.raises(ImportError, match="1.2.3.*build"):
         paged._calls()
+
+
+@pytest.mark.parametrize("heads", [1 << 26, (1 << 31) - 2, 1 << 20])
+def test_attention_counts_its_query_tiles_in_64_bits(lib, heads):  # noqa: F811
+    """rows times query heads past 2^31 are more tiles than a launch has room for, and no small number of them."""
+    a = [at(0), at(1), 8, 1, 128, heads, at(2), heads * 64, at(3), None, at(4), 1.0, at(5) + (1 << 50), at(90), 1 << 60, None, None]
+    p = pool()
+    assert lib.poss_paged_tree_attention(C.byref(p), 0, *a) == CAPACITY
+    assert lib.poss_paged_attention_workspace_bytes(C.byref(p), 1, 128, heads, 8) >= 592 * 32 * 66 * 4
