@@ -7,10 +7,11 @@
 //   a lower bound of the chunk's K-th best value comes for free with the maxima -- the least of K (8 or 16) maxima of
 //   disjoint parts of the chunk has K values at or above it -- so only the values at or above that bound (a few dozen
 //   of 8192 for logits in no order) are ever compared with one another.
-// Measured (fp32, in a captured graph): 32 groups of 8 beams over 128256 tokens, 131 MB, 40 us: 29 the first kernel (4.5 TB/s; the
-// registers of a chunk allow 4 blocks per SM, whose reductions and compares leave the memory idle a third of the time), 11 the
-// second, a chain of trips to memory and barriers in 32 blocks.  4 beams over 32000 tokens: 10.0 us, 4.2 and 5.8; the chunks stay
-// at 8192 there too: with 2048 it takes 8.4, but 8 beams over 128256 take 12.2 for 9.8, since the second kernel's lists grow.
+// Measured (fp32, in a captured graph): 32 groups of 8 beams over 128256 tokens, 131 MB, 43 us: 31 the first kernel (4.2 TB/s; the
+// registers of a chunk allow 4 blocks per SM, whose reductions and compares leave the memory idle a third of the time), 12 the
+// second, a chain of trips to memory and barriers in 32 blocks.  (A finished beam's logits are not read: with 13 % of them 114 MB,
+// 28 and 12 us.)  4 beams over 32000 tokens: 10.4 us, 4.2 and 6.2.  The chunks stay at 8192 there too: with 2048 it took 8.4 for
+// 10.0, but 8 beams over 128256 12.2 for 9.8, since the second kernel's lists grow.
 #include "paged.cuh"
 #include <float.h>
 

@@ -7,8 +7,8 @@
 // every key and value that it reads from shared memory; a thread holds 2 rows x 4 keys of the scores and 2 rows x d/8
 // columns of the output.  With ns > 1 the parts are left in scratch and a second kernel merges them in key order.
 // What bounds it: fp32 multiply-adds and the shared-memory reads that feed them for trees over long contexts (16 trees of 61
-// rows over up to 8191 slots in bf16: 4.6 ms, the tensor-core kernel 0.14), the trips to memory of a 32-key step and of the merge for
-// short ones (3 trees of 15 rows over up to 517 slots, fp32: 12.9 us).
+// rows over up to 8191 slots in bf16: 4.6 ms, the tensor-core kernel 0.15), the trips to memory of a 32-key step and of the merge for
+// short ones (3 trees of 15 rows over up to 517 slots, fp32: 12.3 us).
 #include "paged_attention.cuh"
 #include <math.h>
 

@@ -3,7 +3,7 @@
 // The G = Hq / Hkv query heads of a KV head and a sequence's tree rows form one matrix of query rows (row * G + head), cut
 // into items of up to 256: (sequence, KV head, two slots of floor(128 / G) tree rows).  A unit of work is one item's product
 // with 64 keys; the units of the whole batch, in order of sequence, head, item and key, are cut into one contiguous range per
-// CTA, one CTA per SM, so that every SM streams the same number of keys however long the sequences are.  The part of an item that
+// CTA, one CTA per SM, so that every SM streams the same number of key tiles however long the sequences are.  The part of an item that
 // falls into one CTA is a segment: one pass over its keys with the running maximum and sum of a softmax.  A segment that is
 // the whole item writes the output, any other leaves fp32 partials that a second kernel merges in key order.  Where items are
 // short the ranges end at items instead (Plan).
@@ -31,17 +31,22 @@
 //
 // A probability is cut to bf16 and what that leaves over rounded to bf16, 2^-15 of it in all; the kernel of the contiguous caches
 // splits it as well.  With one bf16 (2^-8) the output's error is 1.4 times that of its own rounding and up to 3.3 times the bound
-// that holds there; 16 trees of 61 rows over up to 8191 slots would take 126 us for 148.  Sums, maxima and accumulators are fp32.
+// that holds there; 16 trees of 1 to 61 rows over up to 8191 slots would take 126 us for 148 in a graph.  Sums, maxima and
+// accumulators are fp32.
 //
-// What bounds it.  One token per sequence: the read of keys and values, once (16 sequences of up to 16384 slots, 834 MB: 137 us
-// with pages of 64, 6.1 TB/s; 153 us with pages of 16, whose boxes are 4 KB).  61 rows of 4 heads over the same slots: 244 us,
-// 830 TFLOP/s; a step of 64 keys and two slots takes 2050 cycles, of which the products alone need 1260 (M128 N64 K16 50
-// cycles, M128 N128 K16 64) and the exponentials 1024.  The rest is latency between the roles: a slot's product lane
-// spends 1000 cycles a step on barriers, commits and operand registers, the softmax 850 on its loads, maxima and barriers, and
-// both slots come to run in step, so that neither fills the other's gaps.  Measured against 246 us and not better: 16 softmax warps
-// of half a row each, 251 us; a lane for each kind of product in place of each slot, 257 us; three product lanes, 252 us; a late
-// start of slot 1, 247 us.  Short sequences: 17 us for 1 row over 1024 slots, 6 us of it before the first scores (lengths, pages,
-// the first copies), the rest two or three steps, partials and the merge's launch.
+// What bounds it.  One token per sequence: the read of keys and values, once (16 sequences of up to 16384 slots, 834 MB: 146 us
+// with pages of 64, 5.7 TB/s; 169 us with pages of 16, whose boxes are 2 KB; in a loop the power limit lowers the clock).  61 rows
+// of 4 heads over the same slots: 298 us, 684 TFLOP/s of scores and one output product; a step of 64 keys and two slots takes 1.7
+// us, of which the products alone need some 1800 cycles (M128 N64 K16 50 cycles, M128 N128 K16 64, two of these per 16 keys) and the
+// exponentials 1024.  The rest is latency between the roles: barriers, commits and operand registers of a slot's product lane, loads,
+// maxima and barriers of its softmax, and both slots come to run in step, so that neither fills the other's gaps.  With
+// probabilities in one bf16, where the same took 246 us, these were measured and not better: 16 softmax warps of half a row each,
+// 251 us; a lane for each kind of product in place of each slot, 257 us; three product lanes, 252 us; a late start of slot 1,
+// 247 us.  Short sequences: 17 us for 1 row over 1024 slots, 6 us of it before the first scores (lengths, pages, the first copies),
+// the rest two or three steps, partials and the merge's launch.
+//
+// Every CTA gets the same number of units, but a unit of an item with rows for both slots takes twice the work of one whose slots
+// take the tiles in turn: with 16 trees of 1 to 61 rows the fullest CTA has 1.33 to 1.37 times the mean, with one of 81 rows 1.42.
 //
 // Every wait is bounded; on expiry the CTA raises POSS_E_TIMEOUT, runs through its (bounded) walk without meaning, waits
 // (bounded) for its copies in flight, frees its TMEM and returns.
@@ -144,8 +149,8 @@ constexpr int CTL_BYTES = 3 * 1024;
 static_assert(sizeof(Ctl) <= CTL_BYTES, "the control block lies behind the tiles");
 
 // CTAs that share `total` units (MIN_UNITS each at least), and the cut: the first total % grid of them take one unit more.
-// Two units and not one: partials and their merge cost more than a second step where few rows meet few keys (1 row over 1024 slots:
-// 18.0 against 19.5 us, over 100 slots 11.1 against 12.6); 61 rows over 100 slots would have 16.2 for 21.1, long ones are alike.
+// Two units and not one: partials and their merge cost more than a second step where few rows meet more keys than the CTAs
+// can take one unit each of (1 row over 1024 slots: 17.4 against 18.2 us; over 400 it would be 13.3 for 15.2, the others are alike).
 constexpr uint32_t MIN_UNITS = 2;
 __device__ __forceinline__ int unit_grid(uint32_t total, uint32_t ctas) {
   const uint32_t n = (total + MIN_UNITS - 1) / MIN_UNITS;
@@ -180,9 +185,9 @@ __device__ __forceinline__ uint32_t inclusive_scan(uint32_t x) {
   return x;
 }
 // Cutting costs the partials' way through L2 and the merge, the more the more rows there are: units that whole items may make the
-// longest range longer.  Measured cut / whole: 61 rows of 4 heads over 100 slots (2 and 3 units) 21.4 / 18.7 us, 7 ragged trees of 25
-// rows over up to 300 slots (2 and 6) 14.1 / 12.0, 16 x 61 rows over up to 500 (8 and 9) 44 / 43; 4 x 61 rows over up to 1000 (4 and 17)
-// 28 / 34, 1 row over 400 (2 and 6) 12.3 / 15.0.
+// longest range longer.  Measured cut / whole: 61 rows of 4 heads over 100 slots (2 and 3 units) 19.5 / 15.6 us, 7 ragged trees of 25
+// rows over up to 300 slots (2 and 6) 13.5 / 11.2, 16 x 61 rows over up to 500 (8 and 9) 41.8 / 39.3; 4 x 61 rows over up to 1000 (4 and 17)
+// 25.9 / 34.1, 1 row over 1024 17.2 / 22.7, over 400 (2 and 6) 14.9 / 14.2.
 __device__ __forceinline__ uint32_t whole_extra(int row_cap) { return 2 + row_cap / 32; }
 __device__ __forceinline__ Plan make_plan(const TcArgs& k, uint32_t ctas, SeqWork* mine) {
   const int lane = threadIdx.x & 31;
@@ -362,7 +367,7 @@ __device__ __forceinline__ float max32(const uint32_t* s, float m) {
   return max3(a, b, m);
 }
 // p = 2^(s * scale + off) for 32 scores as bf16, and what that leaves over in `rest`; their sum goes to l0, l1.  (A part of the 2^x as a polynomial on the
-// multiply-add pipe was measured too: it loses, 261 against 249 us for 16 trees of 61 rows over 16383 slots.)
+// multiply-add pipe was measured too, with one bf16 each: it loses, 261 against 249 us for 16 trees of 61 rows over 16383 slots.)
 __device__ __forceinline__ void exp32(const uint32_t* s, float2 scale, float2 off, uint32_t* p, uint32_t* rest, float2& l0, float2& l1) {
 #pragma unroll
   for (int x = 0; x < 32; x += 2) {

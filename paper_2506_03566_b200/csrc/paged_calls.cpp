@@ -4,7 +4,7 @@
 // Why not ctypes like the calls of poss.h: those run for hundreds of microseconds on the GPU, most of these for 2 to 20, and a
 // loop of small calls runs at the speed of the host.  Checks in Python with a ctypes call took 8.8 us for a commit, 20 us for a
 // remapping or a beam step and 23 us for an append with its attention, mostly attribute reads and argument conversions; here
-// they take 4.2, 11 and 10 us, the kernels' launches among them.
+// they take 3.8, 11 and 10 us, the kernels' launches among them.
 #include <Python.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>

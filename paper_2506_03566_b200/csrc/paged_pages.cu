@@ -144,7 +144,7 @@ __global__ void __launch_bounds__(256) k_pages_compact(PageGeo g, char* pool, co
 //   3  pages without a holder, in order, up to the number needed -> the fresh places, in order
 // A page is free after the call iff step 1 leaves it without holders: where every holder is a writer the last stays.
 // One block and not more: the steps depend on one another over the whole pool, and a grid's barrier costs more than the
-// few thousand counts do.  64 sequences of 32 pages: some 14 us beside the copies' 31; 4 sequences: 4 beside 3, a chain of trips to
+// few thousand counts do.  64 sequences of up to 8 pages: 9.6 us beside the copies' 20 to 36; 4 of 44 pages: 5.5 beside 1.5, a chain of trips to
 // memory and barriers.
 constexpr int REMAP_THREADS = 1024;
 
@@ -206,7 +206,7 @@ __device__ __forceinline__ int block_scan(int v, int* warp_sums, int* total) {
 }
 
 // SMEM: the counts and the free list lie in shared memory (pools of up to SMEM_PAGES pages) and not in scratch: an atomic or a look
-// there saves a trip to L2 each time (64 sequences of 32 pages, copies included, 48.6 -> 45.9 us; 4 sequences 8.1 -> 6.8).
+// there saves a trip to L2 each time (64 sequences of up to 8 pages, copies included, 49.0 -> 46.1 us; 4 of 44 pages 8.4 -> 7.0).
 constexpr int SMEM_PAGES = 12 * 1024;
 template <bool SMEM>
 __global__ void __launch_bounds__(REMAP_THREADS, 1) k_pages_remap(RemapArgs a) {
@@ -340,7 +340,8 @@ __global__ void __launch_bounds__(REMAP_THREADS, 1) k_pages_remap(RemapArgs a) {
 }
 
 // remap: the kept slots of the partly filled pages that were left.  One block per (layer, keys / values, sequence); the
-// slots of one head are one run of bytes.  Bound by memory: 64 pages in 32 layers, 178 MB read and written, 31 us (5.7 TB/s).
+// slots of one head are one run of bytes.  Bound by memory: 20 pages with 38 of 64 slots each on
+// average in 32 layers, 199 MB read and written, 36 us (5.5 TB/s).
 template <int ES>
 __global__ void __launch_bounds__(256) k_pages_copy(PageGeo g, char* pool, const int32_t* copies) {
   pdl_enter(POSS_K_PAGES_COPY);
