@@ -154,26 +154,23 @@ __global__ void __launch_bounds__(THREADS, 4) k_beam_lists(BeamArgs a, const T* 
       }
     }
   }
-  // Sum of exponentials below the chunk's maximum (an all-banned chunk: maximum -inf, sum 0): 2^(x log2 e - c) with c the
-  // rounded mx log2 e; what c leaves over is put right once for the sum.  It is 2^-4 at the most below 2^20, but grows with mx:
-  // behind 2^31 or so the power of it leaves fp32.  So larger maxima (finite masks: -1e10, the type's lowest value) take the
-  // differences first; those that count are exact there, and what overflows goes to -inf, whose power is 0.
+  // Sum of exponentials below the chunk's maximum (an all-banned chunk: maximum -inf, sum 0).  The differences come first: the
+  // maximum's own term is 1 exactly, so that no log-probability is above 0, and logits of any finite size (masks of -1e10, the type's
+  // lowest value) are safe; those that count are near the maximum, where differences lose nothing, and one that overflows is -inf,
+  // whose power is 0.  (2^(x log2 e - maximum log2 e) would be one operation less, but what the rounded second product leaves over
+  // grows with it: from 2^31 on its power leaves fp32.)
   float sum = 0.f;
-  const float L2E = 1.4426950408889634f;
-  if (fabsf(mx) < 0x1p20f) {
-    const float c = mx * L2E;
+  if (mx > -INFINITY) {
+    const float2 L2E = make_float2(1.4426950408889634f, 1.4426950408889634f), off = make_float2(-mx, -mx);
     float2 s0 = make_float2(0.f, 0.f), s1 = s0;
 #pragma unroll
     for (int j = 0; j < PER; j += 4) {
-      const float2 u = fma2(make_float2(x[j], x[j + 1]), make_float2(L2E, L2E), make_float2(-c, -c));
-      const float2 v = fma2(make_float2(x[j + 2], x[j + 3]), make_float2(L2E, L2E), make_float2(-c, -c));
+      const float2 u = fma2(add2(make_float2(x[j], x[j + 1]), off), L2E, make_float2(0.f, 0.f));
+      const float2 v = fma2(add2(make_float2(x[j + 2], x[j + 3]), off), L2E, make_float2(0.f, 0.f));
       s0 = add2(s0, make_float2(ex2(u.x), ex2(u.y)));   // 2^-22 relative
       s1 = add2(s1, make_float2(ex2(v.x), ex2(v.y)));
     }
-    sum = ((s0.x + s0.y) + (s1.x + s1.y)) * ex2(-fmaf(mx, L2E, -c));
-  } else if (mx > -INFINITY) {
-#pragma unroll
-    for (int j = 0; j < PER; ++j) sum += ex2((x[j] - mx) * L2E);
+    sum = (s0.x + s0.y) + (s1.x + s1.y);
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);

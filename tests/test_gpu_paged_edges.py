@@ -239,3 +239,17 @@ def test_scores_of_any_size_up_to_the_documented_one(dtype, d, page, size):
     got = c.run()
     assert int(c.gpu_status) == 0
     pg.check_attention(got, want, tol, big, dtype, dtype == BF)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("v", [3, 100, 8192, 50257])
+def test_no_continuation_scores_better_than_its_beam(dtype, v):
+    """Log-probabilities are 0 at the most, also where one token has nearly all of the probability: the scores of a search never rise."""
+    torch.manual_seed(85)
+    for spread in (1.0, 30.0, 300.0):
+        x = (torch.randn(16, 8, v, device="cuda") * spread).to(dtype)
+        x[::2, ::2] += 1000.0
+        s = -torch.rand(16, 8, device="cuda")
+        r = lib().poss_beam_select(x, s)
+        there = r["parents"] >= 0
+        assert (r["scores"][there] <= s.view(-1)[r["parents"][there].long()]).all()
