@@ -61,7 +61,8 @@ enum { POSS_K_OTHER = 0, POSS_K_GATHER_X = 1, POSS_K_EMBED_ROWS = 2, POSS_K_RMSN
        POSS_K_PAGES_REMAP = 30, POSS_K_PAGES_COPY = 31,
        POSS_K_GEMM_FC = 32, POSS_K_GEMM_QKV = 33, POSS_K_GEMM_O = 34, POSS_K_GEMM_GATE_UP = 35, POSS_K_GEMM_DOWN =
        36,        POSS_K_GEMM_LM_HEAD = 37, POSS_K_GEMM_OTHER = 38, POSS_K_BEAM_LISTS = 39,
-       POSS_K_BEAM_MERGE = 40, POSS_K_COUNT = 41 };
+       POSS_K_BEAM_MERGE = 40, POSS_K_ROTARY = 41, POSS_K_APPEND_ROTARY = 42, POSS_K_SLOT_MASS = 43,
+       POSS_K_EVICT_CHOOSE = 44, POSS_K_EVICT_MOVE = 45, POSS_K_TOKEN_LOGPROBS = 46, POSS_K_COUNT = 47 };
 POSS_API int poss_timeline_read(poss_ctx* ctx, int capacity, int32_t* h_kernel, int64_t* h_time_ns, int* h_count,
                        poss_stream stream);
 

@@ -1,5 +1,5 @@
 /*
- * poss_paged.h -- paged key/value caches and beam selection of the PosS library.
+ * poss_paged.h -- paged key/value caches, rotary positions, beam selection and token scores of the PosS library.
  *
  * The calls of poss.h work on one contiguous cache per sequence.  These work on a batch of sequences of any lengths
  * whose caches lie in pages of one pool, pages that sequences may share: tree-masked attention of all sequences in
@@ -37,7 +37,8 @@ typedef struct {
 } poss_page_pool;
 
 enum { POSS_MAX_PAGE_SLOTS = 1024,
-       POSS_MAX_PAGED_BATCH = 1024 };   /* sequences of one call */
+       POSS_MAX_PAGED_BATCH = 1024,     /* sequences of one call */
+       POSS_MAX_ROTARY_DIM = 512 };     /* elements of a head that turn */
 
 /* Writes the keys and values of every sequence's new rows into its pages of layer `layer`: row r of sequence b goes to
  * slot prefix_len[b] + r.  k, v [batch][rows][n_kv_heads][head_dim] (already rotated), consecutive rows ld_kv elements
@@ -48,6 +49,44 @@ enum { POSS_MAX_PAGE_SLOTS = 1024,
 POSS_API int poss_pages_append(const poss_page_pool* pool, int layer, void* kv_pages, const int32_t* tables,
                       int max_pages, int batch, int rows, const void* k, const void* v, int64_t ld_kv,
                       const int32_t* prefix_len, const int32_t* n_rows, int32_t* status, poss_stream stream);
+
+/* ---- rotary positions
+ * Pairs (u, v) of the first rot_dim (even) elements of a head turn: (u cos a - v sin a, v cos a + u sin a) * magnitude, a =
+ * position * freq[i] radians for pair i < rot_dim / 2.  interleaved 0: pair i is elements i and rot_dim / 2 + i; else elements 2i and
+ * 2i + 1.  Elements from rot_dim on stay as they are (magnitude does not touch them).  freq double[rot_dim / 2] on the device.
+ * Any position, far and negative ones too (the latter turn back), is as exact as a near one: angles are reduced in 64 bits; cosine and
+ * sine are fp32, the result is rounded once to its type.  rot_dim <= POSS_MAX_ROTARY_DIM. */
+
+/* Frequencies of the usual schemes, on the HOST: h_freq double[rot_dim / 2], freq[i] = theta^(-2i / rot_dim), theta > 1, and for
+ * contexts that are `factor` (>= 1) times longer than the original one of original_len tokens
+ *   LINEAR  all divided by factor
+ *   BASE    theta multiplied by factor^(rot_dim / (rot_dim - 2)) (rot_dim >= 4): the fastest stays, the slowest is divided by factor
+ *   BANDS   pairs that make more than `high` turns over original_len stay, those with less than `low` are divided by factor, between
+ *           them the kept share rises with the turns
+ *   RAMP    the same bounds, but the kept share falls with the pair's index, between the pairs (rounded outwards) that make `high` and
+ *           `low` turns
+ * low, high, original_len are used by the last two (0 < low < high).  Such models often want a magnitude too (0.1 ln factor + 1).
+ * Errors: INVALID, CAPACITY. */
+enum { POSS_ROTARY_PLAIN = 0, POSS_ROTARY_LINEAR = 1, POSS_ROTARY_BASE = 2, POSS_ROTARY_BANDS = 3, POSS_ROTARY_RAMP = 4 };
+POSS_API int poss_rotary_frequencies(double* h_freq, int rot_dim, double theta, int scaling, double factor, double low, double high,
+                            double original_len);
+
+/* Turns n rows of `heads` heads: x, out [n][heads][head_dim], consecutive rows ld_x / ld_out elements apart (>= heads * head_dim, a
+ * multiple of 16 bytes), 16-byte aligned; head_dim a multiple of 16 bytes (else SHAPE), n below 2^31.  positions int32[n].  out may be
+ * x (in place, ld_out = ld_x), else they do not overlap.  Errors: INVALID, SHAPE, CAPACITY. */
+POSS_API int poss_rotary(const void* x, int64_t ld_x, void* out, int64_t ld_out, int dtype, int64_t n, int heads, int head_dim,
+                const int32_t* positions, const double* freq, int rot_dim, int interleaved, float magnitude, poss_stream stream);
+
+/* poss_pages_append of rows that are not rotated yet, and the rotation of their queries, in one launch: k turned into the pages, v as
+ * it is, q [batch][rows][n_q_heads][head_dim] turned into out_q of the same shape (rows ld_q and ld_out_q elements apart; out_q may be
+ * q; n_q_heads 0: no queries).  positions int32[batch][rows]; NULL: the slot that the row goes to.  (A tree's row sits at its prefix plus
+ * its depth; after an eviction positions go on where they were and slots do not.)  All else as poss_pages_append; the queries of a row
+ * whose page is missing are turned all the same, rows behind n_rows leave out_q as it was.  Errors: INVALID, SHAPE, CAPACITY. */
+POSS_API int poss_pages_append_rotary(const poss_page_pool* pool, int layer, void* kv_pages, const int32_t* tables, int max_pages,
+                             int batch, int rows, const void* k, const void* v, int64_t ld_kv, int n_q_heads, const void* q,
+                             int64_t ld_q, void* out_q, int64_t ld_out_q, const int32_t* prefix_len, const int32_t* n_rows,
+                             const int32_t* positions, const double* freq, int rot_dim, int interleaved, float magnitude,
+                             int32_t* status, poss_stream stream);
 
 /* Scratch of poss_paged_tree_attention, in bytes (0: arguments out of range).  It grows with batch, rows and
  * max_pages, so one made for the largest call serves the smaller ones. */
@@ -76,6 +115,47 @@ POSS_API int poss_paged_tree_attention(const poss_page_pool* pool, int layer, co
                               const int32_t* prefix_len, const int32_t* n_rows, const uint64_t* anc_mask, float scale,
                               void* out, void* workspace, size_t workspace_bytes, int32_t* status,
                               poss_stream stream);
+
+/* ---- caches that are kept short by the attention that their slots draw
+ * mass float[n_layers][batch][n_kv_heads][mass_slots], mass_slots >= max_pages * page_slots, belongs to the sequences of a batch (not to
+ * pages: sequences that share pages weigh their slots each by itself; a forked sequence starts with a copy of its parent's). */
+
+/* poss_paged_tree_attention, which also adds up the weight that each slot draws in this layer: with P the probabilities of the rows of
+ * sequence b and the query heads of KV head h,
+ *   W[s] = sum over rows r < n_rows[b] and those heads of row_weights[b][r] * P[s],
+ *   mass[layer][b][h][s] += W[s] for s < prefix_len[b],  = W[s] for the rows' own slots prefix_len[b] <= s < prefix_len[b] + n_rows[b].
+ * (The rows' slots are new: what mass held there is of no account.)  All other entries, and those of a sequence without rows, are left
+ * as they were; an unseen slot draws nothing, a missing page's slots neither.  row_weights float[batch][rows] (NULL: 1 each), such as a
+ * tree's draft probabilities; those behind n_rows are not read.  Terms are added in fp32, in one order: equal calls give equal bits.
+ * 2^x is off by 2^-22, the maxima and sums are the attention's own.  mass must not overlap q, out or row_weights.  Scratch: its own
+ * size (below).  All else, errors too, as poss_paged_tree_attention. */
+POSS_API size_t poss_paged_attention_mass_workspace_bytes(const poss_page_pool* pool, int batch, int rows, int n_q_heads,
+                                                 int max_pages);
+POSS_API int poss_paged_tree_attention_mass(const poss_page_pool* pool, int layer, const void* kv_pages, float* mass,
+                                   int64_t mass_slots, const int32_t* tables, int max_pages, int batch, int rows, int n_q_heads,
+                                   const void* q, int64_t ld_q, const int32_t* prefix_len, const int32_t* n_rows,
+                                   const uint64_t* anc_mask, const float* row_weights, float scale, void* out, void* workspace,
+                                   size_t workspace_bytes, int32_t* status, poss_stream stream);
+
+/* Cuts sequences down to their budgets: of the first seq_len[b] slots (int32[batch]) of sequence b, keep[b] (int32[batch]) stay, in
+ * every layer and KV head its own: the first `first`, the last `recent`, and of those between the ones of greatest mass, ties to the
+ * lower slot (-0 equals 0, NaN is below all).  They move to slots 0 .. keep[b] - 1 in their order, keys and values, and their masses to
+ * out_mass (same shape; may be mass).  A sequence with seq_len[b] <= keep[b] keeps its slots (its masses are copied).  out_len int32
+ * [batch] = slots that stay.  Slots and out_mass entries behind them are left as they were; poss_pages_remap gives surplus pages back.
+ * Keys stay rotated as they are: positions of later rows go on.  The slots must lie in pages that no other sequence holds and that a
+ * table names once.  A sequence with seq_len out of range, keep[b] < 0 or, where slots have to go, keep[b] < first + recent, or without
+ * a page that it needs, keeps its slots and gets out_len = seq_len (status; its out_mass entries are left as they were).
+ * out_mass equals mass or does not overlap it; out_len overlaps no input.  Errors: INVALID, SHAPE, CAPACITY, WORKSPACE. */
+POSS_API size_t poss_pages_evict_workspace_bytes(const poss_page_pool* pool, int batch, int max_pages);
+POSS_API int poss_pages_evict(const poss_page_pool* pool, void* kv_pages, const int32_t* tables, int max_pages, int batch,
+                     const float* mass, float* out_mass, int64_t mass_slots, const int32_t* seq_len, const int32_t* keep, int first,
+                     int recent, int32_t* out_len, void* workspace, size_t workspace_bytes, int32_t* status, poss_stream stream);
+
+/* poss_pages_compact whose accepted slots take their masses with them: mass[..][prefix_len[b] + k] = mass[..][prefix_len[b] +
+ * path[b][k]] for k = 1 .. n_accepted[b], in every layer and KV head.  (What lies behind is set by the attention that follows.) */
+POSS_API int poss_pages_compact_mass(const poss_page_pool* pool, void* kv_pages, float* mass, int64_t mass_slots,
+                            const int32_t* tables, int max_pages, int batch, const int32_t* prefix_len, const int32_t* path,
+                            const int32_t* n_accepted, int32_t* out_len, int32_t* status, poss_stream stream);
 
 /* Commit of a round for a batch (the paged form of poss_kv_compact): in every layer sequence b's slot prefix_len[b] +
  * path[b][k] moves to prefix_len[b] + k for k = 1 .. n_accepted[b]; out_len[b] (int32[batch]) = prefix_len[b] +
@@ -142,6 +222,22 @@ POSS_API size_t poss_beam_select_workspace_bytes(int batch, int beams, int vocab
 POSS_API int poss_beam_select(const void* logits, int dtype, int batch, int beams, int vocab, const float* scores,
                      const int32_t* finished, int eos, int32_t* out_tokens, int32_t* out_parents, float* out_scores,
                      int32_t* out_finished, void* workspace, size_t workspace_bytes, poss_stream stream);
+
+/* Log-probabilities of given tokens, and of each row its entropy and best tokens: what a server answers beside tokens, or scores a
+ * prompt with.  p = softmax(logits[r] / temperature), temperature > 0; a logit that is not finite bans its token (p = 0).
+ * logits [rows][vocab] of type dtype (POSS_FP32 | POSS_BF16), rows ld >= vocab elements apart, any alignment of their type.
+ *   out_logp float[n_tokens]: of token tokens[i] (int32) in row token_rows[i] (int32; NULL: row i, n_tokens <= rows).  In a draft tree
+ *     tokens are the nodes' and token_rows their parents: the target's log-probability of every node.  A token or row below 0 is
+ *     none (a tree's root): 0; one that is banned, >= vocab or >= rows: -inf.  n_tokens may be 0.
+ *   out_lse float[rows] (may be NULL): log of the sum of e^(logit / temperature), -inf where all are banned.
+ *   out_entropy float[rows] (may be NULL): - sum p ln p, 0 where all are banned.
+ *   out_top_tokens int32, out_top_logp float [rows][topk], topk 0 .. POSS_MAX_TOPK: the greatest logits, ties to the lower token, with
+ *     their log-probabilities; behind the last token that is not banned -1 and -inf.
+ * Logits of any finite size are safe.  Log-probabilities are never above 0.  Sums are fp32, joined in 64 bits.  The outputs overlap
+ * neither the inputs nor each other.  No scratch.  Errors: INVALID, CAPACITY. */
+POSS_API int poss_token_logprobs(const void* logits, int64_t ld, int dtype, int rows, int vocab, float temperature,
+                        const int32_t* tokens, const int32_t* token_rows, int n_tokens, float* out_logp, float* out_lse,
+                        float* out_entropy, int topk, int32_t* out_top_tokens, float* out_top_logp, poss_stream stream);
 
 #ifdef __cplusplus
 }

@@ -16,6 +16,7 @@ LIB_PATH = os.path.join(HERE, "libposs.so")
 
 POSS_FP32, POSS_BF16 = 0, 1
 POSS_MAX_ROWS, POSS_MAX_TOPK, POSS_MAX_DEPTH = 128, 16, 16
+POSS_MAX_ROTARY_DIM = 512
 PROF_KINDS = ("fc", "qkv", "attention", "o", "gate_up", "down", "lm_head")
 POSS_OPT_ATTENTION_TCGEN05, POSS_OPT_SWIGLU_IN_KERNEL = 0, 1
 KERNEL_NAMES = {0: "other", 1: "gather_x", 2: "embed_rows", 3: "rmsnorm", 4: "reduce_norm", 5: "rope_append",
@@ -24,7 +25,8 @@ KERNEL_NAMES = {0: "other", 1: "gather_x", 2: "embed_rows", 3: "rmsnorm", 4: "re
                 16: "topk_partial", 17: "topk_merge", 18: "topk_merge_expand", 19: "argmax_partial", 20: "rerank",
                 21: "accept_walk", 22: "sample_walk", 23: "kv_compact", 24: "chain_mask", 25: "tile_contrib",
                 26: "paged_attn", 27: "paged_attn_combine", 28: "pages_append", 29: "pages_compact",
-                30: "pages_remap", 31: "pages_copy", 39: "beam_lists", 40: "beam_merge",
+                30: "pages_remap", 31: "pages_copy", 39: "beam_lists", 40: "beam_merge", 41: "rotary", 42: "append_rotary", 43: "slot_mass",
+                44: "evict_choose", 45: "evict_move", 46: "token_logprobs",
                 32: "gemm_fc", 33: "gemm_qkv", 34: "gemm_o", 35: "gemm_gate_up", 36: "gemm_down", 37: "gemm_lm_head",
                 38: "gemm_other"}
 STATUS = {0: "POSS_OK", 1: "POSS_E_INVALID", 2: "POSS_E_SHAPE", 3: "POSS_E_CAPACITY", 4: "POSS_E_WORKSPACE",
@@ -118,6 +120,24 @@ EXPORTS = {
     "poss_beam_select_workspace_bytes": (C.c_size_t, [C.c_int] * 3),
     "poss_beam_select": (C.c_int, [C.c_void_p] + [C.c_int] * 4 + [C.c_void_p, C.c_void_p, C.c_int] + [C.c_void_p] * 5 +
                          [C.c_size_t, C.c_void_p]),
+    "poss_rotary_frequencies": (C.c_int, [C.c_void_p, C.c_int, C.c_double, C.c_int] + [C.c_double] * 4),
+    "poss_rotary": (C.c_int, [C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int, C.c_int64, C.c_int, C.c_int, C.c_void_p,
+                              C.c_void_p, C.c_int, C.c_int, C.c_float, C.c_void_p]),
+    "poss_pages_append_rotary": (C.c_int, [C.POINTER(poss_page_pool), C.c_int, C.c_void_p, C.c_void_p] + [C.c_int] * 3 +
+                                 [C.c_void_p, C.c_void_p, C.c_int64, C.c_int, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64] +
+                                 [C.c_void_p] * 4 + [C.c_int, C.c_int, C.c_float, C.c_void_p, C.c_void_p]),
+    "poss_paged_attention_mass_workspace_bytes": (C.c_size_t, [C.POINTER(poss_page_pool)] + [C.c_int] * 4),
+    "poss_paged_tree_attention_mass": (C.c_int, [C.POINTER(poss_page_pool), C.c_int, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p] +
+                                       [C.c_int] * 4 + [C.c_void_p, C.c_int64] + [C.c_void_p] * 4 +
+                                       [C.c_float, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]),
+    "poss_pages_evict_workspace_bytes": (C.c_size_t, [C.POINTER(poss_page_pool), C.c_int, C.c_int]),
+    "poss_pages_evict": (C.c_int, [C.POINTER(poss_page_pool), C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_void_p,
+                                   C.c_int64, C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_size_t,
+                                   C.c_void_p, C.c_void_p]),
+    "poss_pages_compact_mass": (C.c_int, [C.POINTER(poss_page_pool), C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int, C.c_int] +
+                                [C.c_void_p] * 6),
+    "poss_token_logprobs": (C.c_int, [C.c_void_p, C.c_int64, C.c_int, C.c_int, C.c_int, C.c_float, C.c_void_p, C.c_void_p, C.c_int,
+                                      C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p]),
     "poss_debug_paged_lose_load": (C.c_int, [C.c_int]),
     "poss_debug_page_of_slot": (C.c_int, [C.POINTER(C.c_int32), C.c_int, C.c_int, C.c_int, C.c_int64,
                                           C.POINTER(C.c_int), C.POINTER(C.c_int)]),

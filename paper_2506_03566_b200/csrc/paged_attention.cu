@@ -217,6 +217,7 @@ __global__ void __launch_bounds__(128) k_paged_attn(SimtArgs s, const T* pool) {
 #pragma unroll
       for (int v = 0; v < NV; ++v)
         store4<T>(dst + tx * 4 + 32 * v, make_float4(o[i][v].x * inv, o[i][v].y * inv, o[i][v].z * inv, o[i][v].w * inv));
+      if (a.ml && tx == 0) a.ml[((size_t)b * a.rows + r) * a.Hq + kvh * a.G + qi - r * a.G] = paged_ml(m[i], l[i]);
     } else {
       float* dst = s.part + ((((size_t)b * gridDim.y + blockIdx.y) * s.ns + split) * QB + 2 * ty + i) * (D + 2);
       if (tx == 0) { dst[0] = m[i]; dst[1] = l[i]; }
@@ -291,6 +292,7 @@ __global__ void __launch_bounds__(128) k_paged_attn_merge(SimtArgs s) {
   T* dst = reinterpret_cast<T*>(a.out) + (((size_t)b * a.rows + r) * a.Hq + kvh * a.G + qi - r * a.G) * D;
 #pragma unroll
   for (int e = 0; e < D / 32; ++e) dst[lane + 32 * e] = from_f<T>(o[e] * inv);
+  if (a.ml && lane == 0) a.ml[((size_t)b * a.rows + r) * a.Hq + kvh * a.G + qi - r * a.G] = paged_ml(mx, l);
 }
 
 // Parts per (sequence, KV head, query tile): enough blocks for four per SM of a 148-SM device, at least one 32-key tile
@@ -312,6 +314,67 @@ void launch_simt(Launcher& L, const SimtArgs& s, const void* pool) {
              reinterpret_cast<const T*>(pool));
   if (s.ns > 1)
     launch_pdl(L, k_paged_attn_merge<T, D>, dim3(QB / 4, a.g.Hkv * s.q_tiles, a.batch), dim3(128), 0, s);
+}
+
+struct MassTarget {
+  float* mass;              // [layers][batch][kv heads][slots]
+  int64_t slots;
+  const float* weights;     // NULL, or [batch][rows]
+};
+size_t ml_bytes(int batch, int rows, int Hq) { return ((size_t)batch * rows * Hq * sizeof(float2) + 255) / 256 * 256; }
+
+// both entries; mass NULL: the attention alone
+int attend(const poss_page_pool* pool, int layer, const void* kv_pages, const int32_t* tables, int max_pages, int batch, int rows,
+           int n_q_heads, const void* q, int64_t ld_q, const int32_t* prefix_len, const int32_t* n_rows, const uint64_t* anc_mask,
+           float scale, void* out, void* workspace, size_t workspace_bytes, int32_t* status, poss_stream stream, const MassTarget* mass) {
+  int rc = page_pool_check(pool);
+  if (rc != POSS_OK) return rc;
+  if (batch < 0 || rows < 0 || n_q_heads < 1 || layer < 0 || layer >= pool->n_layers) return POSS_E_INVALID;
+  if (n_q_heads % pool->n_kv_heads) return POSS_E_SHAPE;
+  if (!isfinite(scale)) return POSS_E_INVALID;
+  if (batch == 0 || rows == 0) return POSS_OK;
+  rc = page_table_check(pool, max_pages, batch);
+  if (rc != POSS_OK) return rc;
+  if (rows > POSS_MAX_ROWS) return POSS_E_CAPACITY;
+  // a launch's grid: query tiles of 32 rows times KV heads
+  if (pool->n_kv_heads * (((long long)rows * (n_q_heads / pool->n_kv_heads) + 31) / 32) > 65535) return POSS_E_CAPACITY;
+  if (!kv_pages || !tables || !q || !prefix_len || !anc_mask || !out) return POSS_E_INVALID;
+  const int es = pool->dtype == POSS_BF16 ? 2 : 4;
+  if (ld_q < (int64_t)n_q_heads * pool->head_dim || (ld_q * es) % 16) return POSS_E_INVALID;
+  if (!aligned16(kv_pages) || !aligned16(q) || !aligned16(out)) return POSS_E_INVALID;
+  const size_t ws_bytes = poss_paged_attention_workspace_bytes(pool, batch, rows, n_q_heads, max_pages);
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) ||
+      workspace_bytes < ws_bytes + (mass ? ml_bytes(batch, rows, n_q_heads) : 0))
+    return POSS_E_WORKSPACE;
+  // one block's queries may be read while another's rows are written
+  const size_t row = (size_t)n_q_heads * pool->head_dim * es, n = (size_t)batch * rows;
+  if (overlap(out, n * row, q, (n - 1) * ld_q * es + row)) return POSS_E_INVALID;
+  if (mass) {
+    if (!mass->mass || mass->slots < (int64_t)max_pages * pool->page_slots) return POSS_E_INVALID;
+    const size_t bytes = (size_t)pool->n_layers * batch * pool->n_kv_heads * mass->slots * 4;
+    if (overlap(mass->mass, bytes, q, ((n - 1) * ld_q) * es + row) || overlap(mass->mass, bytes, out, n * row) ||
+        overlap(mass->mass, bytes, mass->weights, n * 4))
+      return POSS_E_INVALID;
+  }
+  int64_t launches = 0;
+  Launcher L{reinterpret_cast<cudaStream_t>(stream), &launches, POSS_OK};
+  PagedAttnArgs a;
+  a.g = page_geo(pool, tables, max_pages);
+  a.layer = layer; a.batch = batch; a.rows = rows; a.Hq = n_q_heads; a.G = n_q_heads / pool->n_kv_heads;
+  a.q = q; a.ld_q = ld_q; a.prefix_len = prefix_len; a.n_rows = n_rows; a.mask = anc_mask;
+  a.mask_words = (rows + 63) / 64; a.scale = scale; a.out = out; a.ws = workspace; a.status = status;
+  a.ml = mass ? reinterpret_cast<float2*>(reinterpret_cast<char*>(workspace) + ws_bytes) : nullptr;
+  if (paged_attn_tc_supported(*pool, a.G, scale)) launch_paged_attn_tc(L, a, kv_pages, *pool);
+  else launch_paged_attn_simt(L, a, kv_pages, pool->dtype);
+  if (!mass || L.err != POSS_OK) return L.err;
+  PagedMassArgs m;
+  m.a = a;
+  m.mass = mass->mass + (size_t)layer * batch * pool->n_kv_heads * mass->slots;
+  m.mass_slots = mass->slots;
+  m.weights = mass->weights;
+  m.scale_log2 = scale * 1.4426950408889634f;
+  launch_paged_mass_simt(L, m, kv_pages, pool->dtype);
+  return L.err;
 }
 
 }  // namespace
@@ -355,37 +418,23 @@ int poss_paged_tree_attention(const poss_page_pool* pool, int layer, const void*
                               const int32_t* prefix_len, const int32_t* n_rows, const uint64_t* anc_mask, float scale,
                               void* out, void* workspace, size_t workspace_bytes, int32_t* status,
                               poss_stream stream) {
-  int rc = page_pool_check(pool);
-  if (rc != POSS_OK) return rc;
-  if (batch < 0 || rows < 0 || n_q_heads < 1 || layer < 0 || layer >= pool->n_layers) return POSS_E_INVALID;
-  if (n_q_heads % pool->n_kv_heads) return POSS_E_SHAPE;
-  if (!isfinite(scale)) return POSS_E_INVALID;
-  if (batch == 0 || rows == 0) return POSS_OK;
-  rc = page_table_check(pool, max_pages, batch);
-  if (rc != POSS_OK) return rc;
-  if (rows > POSS_MAX_ROWS) return POSS_E_CAPACITY;
-  // a launch's grid: query tiles of 32 rows times KV heads
-  if (pool->n_kv_heads * (((long long)rows * (n_q_heads / pool->n_kv_heads) + 31) / 32) > 65535) return POSS_E_CAPACITY;
-  if (!kv_pages || !tables || !q || !prefix_len || !anc_mask || !out) return POSS_E_INVALID;
-  const int es = pool->dtype == POSS_BF16 ? 2 : 4;
-  if (ld_q < (int64_t)n_q_heads * pool->head_dim || (ld_q * es) % 16) return POSS_E_INVALID;
-  if (!aligned16(kv_pages) || !aligned16(q) || !aligned16(out)) return POSS_E_INVALID;
-  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) ||
-      workspace_bytes < poss_paged_attention_workspace_bytes(pool, batch, rows, n_q_heads, max_pages))
-    return POSS_E_WORKSPACE;
-  // one block's queries may be read while another's rows are written
-  const size_t row = (size_t)n_q_heads * pool->head_dim * es, n = (size_t)batch * rows;
-  if (overlap(out, n * row, q, (n - 1) * ld_q * es + row)) return POSS_E_INVALID;
-  int64_t launches = 0;
-  Launcher L{reinterpret_cast<cudaStream_t>(stream), &launches, POSS_OK};
-  PagedAttnArgs a;
-  a.g = page_geo(pool, tables, max_pages);
-  a.layer = layer; a.batch = batch; a.rows = rows; a.Hq = n_q_heads; a.G = n_q_heads / pool->n_kv_heads;
-  a.q = q; a.ld_q = ld_q; a.prefix_len = prefix_len; a.n_rows = n_rows; a.mask = anc_mask;
-  a.mask_words = (rows + 63) / 64; a.scale = scale; a.out = out; a.ws = workspace; a.status = status;
-  if (paged_attn_tc_supported(*pool, a.G, scale)) launch_paged_attn_tc(L, a, kv_pages, *pool);
-  else launch_paged_attn_simt(L, a, kv_pages, pool->dtype);
-  return L.err;
+  return attend(pool, layer, kv_pages, tables, max_pages, batch, rows, n_q_heads, q, ld_q, prefix_len, n_rows, anc_mask, scale, out,
+                workspace, workspace_bytes, status, stream, nullptr);
+}
+
+size_t poss_paged_attention_mass_workspace_bytes(const poss_page_pool* pool, int batch, int rows, int n_q_heads, int max_pages) {
+  const size_t n = poss_paged_attention_workspace_bytes(pool, batch, rows, n_q_heads, max_pages);
+  return n ? n + ml_bytes(batch, rows, n_q_heads) : 0;
+}
+
+int poss_paged_tree_attention_mass(const poss_page_pool* pool, int layer, const void* kv_pages, float* mass, int64_t mass_slots,
+                                   const int32_t* tables, int max_pages, int batch, int rows, int n_q_heads, const void* q,
+                                   int64_t ld_q, const int32_t* prefix_len, const int32_t* n_rows, const uint64_t* anc_mask,
+                                   const float* row_weights, float scale, void* out, void* workspace, size_t workspace_bytes,
+                                   int32_t* status, poss_stream stream) {
+  const MassTarget m = {mass, mass_slots, row_weights};
+  return attend(pool, layer, kv_pages, tables, max_pages, batch, rows, n_q_heads, q, ld_q, prefix_len, n_rows, anc_mask, scale, out,
+                workspace, workspace_bytes, status, stream, &m);
 }
 
 }  // extern "C"

@@ -14,7 +14,12 @@ struct PagedAttnArgs {
   void* out;
   void* ws;
   int32_t* status;
+  float2* ml;                          // NULL, or [batch][rows][Hq]: what a query row leaves for the slots' weights
 };
+// A query row's reference maximum (scores times scale times log2 e) and the inverse of its sum; a row that sees nothing weighs nothing.
+__device__ __forceinline__ float2 paged_ml(float m, float l) {
+  return l == 0.f ? make_float2(INFINITY, 0.f) : make_float2(m == -INFINITY ? 0.f : m, 1.f / l);
+}
 
 // SIMT kernel: every type, head dimension and page size
 size_t paged_attn_simt_workspace(int batch, int rows, int Hq, int Hkv, int d);
@@ -25,6 +30,16 @@ void launch_paged_attn_simt(Launcher& L, const PagedAttnArgs& a, const void* poo
 bool paged_attn_tc_supported(const poss_page_pool& p, int G, float scale);
 size_t paged_attn_tc_workspace(const poss_page_pool& p, int batch, int rows, int Hq, int max_pages);
 void launch_paged_attn_tc(Launcher& L, const PagedAttnArgs& a, const void* pool, const poss_page_pool& p);
+
+// The weight that every slot draws, from the queries and the rows' maxima and sums (a.ml)
+struct PagedMassArgs {
+  PagedAttnArgs a;
+  float* mass;                         // the layer's: [batch][Hkv][mass_slots]
+  long long mass_slots;
+  const float* weights;                // NULL, or [batch][rows]
+  float scale_log2;
+};
+void launch_paged_mass_simt(Launcher& L, const PagedMassArgs& s, const void* pool, int dtype);
 
 // visibility of 32 consecutive slots from `key0` on: every slot below `prefix`, slot prefix + t iff bit t of
 // (lo, hi) is set.  The mask has already been cut to the rows that exist, so slots behind them come out unseen.

@@ -674,6 +674,8 @@ __global__ void __launch_bounds__(N_THREADS, 1) k_paged_attn_tc(const __grid_con
           part = partial_of(k, HD, blockIdx.x, g.tile0 > 0 || u_first == walk.u - g.n ? 0 : 1);
           if (valid && (halves || wg == 0))
             __stcg(reinterpret_cast<float2*>(part + (size_t)k.row_cap * HD) + rr, make_float2(m, l));
+        } else if (a.ml && valid && (halves || wg == 0)) {
+          a.ml[((size_t)g.b * a.rows + r) * a.Hq + g.head * a.G + head] = paged_ml(m, l);
         }
         bf16* const out = reinterpret_cast<bf16*>(a.out) +
                           (((size_t)g.b * a.rows + r) * a.Hq + g.head * a.G + head) * HD;
@@ -1003,6 +1005,7 @@ __global__ void __launch_bounds__(256) k_paged_attn_tc_merge(const TcArgs k, int
   for (int v = 0; v < NV; ++v)
     *reinterpret_cast<uint2*>(out + 4 * v) =
         make_uint2(pack_bf16(o[v].x * inv, o[v].y * inv), pack_bf16(o[v].z * inv, o[v].w * inv));
+  if (a.ml && slice == 0) a.ml[((size_t)b * a.rows + r) * a.Hq + head * a.G + qh] = paged_ml(m, l);
 }
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,

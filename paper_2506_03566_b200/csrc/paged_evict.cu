@@ -1,0 +1,254 @@
+// Eviction from paged caches by accumulated attention weight.
+//
+// Of a sequence's n slots keep[b] stay, for every layer and KV head its own: the first `first`, the last `recent`, and of those between
+// the ones with the greatest weight, ties to the lower slot.  They move to slots 0 .. keep - 1 in their order, weights with them.
+//
+//   choose  a block per (sequence, layer, KV head).  Weights become whole numbers that order alike; three rounds over 11, 11 and 10 of
+//           their bits count how many share each value of those bits and narrow the last one that stays down to its value T and to how
+//           many slots equal to T stay (the lowest ones).  A walk over the slots in order then numbers those that stay.
+//   move    a block per (sequence, layer, KV head, keys / values) brings the rows forward, some dozen at a time.  A row's new place is
+//           never behind its old one and rows go in order, so a step may write as soon as all of its own rows are in registers: what
+//           it overwrites is gone or has been read.
+// What bounds it: memory in the move; in the choice the rounds' trips over the weights (from L2) and the counts in shared memory.
+#include "paged.cuh"
+
+POSS_TRACE_REGISTER()
+
+namespace {
+
+constexpr int CHOOSE_THREADS = 512, MOVE_THREADS = 256;
+constexpr int BINS = 2048;
+
+struct EvictArgs {
+  PageGeo g;
+  int batch, first, recent;
+  const float* mass;
+  float* out_mass;
+  long long mass_slots;                      // weights per (layer, sequence, head)
+  const int32_t *seq_len, *keep;
+  int32_t *out_len, *status;
+  int32_t* src;                              // [layers][batch][heads][slots]: the slot that moves to each place
+  int32_t* hole;                             // [layers][batch][heads]: the first place that changes; out_len where none does
+};
+
+// a weight as a number that orders alike; -0 is 0, NaN below all
+__device__ __forceinline__ uint32_t order_of(float x) {
+  const uint32_t b = __float_as_uint(x + 0.f);
+  return x != x ? 0u : b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+// exclusive prefix sum over the block; *total = the sum.  sums: one int per warp
+template <int THREADS> __device__ __forceinline__ int scan(int v, int* sums, int* total) {
+  constexpr int WARPS = THREADS / 32;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int x = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, x, o);
+    if (lane >= o) x += y;
+  }
+  __syncthreads();                                        // the sums of an earlier scan have been read
+  if (lane == 31) sums[warp] = x;
+  __syncthreads();
+  int w = lane < WARPS ? sums[lane] : 0;
+#pragma unroll
+  for (int o = 1; o < WARPS; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, w, o);
+    if (lane >= o) w += y;
+  }
+  *total = __shfl_sync(0xffffffffu, w, WARPS - 1);
+  const int up = __shfl_sync(0xffffffffu, w, warp ? warp - 1 : 0);
+  return x - v + (warp ? up : 0);
+}
+
+__global__ void __launch_bounds__(CHOOSE_THREADS) k_evict_choose(EvictArgs a) {
+  __shared__ int s_bins[BINS], s_sums[CHOOSE_THREADS / 32], s_bin, s_left;
+  pdl_enter(POSS_K_EVICT_CHOOSE);
+  const int t = threadIdx.x;
+  const int head = blockIdx.x % a.g.Hkv, lb = blockIdx.x / a.g.Hkv, b = lb % a.batch;
+  const int n = a.seq_len[b], keep = a.keep[b];
+  const long long slots = (long long)a.g.max_pages * a.g.page;
+  bool ok = n >= 0 && n <= slots && keep >= 0 && (n <= keep || (long long)a.first + a.recent <= keep);
+  const int32_t* table = a.g.tables + (size_t)b * a.g.max_pages;
+  if (ok && n > keep)
+    for (int i = t; i < (n + a.g.page - 1) / a.g.page; i += CHOOSE_THREADS) ok &= page_at(table, a.g.max_pages, a.g.n_pages, i) >= 0;
+  ok = __syncthreads_and(ok);
+  const int stays = !ok || n <= keep ? n : keep;
+  if (blockIdx.x == (unsigned)(b * a.g.Hkv) && t == 0) {  // (the first layer's first head)
+    a.out_len[b] = stays;
+    if (!ok) raise_status(a.status, POSS_E_INVALID);
+  }
+  const size_t row = (size_t)lb * a.g.Hkv + head;
+  const float* x = a.mass + row * a.mass_slots;
+  float* out = a.out_mass + row * a.mass_slots;
+  if (t == 0) a.hole[row] = stays;
+  if (!ok || n <= keep) {
+    if (ok && out != x)
+      for (int i = t; i < n; i += CHOOSE_THREADS) out[i] = x[i];
+    return;
+  }
+  // ---- the last weight that stays, of slots [lo, hi)
+  const int lo = a.first, hi = n - a.recent;
+  int left = keep - a.first - a.recent;                   // how many of them stay
+  uint32_t fixed = 0, mask = 0;                           // the bits of it that are known
+  int equal = 0;                                          // slots that equal it and stay
+  if (left > 0) {
+#pragma unroll 1
+    for (int round = 0; round < 3; ++round) {
+      const int shift = round == 0 ? 21 : round == 1 ? 10 : 0, bins = round == 2 ? 1024 : 2048;
+      for (int i = t; i < bins; i += CHOOSE_THREADS) s_bins[i] = 0;
+      __syncthreads();
+      for (int i = lo + t; i < hi; i += CHOOSE_THREADS) {
+        const uint32_t u = order_of(x[i]);
+        if ((u & mask) == fixed) atomicAdd(&s_bins[(u >> shift) & (bins - 1)], 1);
+      }
+      __syncthreads();
+      // from the greatest value down: the bin that the left-th falls into
+      const int per = bins / CHOOSE_THREADS;              // 4 or 2 bins per thread, greatest first
+      int mine = 0;
+      for (int i = 0; i < per; ++i) mine += s_bins[bins - 1 - (t * per + i)];
+      int total, before = scan<CHOOSE_THREADS>(mine, s_sums, &total);
+      if (before < left && left <= before + mine) {
+        for (int i = 0; i < per; ++i) {
+          const int bin = bins - 1 - (t * per + i), c = s_bins[bin];
+          if (left <= before + c) { s_bin = bin; s_left = left - before; break; }
+          before += c;
+        }
+      }
+      __syncthreads();
+      fixed |= (uint32_t)s_bin << shift;
+      mask |= (uint32_t)(bins - 1) << shift;
+      left = s_left;
+      __syncthreads();
+    }
+    equal = left;
+  } else {
+    fixed = 0xffffffffu;                                  // (above every weight)
+  }
+  // ---- the slots that stay, in order.  (In place a weight's new place is never behind its old one, and a step's weights are in
+  // registers before the step's barrier.)
+  int32_t* src = a.src + row * slots;
+  int at = 0, ties = 0, hole = 0x7fffffff;
+#pragma unroll 1
+  for (int i0 = 0; i0 < n; i0 += CHOOSE_THREADS) {
+    const int i = i0 + t;
+    const float w = i < n ? x[i] : 0.f;
+    const bool inner = i >= lo && i < hi;
+    const uint32_t u = order_of(w);
+    const bool tie = inner && u == fixed;
+    int total;
+    // both numberings in one scan: ties in the upper half
+    const bool sure = i < n && (!inner || u > fixed);
+    const int both = scan<CHOOSE_THREADS>((tie ? 0x10000 : 0) + (sure ? 1 : 0), s_sums, &total);
+    const int tie_no = ties + (both >> 16);               // ties before this slot
+    const bool on = sure || (tie && tie_no < equal);
+    const int place = at + (both & 0xffff) + min(both >> 16, max(equal - ties, 0));
+    if (on) {
+      src[place] = i;
+      out[place] = w;
+      if (place != i) hole = min(hole, place);
+    }
+    at += (total & 0xffff) + min(total >> 16, max(equal - ties, 0));
+    ties += total >> 16;
+  }
+  hole = __reduce_min_sync(0xffffffffu, hole);
+  __syncthreads();
+  if ((t & 31) == 0) s_sums[t >> 5] = hole;
+  __syncthreads();
+  if (t == 0) {
+    for (int w = 1; w < CHOOSE_THREADS / 32; ++w) hole = min(hole, s_sums[w]);
+    a.hole[row] = min(hole, keep);
+  }
+}
+
+// Block: (sequence, layer, head), keys / values.  A step: ROWS_PER_STEP pieces of 16 bytes per thread.
+template <int ES>
+__global__ void __launch_bounds__(MOVE_THREADS) k_evict_move(EvictArgs a, char* pool) {
+  constexpr int PER = 4;
+  __shared__ long long s_src[2][MOVE_THREADS], s_dst[2][MOVE_THREADS];   // (at least 4 pieces per row: up to 256 rows a step)
+  pdl_enter(POSS_K_EVICT_MOVE);
+  const int t = threadIdx.x, kv = blockIdx.x & 1;
+  const int row = blockIdx.x >> 1, head = row % a.g.Hkv, lb = row / a.g.Hkv, b = lb % a.batch, layer = lb / a.batch;
+  const int keep = a.out_len[b], hole = a.hole[row];
+  if (hole >= keep) return;
+  const long long slots = (long long)a.g.max_pages * a.g.page;
+  const int32_t* src = a.src + (size_t)row * slots;
+  const int32_t* table = a.g.tables + (size_t)b * a.g.max_pages;
+  const int per_row = a.g.d * ES / 16, rows = MOVE_THREADS * PER / per_row;
+  auto where = [&](int slot) {
+    const int place = slot / a.g.page;                    // (every page of the sequence was seen to be there)
+    const int p = page_at(table, a.g.max_pages, a.g.n_pages, place);
+    return (long long)(page_offset(a.g, layer, p < 0 ? 0 : p, kv, head) + (size_t)(slot - place * a.g.page) * a.g.d) * ES;
+  };
+  int buf = 0;
+#pragma unroll 1
+  for (int r0 = hole; r0 < keep; r0 += rows, buf ^= 1) {
+    const int n = min(rows, keep - r0);
+    for (int r = t; r < n; r += MOVE_THREADS) {
+      s_src[buf][r] = where(src[r0 + r]);
+      s_dst[buf][r] = where(r0 + r);
+    }
+    __syncthreads();
+    uint4 x[PER];
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      const int i = t + j * MOVE_THREADS, r = i / per_row;
+      if (r < n) x[j] = *reinterpret_cast<const uint4*>(pool + s_src[buf][r] + (i - r * per_row) * 16);
+    }
+    __syncthreads();                                      // the step's rows are in registers
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      const int i = t + j * MOVE_THREADS, r = i / per_row;
+      if (r < n) *reinterpret_cast<uint4*>(pool + s_dst[buf][r] + (i - r * per_row) * 16) = x[j];
+    }
+  }
+}
+
+size_t round256(size_t n) { return (n + 255) / 256 * 256; }
+
+}  // namespace
+
+extern "C" {
+
+size_t poss_pages_evict_workspace_bytes(const poss_page_pool* pool, int batch, int max_pages) {
+  if (page_pool_check(pool) != POSS_OK || page_table_check(pool, max_pages, batch) != POSS_OK) return 0;
+  const size_t rows = (size_t)pool->n_layers * batch * pool->n_kv_heads;
+  if (rows >= (1ull << 30)) return 0;
+  return round256(rows * 4) + round256(rows * (size_t)max_pages * pool->page_slots * 4);
+}
+
+int poss_pages_evict(const poss_page_pool* pool, void* kv_pages, const int32_t* tables, int max_pages, int batch, const float* mass,
+                     float* out_mass, int64_t mass_slots, const int32_t* seq_len, const int32_t* keep, int first, int recent,
+                     int32_t* out_len, void* workspace, size_t workspace_bytes, int32_t* status, poss_stream stream) {
+  int rc = page_pool_check(pool);
+  if (rc != POSS_OK) return rc;
+  if (batch < 0 || first < 0 || recent < 0) return POSS_E_INVALID;
+  if (batch == 0) return POSS_OK;
+  rc = page_table_check(pool, max_pages, batch);
+  if (rc != POSS_OK) return rc;
+  const size_t need = poss_pages_evict_workspace_bytes(pool, batch, max_pages);
+  if (!need) return POSS_E_CAPACITY;
+  if (!kv_pages || !tables || !mass || !out_mass || !seq_len || !keep || !out_len || !aligned16(kv_pages)) return POSS_E_INVALID;
+  if (mass_slots < (int64_t)max_pages * pool->page_slots) return POSS_E_INVALID;
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < need) return POSS_E_WORKSPACE;
+  const size_t rows = (size_t)pool->n_layers * batch * pool->n_kv_heads;
+  if (out_mass != mass && overlap(out_mass, rows * mass_slots * 4, mass, rows * mass_slots * 4)) return POSS_E_INVALID;
+  const size_t nb = (size_t)batch * 4;
+  if (overlap(out_len, nb, seq_len, nb) || overlap(out_len, nb, keep, nb) || overlap(out_len, nb, tables, nb * max_pages))
+    return POSS_E_INVALID;
+  int64_t launches = 0;
+  Launcher L{reinterpret_cast<cudaStream_t>(stream), &launches, POSS_OK};
+  EvictArgs a;
+  a.g = page_geo(pool, tables, max_pages);
+  a.batch = batch; a.first = first; a.recent = recent;
+  a.mass = mass; a.out_mass = out_mass; a.mass_slots = mass_slots;
+  a.seq_len = seq_len; a.keep = keep; a.out_len = out_len; a.status = status;
+  a.hole = reinterpret_cast<int32_t*>(workspace);
+  a.src = reinterpret_cast<int32_t*>(reinterpret_cast<char*>(workspace) + round256(rows * 4));
+  launch_pdl(L, k_evict_choose, dim3((unsigned)rows), dim3(CHOOSE_THREADS), 0, a);
+  if (L.err != POSS_OK) return L.err;
+  launch_pdl(L, pool->dtype == POSS_BF16 ? k_evict_move<2> : k_evict_move<4>, dim3((unsigned)(2 * rows)), dim3(MOVE_THREADS), 0, a,
+             reinterpret_cast<char*>(kv_pages));
+  return L.err;
+}
+
+}  // extern "C"

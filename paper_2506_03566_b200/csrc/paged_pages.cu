@@ -80,7 +80,8 @@ __global__ void __launch_bounds__(256) k_pages_append(PageGeo g, int layer, char
 template <int ES>
 __global__ void __launch_bounds__(256) k_pages_compact(PageGeo g, char* pool, const int32_t* prefix_len,
                                                        const int32_t* path, const int32_t* n_accepted,
-                                                       int32_t* out_len, int32_t* status) {
+                                                       int32_t* out_len, int32_t* status, float* mass,
+                                                       long long mass_slots) {
   __shared__ int s_src[POSS_MAX_DEPTH], s_dst[POSS_MAX_DEPTH];      // page * page_slots + slot inside it
   pdl_enter(POSS_K_PAGES_COMPACT);
   const int b = blockIdx.y, layer = blockIdx.x >> 1, kv = blockIdx.x & 1, t = threadIdx.x;
@@ -107,6 +108,15 @@ __global__ void __launch_bounds__(256) k_pages_compact(PageGeo g, char* pool, co
     if (!ok) raise_status(status, POSS_E_INVALID);
   }
   if (!ok || a == 0) return;
+  if (mass && kv == 0) {                                  // the slots' weights go with them: a lane per step, a warp per head
+    float* const m = mass + ((size_t)layer * gridDim.y + b) * g.Hkv * mass_slots + prefix;
+    for (int h = t >> 5; h < g.Hkv; h += 8) {
+      const int k = t & 31;
+      const float x = k < a ? m[h * mass_slots + pb[k + 1]] : 0.f;
+      __syncwarp();
+      if (k < a) m[h * mass_slots + k + 1] = x;
+    }
+  }
   const int per_row = g.d * ES / 16, per_head = a * per_row;
   const int heads = per_head < 1024 ? 1024 / per_head : 1;          // heads whose rows fit four pieces per thread
   for (int h0 = 0; h0 < g.Hkv; h0 += heads) {
@@ -433,6 +443,40 @@ int remap(const poss_page_pool* pool, void* kv_pages, const int32_t* tables, int
   return L.err;
 }
 
+// both entries; mass NULL: the pages alone
+int commit(const poss_page_pool* pool, void* kv_pages, const int32_t* tables, int max_pages, int batch,
+           float* mass, int64_t mass_slots, const int32_t* prefix_len, const int32_t* path, const int32_t* n_accepted,
+           int32_t* out_len, int32_t* status, poss_stream stream) {
+  int rc = page_pool_check(pool);
+  if (rc != POSS_OK) return rc;
+  if (batch == 0) return POSS_OK;
+  rc = page_table_check(pool, max_pages, batch);
+  if (rc != POSS_OK) return rc;
+  if (!kv_pages || !tables || !prefix_len || !path || !n_accepted || !out_len || !aligned16(kv_pages))
+    return POSS_E_INVALID;
+  // every block reads the lengths, one of each sequence writes the new one
+  const size_t n = (size_t)batch * 4;
+  if (overlap(out_len, n, prefix_len, n) || overlap(out_len, n, n_accepted, n) ||
+      overlap(out_len, n, path, n * (POSS_MAX_DEPTH + 1)) || overlap(out_len, n, tables, n * max_pages))
+    return POSS_E_INVALID;
+  if (mass) {
+    if (mass_slots < (int64_t)max_pages * pool->page_slots) return POSS_E_INVALID;
+    const size_t bytes = (size_t)pool->n_layers * batch * pool->n_kv_heads * mass_slots * 4;
+    if (overlap(mass, bytes, out_len, n)) return POSS_E_INVALID;
+  }
+  int64_t launches = 0;
+  Launcher L{reinterpret_cast<cudaStream_t>(stream), &launches, POSS_OK};
+  const PageGeo g = page_geo(pool, tables, max_pages);
+  const dim3 grid(pool->n_layers * 2, batch);
+  if (pool->dtype == POSS_BF16)
+    launch_pdl(L, k_pages_compact<2>, grid, dim3(256), 0, g, (char*)kv_pages, prefix_len, path, n_accepted, out_len,
+               status, mass, mass_slots);
+  else
+    launch_pdl(L, k_pages_compact<4>, grid, dim3(256), 0, g, (char*)kv_pages, prefix_len, path, n_accepted, out_len,
+               status, mass, mass_slots);
+  return L.err;
+}
+
 }  // namespace
 
 extern "C" {
@@ -469,29 +513,14 @@ int poss_pages_append(const poss_page_pool* pool, int layer, void* kv_pages, con
 int poss_pages_compact(const poss_page_pool* pool, void* kv_pages, const int32_t* tables, int max_pages, int batch,
                        const int32_t* prefix_len, const int32_t* path, const int32_t* n_accepted, int32_t* out_len,
                        int32_t* status, poss_stream stream) {
-  int rc = page_pool_check(pool);
-  if (rc != POSS_OK) return rc;
-  if (batch == 0) return POSS_OK;
-  rc = page_table_check(pool, max_pages, batch);
-  if (rc != POSS_OK) return rc;
-  if (!kv_pages || !tables || !prefix_len || !path || !n_accepted || !out_len || !aligned16(kv_pages))
-    return POSS_E_INVALID;
-  // every block reads the lengths, one of each sequence writes the new one
-  const size_t n = (size_t)batch * 4;
-  if (overlap(out_len, n, prefix_len, n) || overlap(out_len, n, n_accepted, n) ||
-      overlap(out_len, n, path, n * (POSS_MAX_DEPTH + 1)) || overlap(out_len, n, tables, n * max_pages))
-    return POSS_E_INVALID;
-  int64_t launches = 0;
-  Launcher L{reinterpret_cast<cudaStream_t>(stream), &launches, POSS_OK};
-  const PageGeo g = page_geo(pool, tables, max_pages);
-  const dim3 grid(pool->n_layers * 2, batch);
-  if (pool->dtype == POSS_BF16)
-    launch_pdl(L, k_pages_compact<2>, grid, dim3(256), 0, g, (char*)kv_pages, prefix_len, path, n_accepted, out_len,
-               status);
-  else
-    launch_pdl(L, k_pages_compact<4>, grid, dim3(256), 0, g, (char*)kv_pages, prefix_len, path, n_accepted, out_len,
-               status);
-  return L.err;
+  return commit(pool, kv_pages, tables, max_pages, batch, nullptr, 0, prefix_len, path, n_accepted, out_len, status, stream);
+}
+
+int poss_pages_compact_mass(const poss_page_pool* pool, void* kv_pages, float* mass, int64_t mass_slots, const int32_t* tables,
+                            int max_pages, int batch, const int32_t* prefix_len, const int32_t* path, const int32_t* n_accepted,
+                            int32_t* out_len, int32_t* status, poss_stream stream) {
+  if (!mass) return POSS_E_INVALID;
+  return commit(pool, kv_pages, tables, max_pages, batch, mass, mass_slots, prefix_len, path, n_accepted, out_len, status, stream);
 }
 
 size_t poss_pages_remap_workspace_bytes(const poss_page_pool* pool, int n_before, int n_after, int max_pages) {

@@ -1,0 +1,321 @@
+// Rotary positions: pairs of a head's elements turned by position times the pair's frequency, on rows that stay where they are
+// (poss_rotary) and on rows that go into pages (poss_pages_append_rotary, queries in the same launch).
+//
+//   (u, v) -> (u cos a - v sin a, v cos a + u sin a) * magnitude,  a = position * frequency of the pair
+//
+// The angle of a far position is where 32 bits would fail (at position 10^6 an fp32 product is off by 0.06 radians): position and
+// frequency are multiplied in 64 bits as turns, the whole turns are taken off (the fused multiply-add leaves the fraction exactly), and
+// only the fraction goes on in 32 bits.  What is left is the rounding of the frequency in turns, 2^-52 of the angle.
+//
+// One block per row: a thread per pair leaves cosine and sine in shared memory, then all threads stream the row's heads, two pieces
+// of 16 bytes at a time.  With halves as pairs these are the two partners, so a row may be turned in place.
+// What bounds it: memory for prompts; a chain of trips (lengths and position, table, data) for a token.
+#include "paged.cuh"
+#include <math.h>
+
+POSS_TRACE_REGISTER()
+
+namespace {
+
+constexpr int THREADS = 128;
+constexpr int MAX_HALF = POSS_MAX_ROTARY_DIM / 2;
+
+// What is turned, and how
+struct Turn {
+  const double* freq;        // radians per position, [half]
+  int half;                  // pairs
+  int interleaved;           // pairs are neighbours; else element i and half + i
+  float magnitude;
+};
+// heads of one row in global memory: source, target, head's stride in the target (bytes)
+struct Heads {
+  const char* src;
+  char* dst;
+  size_t dst_step;
+  int n;
+};
+
+__device__ __forceinline__ void angles(const Turn& turn, int position, float2* cs) {
+  for (int i = threadIdx.x; i < turn.half; i += THREADS) {
+    const double t = turn.freq[i] * 0.15915494309189533577;   // 1 / (2 pi)
+    const double p = (double)position;
+    const float fraction = (float)fma(p, t, -rint(p * t));
+    float s, c;
+    sincospif(2.f * fraction, &s, &c);
+    cs[i] = make_float2(c * turn.magnitude, s * turn.magnitude);
+  }
+}
+__device__ __forceinline__ float2 turned(float u, float v, float2 cs) {
+  return make_float2(u * cs.x - v * cs.y, v * cs.x + u * cs.y);
+}
+
+template <typename T> struct Piece;          // 16 bytes as fp32 values
+template <> struct Piece<float> {
+  static constexpr int N = 4;
+  static __device__ __forceinline__ void get(uint4 w, float* x) {
+    x[0] = __uint_as_float(w.x); x[1] = __uint_as_float(w.y); x[2] = __uint_as_float(w.z); x[3] = __uint_as_float(w.w);
+  }
+  static __device__ __forceinline__ uint4 put(const float* x) {
+    return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+  }
+};
+template <> struct Piece<bf16> {
+  static constexpr int N = 8;
+  static __device__ __forceinline__ void get(uint4 w, float* x) {
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(u[i] << 16); x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u); }
+  }
+  static __device__ __forceinline__ uint4 put(const float* x) {
+    uint32_t u[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __nv_bfloat162 v = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+      u[i] = *reinterpret_cast<const uint32_t*>(&v);
+    }
+    return make_uint4(u[0], u[1], u[2], u[3]);
+  }
+};
+
+// The row's heads, two pieces of 16 bytes per thread and step.  Pieces a and b of a head: with halves as pairs a and its partner while
+// there are pairs; behind them, and with neighbours as pairs from the start, consecutive ones.  UNTURNED: values, copied.
+template <typename T, bool UNTURNED>
+__device__ __forceinline__ void stream_heads(const Heads& h, const Turn& turn, int d, const float2* cs) {
+  constexpr int N = Piece<T>::N;
+  const int pieces = d / N, steps = (pieces + 1) / 2, paired = UNTURNED || turn.interleaved ? 0 : turn.half / N;
+  for (int i0 = threadIdx.x; i0 < h.n * steps; i0 += 2 * THREADS) {
+    uint4 x[2][2];
+    int a[2], b[2], head[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int i = i0 + k * THREADS;
+      a[k] = b[k] = -1;
+      if (i < h.n * steps) {
+        head[k] = i / steps;
+        const int j = i - head[k] * steps;
+        a[k] = j < paired ? j : 2 * j;
+        b[k] = j < paired ? j + paired : 2 * j + 1 < pieces ? 2 * j + 1 : -1;
+        const uint4* src = reinterpret_cast<const uint4*>(h.src) + (size_t)head[k] * pieces;
+        x[k][0] = src[a[k]];
+        if (b[k] >= 0) x[k][1] = src[b[k]];
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      if (a[k] < 0) continue;
+      if (!UNTURNED) {
+        float u[N], v[N];
+        Piece<T>::get(x[k][0], u);
+        Piece<T>::get(x[k][1], v);
+        if (turn.interleaved) {
+#pragma unroll
+          for (int e = 0; e < N; e += 2) {
+            const int pa = (a[k] * N + e) / 2, pb = pa + N / 2;
+            if (pa < turn.half) { const float2 y = turned(u[e], u[e + 1], cs[pa]); u[e] = y.x; u[e + 1] = y.y; }
+            if (pb < turn.half) { const float2 y = turned(v[e], v[e + 1], cs[pb]); v[e] = y.x; v[e + 1] = y.y; }
+          }
+        } else if (a[k] < paired) {
+#pragma unroll
+          for (int e = 0; e < N; ++e) {
+            const float2 y = turned(u[e], v[e], cs[a[k] * N + e]);
+            u[e] = y.x;
+            v[e] = y.y;
+          }
+        }
+        x[k][0] = Piece<T>::put(u);
+        x[k][1] = Piece<T>::put(v);
+      }
+      uint4* dst = reinterpret_cast<uint4*>(h.dst + head[k] * h.dst_step);
+      dst[a[k]] = x[k][0];
+      if (b[k] >= 0) dst[b[k]] = x[k][1];
+    }
+  }
+}
+// halves as pairs whose partners do not lie whole pieces apart: one pair, or one element that stays, per thread
+template <typename T>
+__device__ __forceinline__ void stream_elements(const Heads& h, const Turn& turn, int d, const float2* cs) {
+  const int steps = d - turn.half;
+  for (int i = threadIdx.x; i < h.n * steps; i += THREADS) {
+    const int head = i / steps, j = i - head * steps;
+    const T* src = reinterpret_cast<const T*>(h.src) + (size_t)head * d;
+    T* dst = reinterpret_cast<T*>(h.dst + head * h.dst_step);
+    if (j < turn.half) {
+      const float2 y = turned(to_f(src[j]), to_f(src[j + turn.half]), cs[j]);
+      dst[j] = from_f<T>(y.x);
+      dst[j + turn.half] = from_f<T>(y.y);
+    } else {
+      dst[j + turn.half] = src[j + turn.half];
+    }
+  }
+}
+template <typename T>
+__device__ __forceinline__ void turn_heads(const Heads& h, const Turn& turn, int d, const float2* cs) {
+  if (turn.interleaved || turn.half % Piece<T>::N == 0) stream_heads<T, false>(h, turn, d, cs);
+  else stream_elements<T>(h, turn, d, cs);
+}
+
+template <typename T>
+__global__ void __launch_bounds__(THREADS) k_rotary(Turn turn, int heads, int d, const char* x, long long ld, char* out,
+                                                    long long ld_out, const int32_t* positions) {
+  __shared__ float2 cs[MAX_HALF];
+  pdl_enter(POSS_K_ROTARY);
+  const size_t row = blockIdx.x;
+  angles(turn, positions[row], cs);
+  __syncthreads();
+  turn_heads<T>({x + row * ld, out + row * ld_out, (size_t)d * sizeof(T), heads}, turn, d, cs);
+}
+
+struct AppendArgs {
+  PageGeo g;
+  int layer, rows, Hq;
+  char* pool;
+  const char *k, *v, *q;
+  char* out_q;
+  long long ld_kv, ld_q, ld_out_q;           // bytes
+  const int32_t *prefix_len, *n_rows, *positions;
+  int32_t* status;
+};
+template <typename T>
+__global__ void __launch_bounds__(THREADS) k_append_rotary(AppendArgs a, Turn turn) {
+  __shared__ float2 cs[MAX_HALF];
+  pdl_enter(POSS_K_APPEND_ROTARY);
+  const size_t row = blockIdx.x;
+  const int b = blockIdx.x / a.rows, r = blockIdx.x - b * a.rows;
+  const int prefix = a.prefix_len[b], own = a.n_rows ? a.n_rows[b] : a.rows;
+  int position = a.positions ? a.positions[row] : 0;   // (one trip with the lengths)
+  const SeqLen s = seq_len_of(prefix, own, a.rows, (long long)a.g.max_pages * a.g.page);
+  if (s.bad && r == 0 && threadIdx.x == 0) raise_status(a.status, POSS_E_INVALID);
+  if (r >= s.rows) return;
+  const int slot = s.prefix + r, place = slot / a.g.page;
+  if (!a.positions) position = slot;
+  const int p = page_at(a.g.tables + (size_t)b * a.g.max_pages, a.g.max_pages, a.g.n_pages, place);
+  angles(turn, position, cs);
+  __syncthreads();
+  if (a.Hq) turn_heads<T>({a.q + row * a.ld_q, a.out_q + row * a.ld_out_q, (size_t)a.g.d * sizeof(T), a.Hq}, turn, a.g.d, cs);
+  if (p < 0) {
+    if (threadIdx.x == 0) raise_status(a.status, POSS_E_INVALID);
+    return;
+  }
+  const size_t head_bytes = (size_t)a.g.page * a.g.d * sizeof(T);
+  char* const dk = a.pool + (page_offset(a.g, a.layer, p, 0, 0) + (size_t)(slot - place * a.g.page) * a.g.d) * sizeof(T);
+  turn_heads<T>({a.k + row * a.ld_kv, dk, head_bytes, a.g.Hkv}, turn, a.g.d, cs);
+  stream_heads<T, true>({a.v + row * a.ld_kv, dk + a.g.Hkv * head_bytes, head_bytes, a.g.Hkv}, turn, a.g.d, cs);
+}
+
+int turn_check(int head_dim, int rot_dim, float magnitude, const double* freq) {
+  if (rot_dim < 2 || rot_dim % 2 || rot_dim > head_dim || !isfinite(magnitude) || !freq) return POSS_E_INVALID;
+  return rot_dim > POSS_MAX_ROTARY_DIM ? POSS_E_CAPACITY : POSS_OK;
+}
+// rows of `bytes` bytes, ld apart, n of them: does the target touch a source that it is not, row for row
+bool crossed(const void* out, int64_t ld_out, const void* in, int64_t ld_in, size_t bytes, int64_t n) {
+  if (out == in && ld_out == ld_in) return false;
+  return overlap(out, (size_t)(n - 1) * ld_out + bytes, in, (size_t)(n - 1) * ld_in + bytes);
+}
+
+}  // namespace
+
+extern "C" {
+
+int poss_rotary_frequencies(double* h_freq, int rot_dim, double theta, int scaling, double factor, double low, double high,
+                            double original_len) {
+  if (!h_freq || rot_dim < 2 || rot_dim % 2 || !(theta > 1.0) || !isfinite(theta)) return POSS_E_INVALID;
+  if (rot_dim > POSS_MAX_ROTARY_DIM) return POSS_E_CAPACITY;
+  if (scaling < POSS_ROTARY_PLAIN || scaling > POSS_ROTARY_RAMP) return POSS_E_INVALID;
+  if (scaling != POSS_ROTARY_PLAIN && (!(factor >= 1.0) || !isfinite(factor))) return POSS_E_INVALID;
+  const bool parts = scaling == POSS_ROTARY_BANDS || scaling == POSS_ROTARY_RAMP;
+  if (parts && (!(low > 0.0) || !(high > low) || !isfinite(high) || !(original_len > 0.0) || !isfinite(original_len)))
+    return POSS_E_INVALID;
+  if (scaling == POSS_ROTARY_BASE) {
+    if (rot_dim < 4) return POSS_E_INVALID;
+    theta *= pow(factor, (double)rot_dim / (rot_dim - 2));
+  }
+  const double two_pi = 6.283185307179586477, half = rot_dim / 2;
+  // the pair that makes `turns` turns over the original context
+  auto pair_of = [&](double turns) { return half * log(original_len / (turns * two_pi)) / log(theta); };
+  double first = 0.0, last = 0.0;
+  if (scaling == POSS_ROTARY_RAMP) {
+    first = fmax(floor(pair_of(high)), 0.0);
+    last = fmin(ceil(pair_of(low)), (double)rot_dim - 1.0);
+    if (last <= first) last = first + 0.001;
+  }
+  for (int i = 0; i < rot_dim / 2; ++i) {
+    const double f = pow(theta, -(double)i / half);
+    double kept = 1.0;                                    // share of the frequency that is not divided
+    if (scaling == POSS_ROTARY_LINEAR) kept = 0.0;
+    if (scaling == POSS_ROTARY_BANDS) kept = (original_len * f / two_pi - low) / (high - low);
+    if (scaling == POSS_ROTARY_RAMP) kept = 1.0 - (i - first) / (last - first);
+    kept = fmin(fmax(kept, 0.0), 1.0);
+    h_freq[i] = kept * f + (1.0 - kept) * (f / factor);
+    if (scaling == POSS_ROTARY_BASE || scaling == POSS_ROTARY_PLAIN) h_freq[i] = f;
+  }
+  return POSS_OK;
+}
+
+int poss_rotary(const void* x, int64_t ld_x, void* out, int64_t ld_out, int dtype, int64_t n, int heads, int head_dim,
+                const int32_t* positions, const double* freq, int rot_dim, int interleaved, float magnitude, poss_stream stream) {
+  if (dtype != POSS_FP32 && dtype != POSS_BF16) return POSS_E_INVALID;
+  if (n < 0 || heads < 1 || head_dim < 2) return POSS_E_INVALID;
+  const int es = dtype == POSS_BF16 ? 2 : 4;
+  if (head_dim * (int64_t)es % 16) return POSS_E_SHAPE;
+  int rc = turn_check(head_dim, rot_dim, magnitude, freq);
+  if (rc != POSS_OK) return rc;
+  if (n == 0) return POSS_OK;
+  if (n >= (1ll << 31) || head_dim > (1 << 16) || (int64_t)heads * head_dim >= (1ll << 28)) return POSS_E_CAPACITY;
+  if (!x || !out || !positions || !aligned16(x) || !aligned16(out)) return POSS_E_INVALID;
+  const int64_t row = (int64_t)heads * head_dim;
+  if (ld_x < row || ld_out < row || (ld_x * es) % 16 || (ld_out * es) % 16) return POSS_E_INVALID;
+  if (crossed(out, ld_out * es, x, ld_x * es, row * es, n)) return POSS_E_INVALID;
+  int64_t launches = 0;
+  Launcher L{reinterpret_cast<cudaStream_t>(stream), &launches, POSS_OK};
+  const Turn turn = {freq, rot_dim / 2, interleaved != 0, magnitude};
+  launch_pdl(L, dtype == POSS_BF16 ? k_rotary<bf16> : k_rotary<float>, dim3((unsigned)n), dim3(THREADS), 0, turn, heads, head_dim,
+             reinterpret_cast<const char*>(x), ld_x * es, reinterpret_cast<char*>(out), ld_out * es, positions);
+  return L.err;
+}
+
+int poss_pages_append_rotary(const poss_page_pool* pool, int layer, void* kv_pages, const int32_t* tables, int max_pages, int batch,
+                             int rows, const void* k, const void* v, int64_t ld_kv, int n_q_heads, const void* q, int64_t ld_q,
+                             void* out_q, int64_t ld_out_q, const int32_t* prefix_len, const int32_t* n_rows,
+                             const int32_t* positions, const double* freq, int rot_dim, int interleaved, float magnitude,
+                             int32_t* status, poss_stream stream) {
+  int rc = page_pool_check(pool);
+  if (rc != POSS_OK) return rc;
+  if (batch < 0 || rows < 0 || n_q_heads < 0 || layer < 0 || layer >= pool->n_layers) return POSS_E_INVALID;
+  rc = turn_check(pool->head_dim, rot_dim, magnitude, freq);
+  if (rc != POSS_OK) return rc;
+  if (batch == 0 || rows == 0) return POSS_OK;
+  rc = page_table_check(pool, max_pages, batch);
+  if (rc != POSS_OK) return rc;
+  if (rows > 65535 || n_q_heads > (1 << 16)) return POSS_E_CAPACITY;
+  if (!kv_pages || !tables || !k || !v || !prefix_len) return POSS_E_INVALID;
+  const int64_t es = pool->dtype == POSS_BF16 ? 2 : 4, d = pool->head_dim;
+  if (ld_kv < pool->n_kv_heads * d || (ld_kv * es) % 16) return POSS_E_INVALID;
+  if (!aligned16(kv_pages) || !aligned16(k) || !aligned16(v)) return POSS_E_INVALID;
+  if (n_q_heads) {
+    if (!q || !out_q || !aligned16(q) || !aligned16(out_q)) return POSS_E_INVALID;
+    const int64_t row = n_q_heads * d, n = (int64_t)batch * rows;
+    if (ld_q < row || ld_out_q < row || (ld_q * es) % 16 || (ld_out_q * es) % 16) return POSS_E_INVALID;
+    if (crossed(out_q, ld_out_q * es, q, ld_q * es, row * es, n)) return POSS_E_INVALID;
+    // (in place the three may be parts of one projection, whose rows lie between one another)
+    const size_t kv_bytes = (size_t)((n - 1) * ld_kv + pool->n_kv_heads * d) * es;
+    if (out_q != q && (overlap(out_q, ((n - 1) * ld_out_q + row) * es, k, kv_bytes) ||
+                       overlap(out_q, ((n - 1) * ld_out_q + row) * es, v, kv_bytes)))
+      return POSS_E_INVALID;
+  }
+  int64_t launches = 0;
+  Launcher L{reinterpret_cast<cudaStream_t>(stream), &launches, POSS_OK};
+  AppendArgs a;
+  a.g = page_geo(pool, tables, max_pages);
+  a.layer = layer; a.rows = rows; a.Hq = n_q_heads;
+  a.pool = reinterpret_cast<char*>(kv_pages);
+  a.k = reinterpret_cast<const char*>(k); a.v = reinterpret_cast<const char*>(v); a.q = reinterpret_cast<const char*>(q);
+  a.out_q = reinterpret_cast<char*>(out_q);
+  a.ld_kv = ld_kv * es; a.ld_q = ld_q * es; a.ld_out_q = ld_out_q * es;
+  a.prefix_len = prefix_len; a.n_rows = n_rows; a.positions = positions; a.status = status;
+  const Turn turn = {freq, rot_dim / 2, interleaved != 0, magnitude};
+  launch_pdl(L, pool->dtype == POSS_BF16 ? k_append_rotary<bf16> : k_append_rotary<float>, dim3((unsigned)(batch * rows)),
+             dim3(THREADS), 0, a, turn);
+  return L.err;
+}
+
+}  // extern "C"
