@@ -14,7 +14,7 @@ OUT = os.path.join(HERE, "libposs.so")
 CALLS = os.path.join(HERE, "_paged_calls" + sysconfig.get_config_var("EXT_SUFFIX"))
 CALLS_TORCH = os.path.join(HERE, "_build", "_paged_calls.torch")   # the torch that it was built with
 SOURCES = ["kernels_basic.cu", "kernels_attention.cu", "kernels_attention_mma.cu", "kernels_tree.cu", "gemm_tc.cu", "attention_tc.cu", "poss_api.cu", "no_alloc.cu",
-           "paged_pages.cu", "paged_attention.cu", "paged_attention_tc.cu", "beam_select.cu", "rotary.cu", "paged_mass.cu", "paged_evict.cu",
+           "paged_pages.cu", "paged_attention.cu", "paged_attention_tc.cu", "beam_select.cu", "rotary.cu", "paged_mass.cu", "paged_mass_tc.cu", "paged_evict.cu",
            "token_logprobs.cu"]
 FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
          "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden"]

@@ -373,7 +373,8 @@ int attend(const poss_page_pool* pool, int layer, const void* kv_pages, const in
   m.mass_slots = mass->slots;
   m.weights = mass->weights;
   m.scale_log2 = scale * 1.4426950408889634f;
-  launch_paged_mass_simt(L, m, kv_pages, pool->dtype);
+  if (paged_attn_tc_supported(*pool, a.G, scale)) launch_paged_mass_tc(L, m, kv_pages);
+  else launch_paged_mass_simt(L, m, kv_pages, pool->dtype);
   return L.err;
 }
 

@@ -1,6 +1,7 @@
 // Tree-masked attention over pages: what the two kernels and their host side share.
 #pragma once
 #include "paged.cuh"
+#include <cuda.h>
 
 struct PagedAttnArgs {
   PageGeo g;
@@ -31,6 +32,12 @@ bool paged_attn_tc_supported(const poss_page_pool& p, int G, float scale);
 size_t paged_attn_tc_workspace(const poss_page_pool& p, int batch, int rows, int Hq, int max_pages);
 void launch_paged_attn_tc(Launcher& L, const PagedAttnArgs& a, const void* pool, const poss_page_pool& p);
 
+// Tensor maps of the tcgen05 kernels.  The layer as a matrix of slots: rows (page, keys / values, head, slot), head_dim columns, a box of
+// `slots` rows times 64 columns; rows_total is the first row behind it.  The queries: columns, heads of a group, groups (KV heads), tree
+// rows, sequences, a box of `tree_rows` tree rows of one KV head times 64 columns; rows behind the call's last one arrive as zeros.
+bool paged_kv_map(CUtensorMap* map, const PagedAttnArgs& a, const void* layer, int slots);
+bool paged_q_map(CUtensorMap* map, const PagedAttnArgs& a, int tree_rows);
+
 // The weight that every slot draws, from the queries and the rows' maxima and sums (a.ml)
 struct PagedMassArgs {
   PagedAttnArgs a;
@@ -39,6 +46,9 @@ struct PagedMassArgs {
   const float* weights;                // NULL, or [batch][rows]
   float scale_log2;
 };
+// tcgen05 kernel: the shapes of the attention's
+void launch_paged_mass_tc(Launcher& L, const PagedMassArgs& s, const void* pool);
+// SIMT kernel: every type and shape
 void launch_paged_mass_simt(Launcher& L, const PagedMassArgs& s, const void* pool, int dtype);
 
 // visibility of 32 consecutive slots from `key0` on: every slot below `prefix`, slot prefix + t iff bit t of

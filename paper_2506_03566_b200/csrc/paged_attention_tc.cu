@@ -266,17 +266,6 @@ __device__ __forceinline__ bool two_halves(const TcArgs& k, const Segment& g) {
 }
 
 // ---- PTX
-__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t* r) {
-  asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {"
-               "%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-               "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-                 "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]),
-                 "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]),
-                 "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]),
-                 "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-               : "r"(taddr));
-}
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {"
                "%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
@@ -294,28 +283,7 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* r) {
                  "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
                : "memory");
 }
-__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1) {
-  asm volatile(
-      "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
-      ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1)
-      : "memory");
-}
-__device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int col, int head, int row,
-                                            int seq) {
-  asm volatile(
-      "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];"
-      ::"r"(dst), "l"(map), "r"(bar), "r"(col), "r"(0), "r"(head), "r"(row), "r"(seq)
-      : "memory");
-}
-// orders the use of registers behind the wait for the loads that fill them
-__device__ __forceinline__ void tie32(uint32_t* r) {
-#pragma unroll
-  for (int i = 0; i < 32; i += 8)
-    asm volatile("" : "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]), "+r"(r[i + 4]), "+r"(r[i + 5]),
-                 "+r"(r[i + 6]), "+r"(r[i + 7]));
-}
 __device__ __forceinline__ uint64_t pack64(uint32_t lo, uint32_t hi) {
   uint64_t d;
   asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "r"(lo), "r"(hi));
@@ -341,11 +309,6 @@ __device__ __forceinline__ uint64_t smem_desc_values(uint32_t addr) {
   d |= 1ull << 46;
   d |= 2ull << 61;
   return d;
-}
-__device__ __forceinline__ bool elect_one() {
-  uint32_t e;
-  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(e));
-  return e != 0;
 }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
@@ -1008,21 +971,6 @@ __global__ void __launch_bounds__(256) k_paged_attn_tc_merge(const TcArgs k, int
   if (a.ml && slice == 0) a.ml[((size_t)b * a.rows + r) * a.Hq + head * a.G + qh] = paged_ml(m, l);
 }
 
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-EncodeTiledFn encode_fn() {
-  static const EncodeTiledFn fn = [] {
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess ||
-        q != cudaDriverEntryPointSuccess)
-      p = nullptr;
-    return reinterpret_cast<EncodeTiledFn>(p);
-  }();
-  return fn;
-}
-
 std::atomic<int> g_lost_loads{0};
 
 constexpr size_t PLAN_BYTES = (sizeof(PlanOut) + 255) / 256 * 256;
@@ -1056,6 +1004,43 @@ void launch(Launcher& L, const TcArgs& k0, const CUtensorMap& map, const CUtenso
 
 }  // namespace
 
+namespace {
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiledFn encode_fn() {
+  static const EncodeTiledFn fn = [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess ||
+        q != cudaDriverEntryPointSuccess)
+      p = nullptr;
+    return reinterpret_cast<EncodeTiledFn>(p);
+  }();
+  return fn;
+}
+}  // namespace
+
+bool paged_kv_map(CUtensorMap* map, const PagedAttnArgs& a, const void* layer, int slots) {
+  const EncodeTiledFn encode = encode_fn();
+  const cuuint64_t dim[2] = {(cuuint64_t)a.g.d, (cuuint64_t)a.g.n_pages * 2 * a.g.Hkv * a.g.page};
+  const cuuint64_t str[1] = {(cuuint64_t)a.g.d * 2};
+  const cuuint32_t box[2] = {64, (cuuint32_t)slots}, one[2] = {1, 1};
+  return encode && encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(layer), dim, str, box, one,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+bool paged_q_map(CUtensorMap* map, const PagedAttnArgs& a, int tree_rows) {
+  const EncodeTiledFn encode = encode_fn();
+  const cuuint64_t row = (cuuint64_t)a.ld_q * 2;
+  const cuuint64_t dim[5] = {(cuuint64_t)a.g.d, (cuuint64_t)a.G, (cuuint64_t)a.g.Hkv, (cuuint64_t)a.rows, (cuuint64_t)a.batch};
+  const cuuint64_t str[4] = {(cuuint64_t)a.g.d * 2, (cuuint64_t)a.G * a.g.d * 2, row, row * a.rows};
+  const cuuint32_t box[5] = {64, (cuuint32_t)a.G, 1, (cuuint32_t)tree_rows, 1}, one[5] = {1, 1, 1, 1, 1};
+  return encode && encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void*>(a.q), dim, str, box, one,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 bool paged_attn_tc_supported(const poss_page_pool& p, int G, float scale) {
   if (G > QR) return false;
   if (p.dtype != POSS_BF16 || (p.head_dim != 64 && p.head_dim != 128)) return false;
@@ -1076,8 +1061,6 @@ void launch_paged_attn_tc(Launcher& L, const PagedAttnArgs& a, const void* pool,
   const int groups = (a.rows + 2 * (QR / a.G) - 1) / (2 * (QR / a.G));
   const long long units = (long long)a.batch * a.g.Hkv * groups * tiles;
   if (units >= (1ll << 31)) { L.err = POSS_E_CAPACITY; return; }
-  EncodeTiledFn encode = encode_fn();
-  if (!encode) { L.err = POSS_E_CUDA; return; }
   TcArgs k;
   memset(&k, 0, sizeof(k));
   k.a = a;
@@ -1091,34 +1074,10 @@ void launch_paged_attn_tc(Launcher& L, const PagedAttnArgs& a, const void* pool,
   int lost = g_lost_loads.load();
   while (lost > 0 && !g_lost_loads.compare_exchange_weak(lost, lost - 1)) {}
   k.inject_lost_load = lost > 0;
-  // The layer as a matrix of slots: rows (page, keys / values, head, slot), head_dim columns.  A box is a page's slots of
-  // one head (at most one tile of keys) times 64 columns.
-  CUtensorMap map;
-  cuuint64_t gdim[2] = {(cuuint64_t)a.g.d, (cuuint64_t)k.rows_total};
-  cuuint64_t gstr[1] = {(cuuint64_t)a.g.d * 2};
-  cuuint32_t box[2] = {64, (cuuint32_t)(a.g.page < KT ? a.g.page : KT)};
-  cuuint32_t estr[2] = {1, 1};
-  if (encode(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<bf16*>(k.layer), gdim, gstr, box, estr,
-             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS) {
+  CUtensorMap map, map_q;
+  if (!paged_kv_map(&map, a, k.layer, a.g.page < KT ? a.g.page : KT) || !paged_q_map(&map_q, a, k.slot_rows)) {
     L.err = POSS_E_CUDA;
     return;
-  }
-  // The queries: columns, heads of a group, groups (KV heads), tree rows, sequences.  A box is a slot's tree rows of one KV
-  // head times 64 columns; rows behind the call's last one arrive as zeros.
-  CUtensorMap map_q;
-  {
-    const cuuint64_t row = (cuuint64_t)a.ld_q * 2;
-    cuuint64_t dim[5] = {(cuuint64_t)a.g.d, (cuuint64_t)a.G, (cuuint64_t)a.g.Hkv, (cuuint64_t)a.rows, (cuuint64_t)a.batch};
-    cuuint64_t str[4] = {(cuuint64_t)a.g.d * 2, (cuuint64_t)a.G * a.g.d * 2, row, row * a.rows};
-    cuuint32_t qbox[5] = {64, (cuuint32_t)a.G, 1, (cuuint32_t)k.slot_rows, 1};
-    cuuint32_t one[5] = {1, 1, 1, 1, 1};
-    if (encode(&map_q, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void*>(a.q), dim, str, qbox, one,
-               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
-               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS) {
-      L.err = POSS_E_CUDA;
-      return;
-    }
   }
   if (a.g.d == 128) launch<128>(L, k, map, map_q, units, tiles, groups);
   else launch<64>(L, k, map, map_q, units, tiles, groups);
