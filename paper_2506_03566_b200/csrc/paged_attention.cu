@@ -322,6 +322,10 @@ struct MassTarget {
   const float* weights;     // NULL, or [batch][rows]
 };
 size_t ml_bytes(int batch, int rows, int Hq) { return ((size_t)batch * rows * Hq * sizeof(float2) + 255) / 256 * 256; }
+size_t scores_bytes(const poss_page_pool* pool, int batch, int rows, int Hq, int max_pages) {
+  if (!paged_attn_tc_supported(*pool, Hq / pool->n_kv_heads, 1.f)) return 0;
+  return (paged_attn_tc_scores(*pool, batch, rows, Hq, max_pages) + 255) / 256 * 256;
+}
 
 // both entries; mass NULL: the attention alone
 int attend(const poss_page_pool* pool, int layer, const void* kv_pages, const int32_t* tables, int max_pages, int batch, int rows,
@@ -344,7 +348,7 @@ int attend(const poss_page_pool* pool, int layer, const void* kv_pages, const in
   if (!aligned16(kv_pages) || !aligned16(q) || !aligned16(out)) return POSS_E_INVALID;
   const size_t ws_bytes = poss_paged_attention_workspace_bytes(pool, batch, rows, n_q_heads, max_pages);
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) ||
-      workspace_bytes < ws_bytes + (mass ? ml_bytes(batch, rows, n_q_heads) : 0))
+      workspace_bytes < ws_bytes + (mass ? ml_bytes(batch, rows, n_q_heads) + scores_bytes(pool, batch, rows, n_q_heads, max_pages) : 0))
     return POSS_E_WORKSPACE;
   // one block's queries may be read while another's rows are written
   const size_t row = (size_t)n_q_heads * pool->head_dim * es, n = (size_t)batch * rows;
@@ -364,16 +368,28 @@ int attend(const poss_page_pool* pool, int layer, const void* kv_pages, const in
   a.q = q; a.ld_q = ld_q; a.prefix_len = prefix_len; a.n_rows = n_rows; a.mask = anc_mask;
   a.mask_words = (rows + 63) / 64; a.scale = scale; a.out = out; a.ws = workspace; a.status = status;
   a.ml = mass ? reinterpret_cast<float2*>(reinterpret_cast<char*>(workspace) + ws_bytes) : nullptr;
-  if (paged_attn_tc_supported(*pool, a.G, scale)) launch_paged_attn_tc(L, a, kv_pages, *pool);
-  else launch_paged_attn_simt(L, a, kv_pages, pool->dtype);
-  if (!mass || L.err != POSS_OK) return L.err;
+  const bool tc = paged_attn_tc_supported(*pool, a.G, scale);
+  if (!mass) {
+    if (tc) launch_paged_attn_tc(L, a, kv_pages, *pool);
+    else launch_paged_attn_simt(L, a, kv_pages, pool->dtype);
+    return L.err;
+  }
   PagedMassArgs m;
   m.a = a;
   m.mass = mass->mass + (size_t)layer * batch * pool->n_kv_heads * mass->slots;
   m.mass_slots = mass->slots;
   m.weights = mass->weights;
   m.scale_log2 = scale * 1.4426950408889634f;
-  if (paged_attn_tc_supported(*pool, a.G, scale)) launch_paged_mass_tc(L, m, kv_pages);
+  m.scores = nullptr;
+  if (tc && scores_bytes(pool, batch, rows, n_q_heads, max_pages)) {
+    m.scores = reinterpret_cast<float*>(reinterpret_cast<char*>(a.ml) + ml_bytes(batch, rows, n_q_heads));
+    launch_paged_attn_tc(L, a, kv_pages, *pool, &m);
+    return L.err;
+  }
+  if (tc) launch_paged_attn_tc(L, a, kv_pages, *pool);
+  else launch_paged_attn_simt(L, a, kv_pages, pool->dtype);
+  if (L.err != POSS_OK) return L.err;
+  if (tc) launch_paged_mass_tc(L, m, kv_pages);
   else launch_paged_mass_simt(L, m, kv_pages, pool->dtype);
   return L.err;
 }
@@ -425,7 +441,7 @@ int poss_paged_tree_attention(const poss_page_pool* pool, int layer, const void*
 
 size_t poss_paged_attention_mass_workspace_bytes(const poss_page_pool* pool, int batch, int rows, int n_q_heads, int max_pages) {
   const size_t n = poss_paged_attention_workspace_bytes(pool, batch, rows, n_q_heads, max_pages);
-  return n ? n + ml_bytes(batch, rows, n_q_heads) : 0;
+  return n ? n + ml_bytes(batch, rows, n_q_heads) + scores_bytes(pool, batch, rows, n_q_heads, max_pages) : 0;
 }
 
 int poss_paged_tree_attention_mass(const poss_page_pool* pool, int layer, const void* kv_pages, float* mass, int64_t mass_slots,

@@ -30,7 +30,12 @@ void launch_paged_attn_simt(Launcher& L, const PagedAttnArgs& a, const void* poo
 // scale > 0
 bool paged_attn_tc_supported(const poss_page_pool& p, int G, float scale);
 size_t paged_attn_tc_workspace(const poss_page_pool& p, int batch, int rows, int Hq, int max_pages);
-void launch_paged_attn_tc(Launcher& L, const PagedAttnArgs& a, const void* pool, const poss_page_pool& p);
+// mass (with room for scores): the slots' weights too, for calls of so few lines (rows x heads of a group) that paged_attn_tc_scores, the
+// bytes of that room, is not 0
+struct PagedMassArgs;
+size_t paged_attn_tc_scores(const poss_page_pool& p, int batch, int rows, int Hq, int max_pages);
+void launch_paged_attn_tc(Launcher& L, const PagedAttnArgs& a, const void* pool, const poss_page_pool& p,
+                          const PagedMassArgs* mass = nullptr);
 
 // Tensor maps of the tcgen05 kernels.  The layer as a matrix of slots: rows (page, keys / values, head, slot), head_dim columns, a box of
 // `slots` rows times 64 columns; rows_total is the first row behind it.  The queries: columns, heads of a group, groups (KV heads), tree
@@ -45,6 +50,7 @@ struct PagedMassArgs {
   long long mass_slots;
   const float* weights;                // NULL, or [batch][rows]
   float scale_log2;
+  float* scores;                       // NULL, or scratch of paged_attn_tc_scores bytes
 };
 // tcgen05 kernel: the shapes of the attention's
 void launch_paged_mass_tc(Launcher& L, const PagedMassArgs& s, const void* pool);

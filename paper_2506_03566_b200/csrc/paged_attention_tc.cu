@@ -95,6 +95,13 @@ struct TcArgs {
   int inject_lost_load;
   uint32_t smem_bytes;
   const bf16* layer;                    // the layer's first element
+  // SCORES: few rows leave their scores for the slots' weights, -inf where they do not see a slot: [batch][Hkv][rows * G][scores_ld]
+  float* scores;
+  long long scores_ld;
+  float* mass;                          // the layer's weights, see PagedMassArgs
+  long long mass_slots;
+  const float* row_weights;
+  int merge_blocks;                     // blocks of the merge; those behind them add up weights
   struct PlanOut* plan;                 // what the merge needs to know, left by the first CTA
 };
 
@@ -366,7 +373,7 @@ __device__ __forceinline__ float* partial_of(const TcArgs& k, int hd, int cta, i
 // ---------------------------------------------------------------------------------------------------- the kernel
 // Every role walks the CTA's segments by itself, in one loop that they share: code that a launch runs once costs its
 // instruction fetches (about 25 cycles per instruction that no warp of the SM has run yet), so there is one copy of it.
-template <int HD>
+template <int HD, bool SCORES>
 __global__ void __launch_bounds__(N_THREADS, 1) k_paged_attn_tc(const __grid_constant__ CUtensorMap map,
                                                                  const __grid_constant__ CUtensorMap map_q,
                                                                  const TcArgs k) {
@@ -569,6 +576,16 @@ __global__ void __launch_bounds__(N_THREADS, 1) k_paged_attn_tc(const __grid_con
             for (int x = 0; x < 32; ++x) {
               if (!((va >> x) & 1u)) sa[x] = 0xff800000u;
               if (!((vb >> x) & 1u)) sb[x] = 0xff800000u;
+            }
+          }
+          if constexpr (SCORES) {                       // (an item of one slot: its line is the thread's row)
+            if (valid) {
+              uint4* const to = reinterpret_cast<uint4*>(k.scores + (((size_t)g.b * a.g.Hkv + g.head) * (a.rows * a.G) + row) * k.scores_ld + key0);
+#pragma unroll
+              for (int x = 0; x < 8; ++x) {
+                to[x] = make_uint4(sa[4 * x], sa[4 * x + 1], sa[4 * x + 2], sa[4 * x + 3]);
+                to[8 + x] = make_uint4(sb[4 * x], sb[4 * x + 1], sb[4 * x + 2], sb[4 * x + 3]);
+              }
             }
           }
           const float mx = max32(sb, max32(sa, -INFINITY)) * k.scale_log2;
@@ -897,7 +914,75 @@ __global__ void __launch_bounds__(N_THREADS, 1) k_paged_attn_tc(const __grid_con
 
 // ---------------------------------------------------------------------------------------------------- merge
 // A block: 32 query rows of one item, eight threads per row.  The item's segments lie in consecutive CTAs, in key order.
+// SCORES: the blocks behind them are dealt the slots of the item, 1024 at a time, and add their weights up from the scores: in the same
+// launch, so that a token's call has no third one.  The lines' maxima and sums come from the parts once more.
 template <int HD>
+__device__ __forceinline__ void add_weights(const TcArgs& k, const SeqWork& s, int b, int head, uint32_t total, uint32_t before, int whole,
+                                            int cut_grid, float2 (*s_ml)[32]) {
+  const PagedAttnArgs& a = k.a;
+  const int t = threadIdx.x, lines = s.rows * a.G;
+  int first = 0, last = 0, which = 0;
+  if (!whole) {
+    const Cut cut(total, cut_grid);
+    const uint32_t u0 = before + (uint32_t)head * s.tiles;
+    first = cut.cta_of(u0);
+    last = cut.cta_of(u0 + s.tiles - 1);
+    which = cut.begin(first) < u0 ? 1 : 0;
+  }
+  const bool parts = first != last;
+  if (parts) {
+    for (int i = t >> 5; i <= last - first; i += 8)
+      if ((t & 31) < lines)
+        s_ml[i][t & 31] = __ldcg(reinterpret_cast<const float2*>(partial_of(k, HD, first + i, i == 0 ? which : 0) + (size_t)k.row_cap * HD) + (t & 31));
+    __syncthreads();
+  }
+  float2 own = make_float2(INFINITY, 0.f);                // thread < 32: its line's maximum and the inverse of its sum times the row's weight
+  if (t < lines) {
+    const size_t row = (size_t)b * a.rows + t / a.G;
+    if (parts) {
+      float m = -INFINITY, l = 0.f;
+      for (int i = 0; i <= last - first; ++i) m = fmaxf(m, s_ml[i][t].x);
+      for (int i = 0; i <= last - first; ++i) {           // (as the merge does)
+        const float2 x = s_ml[i][t];
+        const float c = x.x == -INFINITY ? (x.y == 0.f ? 0.f : 1.f) : ex2(x.x - m);
+        if (c != 0.f) l = fmaf(x.y, c, l);
+      }
+      own = paged_ml(m, l);
+    } else {
+      own = __ldcg(a.ml + row * a.Hq + head * a.G + t % a.G);
+    }
+    own.y *= k.row_weights ? k.row_weights[row] : 1.f;
+  }
+  __syncthreads();
+  if (t < 32) s_ml[0][t] = own;
+  __syncthreads();
+  const float* const scores = k.scores + ((size_t)b * a.g.Hkv + head) * (a.rows * a.G) * k.scores_ld;
+  float* const mass = k.mass + ((size_t)b * a.g.Hkv + head) * k.mass_slots;
+  const int step = (gridDim.x - k.merge_blocks) * 1024;
+  for (int key = (blockIdx.x - k.merge_blocks) * 1024 + 4 * t; key < s.total; key += step) {
+    float old[4], sum[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      old[x] = key + x < s.prefix ? mass[key + x] : 0.f;
+      sum[x] = 0.f;
+    }
+#pragma unroll 4
+    for (int i = 0; i < lines; ++i) {
+      const float4 y = __ldcg(reinterpret_cast<const float4*>(scores + i * k.scores_ld + key));
+      const float2 c = s_ml[0][i];
+      const float v[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const float p = ex2(fmaf(v[x], k.scale_log2, -c.x)) * c.y;
+        sum[x] += v[x] == -INFINITY ? 0.f : p;            // (unseen: nothing, even where the row's sum is NaN)
+      }
+    }
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+      if (key + x < s.total) mass[key + x] = old[x] + sum[x];
+  }
+}
+template <int HD, bool SCORES>
 __global__ void __launch_bounds__(256) k_paged_attn_tc_merge(const TcArgs k, int max_groups) {
   constexpr int NV = HD / 32;                             // float4 per thread
   __shared__ float2 s_ml[MAX_CTAS][32];
@@ -908,6 +993,12 @@ __global__ void __launch_bounds__(256) k_paged_attn_tc_merge(const TcArgs k, int
   const uint32_t total = __ldcg(&plan->total), before = __ldcg(&plan->before[b]);
   const int whole = __ldcg(&plan->whole), cut_grid = __ldcg(&plan->grid);
   const SeqWork s = seq_work(k, b);
+  if constexpr (SCORES) {
+    if ((int)blockIdx.x >= k.merge_blocks) {
+      if (s.rows) add_weights<HD>(k, s, b, head, total, before, whole, cut_grid, s_ml);
+      return;
+    }
+  }
   if (whole || group >= s.groups) return;                 // (whole: nothing was cut)
   // line rr of the item: slot, tree row and head
   const int rr = blockIdx.x * 32 + (threadIdx.x & 31), slice = threadIdx.x >> 5, line = rr % QR;
@@ -968,7 +1059,7 @@ __global__ void __launch_bounds__(256) k_paged_attn_tc_merge(const TcArgs k, int
   for (int v = 0; v < NV; ++v)
     *reinterpret_cast<uint2*>(out + 4 * v) =
         make_uint2(pack_bf16(o[v].x * inv, o[v].y * inv), pack_bf16(o[v].z * inv, o[v].w * inv));
-  if (a.ml && slice == 0) a.ml[((size_t)b * a.rows + r) * a.Hq + head * a.G + qh] = paged_ml(m, l);
+  if (!SCORES && a.ml && slice == 0) a.ml[((size_t)b * a.rows + r) * a.Hq + head * a.G + qh] = paged_ml(m, l);
 }
 
 std::atomic<int> g_lost_loads{0};
@@ -977,7 +1068,7 @@ constexpr size_t PLAN_BYTES = (sizeof(PlanOut) + 255) / 256 * 256;
 // lines of an item that can hold query rows: one slot's, or both
 int row_cap_of(int rows, int G) { return rows > QR / G ? 2 * QR : (rows * G + 31) / 32 * 32; }
 
-template <int HD>
+template <int HD, bool SCORES>
 void launch(Launcher& L, const TcArgs& k0, const CUtensorMap& map, const CUtensorMap& map_q, long long units, long long tiles, int groups) {
   using Z = Shape<HD>;
   TcArgs k = k0;
@@ -987,7 +1078,7 @@ void launch(Launcher& L, const TcArgs& k0, const CUtensorMap& map, const CUtenso
   static PerDeviceFlags attr_done;
   bool* attr = attr_done.current();
   if (!attr || !*attr) {
-    if (cudaFuncSetAttribute(k_paged_attn_tc<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) {
+    if (cudaFuncSetAttribute(k_paged_attn_tc<HD, SCORES>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) {
       L.err = POSS_E_CUDA;
       return;
     }
@@ -997,9 +1088,17 @@ void launch(Launcher& L, const TcArgs& k0, const CUtensorMap& map, const CUtenso
   const int sms = current_sm_count();
   int ctas = units < sms ? (int)units : sms;
   if (ctas > MAX_CTAS) ctas = MAX_CTAS;
-  launch_pdl(L, k_paged_attn_tc<HD>, dim3(ctas), dim3(N_THREADS), smem, map, map_q, k);
-  if (tiles > 1 && L.err == POSS_OK)                      // (an item of one tile is never cut)
-    launch_pdl(L, k_paged_attn_tc_merge<HD>, dim3(k.row_cap / 32, a.g.Hkv * groups, a.batch), dim3(256), 0, k, groups);
+  k.merge_blocks = tiles > 1 ? k.row_cap / 32 : 0;        // (an item of one tile is never cut)
+  launch_pdl(L, k_paged_attn_tc<HD, SCORES>, dim3(ctas), dim3(N_THREADS), smem, map, map_q, k);
+  int blocks = k.merge_blocks;
+  if (SCORES) {
+    // weights: some eight blocks per SM in all, each with 1024 slots at least
+    const long long items = (long long)a.batch * a.g.Hkv, most = (tiles * KT + 1023) / 1024;
+    const long long n = (8 * sms + items - 1) / items;
+    blocks += (int)(n < most ? n : most);
+  }
+  if (blocks && L.err == POSS_OK)
+    launch_pdl(L, k_paged_attn_tc_merge<HD, SCORES>, dim3(blocks, a.g.Hkv * groups, a.batch), dim3(256), 0, k, groups);
 }
 
 }  // namespace
@@ -1049,6 +1148,17 @@ bool paged_attn_tc_supported(const poss_page_pool& p, int G, float scale) {
   return s == 16 || s == 32 || s == 64 || s == 128 || s == 256;
 }
 
+// Scores go through memory (4 bytes to and fro per line and slot) where that is no more than reading the keys again (2 bytes per element) to
+// form them anew.  16 trees of 4 heads over up to 8191 slots, attention and weights: 1 row 106 us (keys again: 144), 4 rows 114 (150), 8 rows
+// 141 (147), 9 rows, just above, 148; 64 single tokens over up to 8000: 306 (413).
+constexpr size_t MAX_SCORES = (size_t)1 << 29;            // a table with room for far more slots than that reads keys again
+size_t paged_attn_tc_scores(const poss_page_pool& p, int batch, int rows, int Hq, int max_pages) {
+  const int lines = rows * (Hq / p.n_kv_heads);
+  if (lines > p.head_dim / 4) return 0;
+  const size_t ld = ((size_t)max_pages * p.page_slots + KT - 1) / KT * KT, n = (size_t)batch * p.n_kv_heads * lines * ld * 4;
+  return n <= MAX_SCORES ? n : 0;
+}
+
 size_t paged_attn_tc_workspace(const poss_page_pool& p, int batch, int rows, int Hq, int max_pages) {
   // the plan; two partials per CTA (its first and its last segment); the grid is at most the SM count
   (void)batch; (void)max_pages;
@@ -1056,7 +1166,7 @@ size_t paged_attn_tc_workspace(const poss_page_pool& p, int batch, int rows, int
   return PLAN_BYTES + (size_t)(sms < MAX_CTAS ? sms : MAX_CTAS) * 2 * row_cap_of(rows, Hq / p.n_kv_heads) * (p.head_dim + 2) * 4;
 }
 
-void launch_paged_attn_tc(Launcher& L, const PagedAttnArgs& a, const void* pool, const poss_page_pool& p) {
+void launch_paged_attn_tc(Launcher& L, const PagedAttnArgs& a, const void* pool, const poss_page_pool& p, const PagedMassArgs* mass) {
   const long long tiles = ((long long)a.g.max_pages * a.g.page + KT - 1) / KT;
   const int groups = (a.rows + 2 * (QR / a.G) - 1) / (2 * (QR / a.G));
   const long long units = (long long)a.batch * a.g.Hkv * groups * tiles;
@@ -1079,8 +1189,18 @@ void launch_paged_attn_tc(Launcher& L, const PagedAttnArgs& a, const void* pool,
     L.err = POSS_E_CUDA;
     return;
   }
-  if (a.g.d == 128) launch<128>(L, k, map, map_q, units, tiles, groups);
-  else launch<64>(L, k, map, map_q, units, tiles, groups);
+  if (!mass) {
+    if (a.g.d == 128) launch<128, false>(L, k, map, map_q, units, tiles, groups);
+    else launch<64, false>(L, k, map, map_q, units, tiles, groups);
+    return;
+  }
+  k.scores = mass->scores;
+  k.scores_ld = tiles * KT;
+  k.mass = mass->mass;
+  k.mass_slots = mass->mass_slots;
+  k.row_weights = mass->weights;
+  if (a.g.d == 128) launch<128, true>(L, k, map, map_q, units, tiles, groups);
+  else launch<64, true>(L, k, map, map_q, units, tiles, groups);
 }
 
 extern "C" int poss_debug_paged_lose_load(int launches) {
