@@ -3,20 +3,24 @@
 // Of a sequence's n slots keep[b] stay, for every layer and KV head its own: the first `first`, the last `recent`, and of those between
 // the ones with the greatest weight, ties to the lower slot.  They move to slots 0 .. keep - 1 in their order, weights with them.
 //
-//   choose  a block per (sequence, layer, KV head).  Weights become whole numbers that order alike; three rounds over 11, 11 and 10 of
-//           their bits count how many share each value of those bits and narrow the last one that stays down to its value T and to how
-//           many slots equal to T stay (the lowest ones).  A walk over the slots in order then numbers those that stay.
+//   choose  a block per (sequence, layer, KV head).  Weights become whole numbers that order alike; a block has 8192 in registers (16 rows
+//           of 512 slots), more are read again in each round.  Three rounds over 11, 11 and 10 of the numbers' bits count how many
+//           share each value of those bits and narrow the last one that stays down to its value T and to how many slots equal to T
+//           stay (the lowest ones).  Ballots and one sum over rows and warps then number the slots that stay.
 //   move    a block per (sequence, layer, KV head, keys / values) brings the rows forward, some dozen at a time.  A row's new place is
 //           never behind its old one and rows go in order, so a step may write as soon as all of its own rows are in registers: what
-//           it overwrites is gone or has been read.
-// What bounds it: memory in the move; in the choice the rounds' trips over the weights (from L2) and the counts in shared memory.
+//           it overwrites is gone or has been read.  The next step's places are looked up while a step's rows are on their way.  Where
+//           blocks are few, several share a row, each with columns of its own.
+// What bounds it: memory in the move (XX); trips and barriers in the choice (YY).
 #include "paged.cuh"
 
 POSS_TRACE_REGISTER()
 
 namespace {
 
-constexpr int CHOOSE_THREADS = 512, MOVE_THREADS = 256;
+constexpr int CHOOSE_THREADS = 512, CHOOSE_WARPS = 16, MOVE_THREADS = 256;
+constexpr int PER = 16;                      // slots per thread and chunk
+constexpr int CHUNK = CHOOSE_THREADS * PER;
 constexpr int BINS = 2048;
 
 struct EvictArgs {
@@ -36,9 +40,8 @@ __device__ __forceinline__ uint32_t order_of(float x) {
   const uint32_t b = __float_as_uint(x + 0.f);
   return x != x ? 0u : b & 0x80000000u ? ~b : b | 0x80000000u;
 }
-// exclusive prefix sum over the block; *total = the sum.  sums: one int per warp
-template <int THREADS> __device__ __forceinline__ int scan(int v, int* sums, int* total) {
-  constexpr int WARPS = THREADS / 32;
+// exclusive prefix sum over the block; *total = the sum.  sums: one int per warp, free for use behind the barrier before the call
+__device__ __forceinline__ int scan(int v, int* sums, int* total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   int x = v;
 #pragma unroll
@@ -46,42 +49,53 @@ template <int THREADS> __device__ __forceinline__ int scan(int v, int* sums, int
     const int y = __shfl_up_sync(0xffffffffu, x, o);
     if (lane >= o) x += y;
   }
-  __syncthreads();                                        // the sums of an earlier scan have been read
   if (lane == 31) sums[warp] = x;
   __syncthreads();
-  int w = lane < WARPS ? sums[lane] : 0;
-#pragma unroll
-  for (int o = 1; o < WARPS; o <<= 1) {
-    const int y = __shfl_up_sync(0xffffffffu, w, o);
-    if (lane >= o) w += y;
-  }
-  *total = __shfl_sync(0xffffffffu, w, WARPS - 1);
-  const int up = __shfl_sync(0xffffffffu, w, warp ? warp - 1 : 0);
-  return x - v + (warp ? up : 0);
+  const int w = lane < CHOOSE_WARPS ? sums[lane] : 0;
+  *total = __reduce_add_sync(0xffffffffu, w);
+  return x - v + __reduce_add_sync(0xffffffffu, lane < warp ? w : 0);
 }
 
 __global__ void __launch_bounds__(CHOOSE_THREADS) k_evict_choose(EvictArgs a) {
-  __shared__ int s_bins[BINS], s_sums[CHOOSE_THREADS / 32], s_bin, s_left;
+  static_assert(PER * CHOOSE_WARPS <= CHOOSE_THREADS && CHOOSE_WARPS * 32 == CHOOSE_THREADS, "a count per row and warp");
+  __shared__ int s_bins[BINS], s_sums[4][CHOOSE_WARPS], s_bin, s_left, s_hole;
+  __shared__ int s_sure[PER * CHOOSE_WARPS], s_tie[PER * CHOOSE_WARPS];
   pdl_enter(POSS_K_EVICT_CHOOSE);
-  const int t = threadIdx.x;
+  const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
   const int head = blockIdx.x % a.g.Hkv, lb = blockIdx.x / a.g.Hkv, b = lb % a.batch;
   const int n = a.seq_len[b], keep = a.keep[b];
   const long long slots = (long long)a.g.max_pages * a.g.page;
   bool ok = n >= 0 && n <= slots && keep >= 0 && (n <= keep || (long long)a.first + a.recent <= keep);
+  const size_t row = (size_t)lb * a.g.Hkv + head;
+  const float* x = a.mass + row * a.mass_slots;
+  float* out = a.out_mass + row * a.mass_slots;
+  float w[PER];                                           // the thread's slots of a chunk, one of each row
+  auto slot = [&](int chunk, int p) { return chunk * CHUNK + p * CHOOSE_THREADS + t; };
+  auto rows_of = [&](int chunk) { return min(PER, (n - chunk * CHUNK + CHOOSE_THREADS - 1) / CHOOSE_THREADS); };
+  auto load = [&](int chunk) {
+#pragma unroll
+    for (int p = 0; p < PER; ++p) {
+      const int i = slot(chunk, p);
+      w[p] = i < n ? x[i] : 0.f;
+    }
+  };
+  const bool cuts = ok && n > keep;
+  const int chunks = cuts ? (n + CHUNK - 1) / CHUNK : 0;
+  if (chunks == 1) load(0);
+  // (the pages are looked at while the weights are on their way)
   const int32_t* table = a.g.tables + (size_t)b * a.g.max_pages;
-  if (ok && n > keep)
+  if (cuts)
     for (int i = t; i < (n + a.g.page - 1) / a.g.page; i += CHOOSE_THREADS) ok &= page_at(table, a.g.max_pages, a.g.n_pages, i) >= 0;
+  for (int i = t; i < BINS; i += CHOOSE_THREADS) s_bins[i] = 0;
+  if (t == 0) s_hole = keep;
   ok = __syncthreads_and(ok);
   const int stays = !ok || n <= keep ? n : keep;
   if (blockIdx.x == (unsigned)(b * a.g.Hkv) && t == 0) {  // (the first layer's first head)
     a.out_len[b] = stays;
     if (!ok) raise_status(a.status, POSS_E_INVALID);
   }
-  const size_t row = (size_t)lb * a.g.Hkv + head;
-  const float* x = a.mass + row * a.mass_slots;
-  float* out = a.out_mass + row * a.mass_slots;
-  if (t == 0) a.hole[row] = stays;
   if (!ok || n <= keep) {
+    if (t == 0) a.hole[row] = stays;
     if (ok && out != x)
       for (int i = t; i < n; i += CHOOSE_THREADS) out[i] = x[i];
     return;
@@ -95,18 +109,28 @@ __global__ void __launch_bounds__(CHOOSE_THREADS) k_evict_choose(EvictArgs a) {
 #pragma unroll 1
     for (int round = 0; round < 3; ++round) {
       const int shift = round == 0 ? 21 : round == 1 ? 10 : 0, bins = round == 2 ? 1024 : 2048;
-      for (int i = t; i < bins; i += CHOOSE_THREADS) s_bins[i] = 0;
-      __syncthreads();
-      for (int i = lo + t; i < hi; i += CHOOSE_THREADS) {
-        const uint32_t u = order_of(x[i]);
-        if ((u & mask) == fixed) atomicAdd(&s_bins[(u >> shift) & (bins - 1)], 1);
+      if (round > 0) {
+        for (int i = t; i < bins; i += CHOOSE_THREADS) s_bins[i] = 0;
+        __syncthreads();
+      }
+#pragma unroll 1
+      for (int c = 0; c < chunks; ++c) {
+        if (chunks > 1) load(c);
+        const int n_rows = rows_of(c);
+#pragma unroll
+        for (int p = 0; p < PER; ++p) {
+          if (p >= n_rows) break;
+          const int i = slot(c, p);
+          const uint32_t u = order_of(w[p]);
+          if (i >= lo && i < hi && (u & mask) == fixed) atomicAdd(&s_bins[(u >> shift) & (bins - 1)], 1);
+        }
       }
       __syncthreads();
       // from the greatest value down: the bin that the left-th falls into
       const int per = bins / CHOOSE_THREADS;              // 4 or 2 bins per thread, greatest first
-      int mine = 0;
+      int mine = 0, total;
       for (int i = 0; i < per; ++i) mine += s_bins[bins - 1 - (t * per + i)];
-      int total, before = scan<CHOOSE_THREADS>(mine, s_sums, &total);
+      int before = scan(mine, s_sums[round], &total);
       if (before < left && left <= before + mine) {
         for (int i = 0; i < per; ++i) {
           const int bin = bins - 1 - (t * per + i), c = s_bins[bin];
@@ -118,87 +142,111 @@ __global__ void __launch_bounds__(CHOOSE_THREADS) k_evict_choose(EvictArgs a) {
       fixed |= (uint32_t)s_bin << shift;
       mask |= (uint32_t)(bins - 1) << shift;
       left = s_left;
-      __syncthreads();
+      // (the next round's counts begin behind a barrier, and with them the writes of s_bin and s_left)
     }
     equal = left;
   } else {
     fixed = 0xffffffffu;                                  // (above every weight)
   }
-  // ---- the slots that stay, in order.  (In place a weight's new place is never behind its old one, and a step's weights are in
-  // registers before the step's barrier.)
+  // ---- the slots that stay, in order: their places.  (In place a weight's new place is never behind its old one, and a chunk's weights are
+  // in registers before the chunk's barrier.)
   int32_t* src = a.src + row * slots;
-  int at = 0, ties = 0, hole = 0x7fffffff;
+  int at = 0, ties = 0, hole = keep;                      // places given so far, ties met so far
 #pragma unroll 1
-  for (int i0 = 0; i0 < n; i0 += CHOOSE_THREADS) {
-    const int i = i0 + t;
-    const float w = i < n ? x[i] : 0.f;
-    const bool inner = i >= lo && i < hi;
-    const uint32_t u = order_of(w);
-    const bool tie = inner && u == fixed;
-    int total;
-    // both numberings in one scan: ties in the upper half
-    const bool sure = i < n && (!inner || u > fixed);
-    const int both = scan<CHOOSE_THREADS>((tie ? 0x10000 : 0) + (sure ? 1 : 0), s_sums, &total);
-    const int tie_no = ties + (both >> 16);               // ties before this slot
-    const bool on = sure || (tie && tie_no < equal);
-    const int place = at + (both & 0xffff) + min(both >> 16, max(equal - ties, 0));
-    if (on) {
-      src[place] = i;
-      out[place] = w;
-      if (place != i) hole = min(hole, place);
+  for (int c = 0; c < chunks; ++c) {
+    if (chunks > 1) load(c);
+    const int n_rows = rows_of(c);
+    uint32_t sure, tie;
+    auto look = [&](int p) {
+      const int i = slot(c, p);
+      const bool inner = i >= lo && i < hi;
+      const uint32_t u = order_of(w[p]);
+      sure = __ballot_sync(0xffffffffu, i < n && (!inner || u > fixed));
+      tie = __ballot_sync(0xffffffffu, inner && u == fixed);
+    };
+    __syncthreads();                                      // the last use of the counts is over
+#pragma unroll
+    for (int p = 0; p < PER; ++p) {
+      if (p >= n_rows) break;
+      look(p);
+      if (lane == 0) { s_sure[p * CHOOSE_WARPS + warp] = __popc(sure); s_tie[p * CHOOSE_WARPS + warp] = __popc(tie); }
     }
-    at += (total & 0xffff) + min(total >> 16, max(equal - ties, 0));
-    ties += total >> 16;
+    __syncthreads();
+    // counts before each row's warp: in place
+    const bool has = t < n_rows * CHOOSE_WARPS;
+    int all_sure, all_ties;
+    const int vs = scan(has ? s_sure[t] : 0, s_sums[0], &all_sure), vt = scan(has ? s_tie[t] : 0, s_sums[3], &all_ties);
+    if (has) { s_sure[t] = vs; s_tie[t] = vt; }
+    __syncthreads();
+    const uint32_t below = (1u << lane) - 1;
+    auto kept_of = [&](int ties_before) { return min(ties_before, equal); };   // of the first ties_before ties
+#pragma unroll
+    for (int p = 0; p < PER; ++p) {
+      if (p >= n_rows) break;
+      look(p);                                            // (once more: 32 words of bits would not fit the registers)
+      const int tb = ties + s_tie[p * CHOOSE_WARPS + warp] + __popc(tie & below);
+      const bool on = (sure >> lane & 1u) || ((tie >> lane & 1u) && tb < equal);
+      const int place = at + s_sure[p * CHOOSE_WARPS + warp] + __popc(sure & below) + kept_of(tb) - kept_of(ties), i = slot(c, p);
+      if (on) {
+        src[place] = i;
+        out[place] = w[p];
+        if (place != i) hole = min(hole, place);
+      }
+    }
+    at += all_sure + kept_of(ties + all_ties) - kept_of(ties);
+    ties += all_ties;
   }
   hole = __reduce_min_sync(0xffffffffu, hole);
+  if (lane == 0) atomicMin(&s_hole, hole);
   __syncthreads();
-  if ((t & 31) == 0) s_sums[t >> 5] = hole;
-  __syncthreads();
-  if (t == 0) {
-    for (int w = 1; w < CHOOSE_THREADS / 32; ++w) hole = min(hole, s_sums[w]);
-    a.hole[row] = min(hole, keep);
-  }
+  if (t == 0) a.hole[row] = s_hole;
 }
 
-// Block: (sequence, layer, head), keys / values.  A step: ROWS_PER_STEP pieces of 16 bytes per thread.
+// Block: (sequence, layer, head), keys / values, and one of `parts` parts of the columns.  A step: four pieces of 16 bytes per thread.
 template <int ES>
-__global__ void __launch_bounds__(MOVE_THREADS) k_evict_move(EvictArgs a, char* pool) {
-  constexpr int PER = 4;
-  __shared__ long long s_src[2][MOVE_THREADS], s_dst[2][MOVE_THREADS];   // (at least 4 pieces per row: up to 256 rows a step)
+__global__ void __launch_bounds__(MOVE_THREADS) k_evict_move(EvictArgs a, char* pool, int log_parts) {
+  constexpr int PIECES = 4;
+  __shared__ long long s_src[2][MOVE_THREADS * PIECES / 2], s_dst[2][MOVE_THREADS * PIECES / 2];   // (two pieces per row at the least)
   pdl_enter(POSS_K_EVICT_MOVE);
-  const int t = threadIdx.x, kv = blockIdx.x & 1;
-  const int row = blockIdx.x >> 1, head = row % a.g.Hkv, lb = row / a.g.Hkv, b = lb % a.batch, layer = lb / a.batch;
+  const int t = threadIdx.x, part = blockIdx.x & ((1 << log_parts) - 1), kv = blockIdx.x >> log_parts & 1;
+  const int row = blockIdx.x >> log_parts >> 1, head = row % a.g.Hkv, lb = row / a.g.Hkv, b = lb % a.batch, layer = lb / a.batch;
   const int keep = a.out_len[b], hole = a.hole[row];
   if (hole >= keep) return;
   const long long slots = (long long)a.g.max_pages * a.g.page;
   const int32_t* src = a.src + (size_t)row * slots;
   const int32_t* table = a.g.tables + (size_t)b * a.g.max_pages;
-  const int per_row = a.g.d * ES / 16, rows = MOVE_THREADS * PER / per_row;
+  const int per_row = a.g.d * ES / 16 >> log_parts, rows = MOVE_THREADS * PIECES / per_row;   // (a power of two)
+  const int shift = __ffs(per_row) - 1;
+  pool += part * per_row * 16;
   auto where = [&](int slot) {
     const int place = slot / a.g.page;                    // (every page of the sequence was seen to be there)
     const int p = page_at(table, a.g.max_pages, a.g.n_pages, place);
     return (long long)(page_offset(a.g, layer, p < 0 ? 0 : p, kv, head) + (size_t)(slot - place * a.g.page) * a.g.d) * ES;
   };
-  int buf = 0;
-#pragma unroll 1
-  for (int r0 = hole; r0 < keep; r0 += rows, buf ^= 1) {
-    const int n = min(rows, keep - r0);
-    for (int r = t; r < n; r += MOVE_THREADS) {
+  auto look_up = [&](int r0, int buf) {
+    for (int r = t; r < min(rows, keep - r0); r += MOVE_THREADS) {
       s_src[buf][r] = where(src[r0 + r]);
       s_dst[buf][r] = where(r0 + r);
     }
-    __syncthreads();
-    uint4 x[PER];
+  };
+  int buf = 0;
+  look_up(hole, 0);
+  __syncthreads();
+#pragma unroll 1
+  for (int r0 = hole; r0 < keep; r0 += rows, buf ^= 1) {
+    const int n = min(rows, keep - r0);
+    uint4 x[PIECES];
 #pragma unroll
-    for (int j = 0; j < PER; ++j) {
-      const int i = t + j * MOVE_THREADS, r = i / per_row;
-      if (r < n) x[j] = *reinterpret_cast<const uint4*>(pool + s_src[buf][r] + (i - r * per_row) * 16);
+    for (int j = 0; j < PIECES; ++j) {
+      const int i = t + j * MOVE_THREADS, r = i >> shift;
+      if (r < n) x[j] = *reinterpret_cast<const uint4*>(pool + s_src[buf][r] + (i - (r << shift)) * 16);
     }
-    __syncthreads();                                      // the step's rows are in registers
+    if (r0 + rows < keep) look_up(r0 + rows, buf ^ 1);
+    __syncthreads();                                      // the step's rows are in registers, the next one's places known
 #pragma unroll
-    for (int j = 0; j < PER; ++j) {
-      const int i = t + j * MOVE_THREADS, r = i / per_row;
-      if (r < n) *reinterpret_cast<uint4*>(pool + s_dst[buf][r] + (i - r * per_row) * 16) = x[j];
+    for (int j = 0; j < PIECES; ++j) {
+      const int i = t + j * MOVE_THREADS, r = i >> shift;
+      if (r < n) *reinterpret_cast<uint4*>(pool + s_dst[buf][r] + (i - (r << shift)) * 16) = x[j];
     }
   }
 }
@@ -246,8 +294,12 @@ int poss_pages_evict(const poss_page_pool* pool, void* kv_pages, const int32_t* 
   a.src = reinterpret_cast<int32_t*>(reinterpret_cast<char*>(workspace) + round256(rows * 4));
   launch_pdl(L, k_evict_choose, dim3((unsigned)rows), dim3(CHOOSE_THREADS), 0, a);
   if (L.err != POSS_OK) return L.err;
-  launch_pdl(L, pool->dtype == POSS_BF16 ? k_evict_move<2> : k_evict_move<4>, dim3((unsigned)(2 * rows)), dim3(MOVE_THREADS), 0, a,
-             reinterpret_cast<char*>(kv_pages));
+  // columns are shared out while that leaves a piece or more to each and the device has room: fewer steps, one behind the other
+  int log_parts = 0;
+  const int pieces = pool->head_dim * (pool->dtype == POSS_BF16 ? 2 : 4) / 16;
+  while (log_parts < 2 && pieces >> (log_parts + 1) >= 2 && (rows << (log_parts + 2)) <= 4 * (size_t)current_sm_count()) ++log_parts;
+  launch_pdl(L, pool->dtype == POSS_BF16 ? k_evict_move<2> : k_evict_move<4>, dim3((unsigned)(rows << (1 + log_parts))),
+             dim3(MOVE_THREADS), 0, a, reinterpret_cast<char*>(kv_pages), log_parts);
   return L.err;
 }
 
