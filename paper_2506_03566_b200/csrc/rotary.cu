@@ -7,9 +7,10 @@
 // frequency are multiplied in 64 bits as turns, the whole turns are taken off (the fused multiply-add leaves the fraction exactly), and
 // only the fraction goes on in 32 bits.  What is left is the rounding of the frequency in turns, 2^-52 of the angle.
 //
-// One block per row: a thread per pair leaves cosine and sine in shared memory, then all threads stream the row's heads, two pieces
-// of 16 bytes at a time.  With halves as pairs these are the two partners, so a row may be turned in place.
-// What bounds it: memory for prompts; a chain of trips (lengths and position, table, data) for a token.
+// One block per row: all threads stream the row's heads, two pieces of 16 bytes at a time; while the first are on their way a thread per
+// pair leaves cosine and sine in shared memory.  With halves as pairs the two pieces are partners, so a row may be turned in place.
+// What bounds it: memory for prompts (8192 rows of 48 heads in bf16, 201 MB: 37.8 us, 5.3 TB/s); a chain of trips (lengths and position,
+// table, data) for a token: 3.1 us.
 #include "paged.cuh"
 #include <math.h>
 
@@ -27,13 +28,15 @@ struct Turn {
   int interleaved;           // pairs are neighbours; else element i and half + i
   float magnitude;
 };
-// heads of one row in global memory: source, target, head's stride in the target (bytes)
-struct Heads {
+// The heads of a row in global memory: those that turn from two places (queries and keys), then those that do not (values).  Sources are
+// contiguous, targets dst_step bytes apart per head.
+struct Group {
   const char* src;
   char* dst;
   size_t dst_step;
   int n;
 };
+struct Row { Group g[3]; };
 
 __device__ __forceinline__ void angles(const Turn& turn, int position, float2* cs) {
   for (int i = threadIdx.x; i < turn.half; i += THREADS) {
@@ -77,33 +80,50 @@ template <> struct Piece<bf16> {
   }
 };
 
-// The row's heads, two pieces of 16 bytes per thread and step.  Pieces a and b of a head: with halves as pairs a and its partner while
-// there are pairs; behind them, and with neighbours as pairs from the start, consecutive ones.  UNTURNED: values, copied.
-template <typename T, bool UNTURNED>
-__device__ __forceinline__ void stream_heads(const Heads& h, const Turn& turn, int d, const float2* cs) {
+// The row's heads, two pieces of 16 bytes per task, BATCH tasks per thread at a time: the first ones' loads go out before the angles are
+// worked out.  Pieces a and b of a head: with halves as pairs a and its partner while there are pairs; behind them, and with neighbours as
+// pairs from the start, consecutive ones.
+// BATCH 3 hides a row's latency and takes 104 registers; with BATCH 1 twelve blocks fit an SM, which hide it in one another.  One token of 48
+// heads 3.1 us (with BATCH 1 3.5), 976 rows 5.6 (9.0), 8192 rows 51 (37.8).
+template <typename T, int BATCH>
+__device__ __forceinline__ void stream_row(const Row& row, const Turn& turn, int position, int d, float2* cs) {
   constexpr int N = Piece<T>::N;
-  const int pieces = d / N, steps = (pieces + 1) / 2, paired = UNTURNED || turn.interleaved ? 0 : turn.half / N;
-  for (int i0 = threadIdx.x; i0 < h.n * steps; i0 += 2 * THREADS) {
-    uint4 x[2][2];
-    int a[2], b[2], head[2];
+  const int pieces = d / N, steps = (pieces + 1) / 2, paired = turn.interleaved ? 0 : turn.half / N;
+  const int turning = row.g[0].n + row.g[1].n, tasks = (turning + row.g[2].n) * steps;
+  for (int i0 = threadIdx.x;; i0 += BATCH * THREADS) {
+    uint4 x[BATCH][2];
+    uint4* to[BATCH];
+    int a[BATCH], b[BATCH];                               // b < 0: a head's last, odd piece; a < 0: nothing
+    bool turns[BATCH];
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
+    for (int k = 0; k < BATCH; ++k) {
       const int i = i0 + k * THREADS;
       a[k] = b[k] = -1;
-      if (i < h.n * steps) {
-        head[k] = i / steps;
-        const int j = i - head[k] * steps;
-        a[k] = j < paired ? j : 2 * j;
-        b[k] = j < paired ? j + paired : 2 * j + 1 < pieces ? 2 * j + 1 : -1;
-        const uint4* src = reinterpret_cast<const uint4*>(h.src) + (size_t)head[k] * pieces;
-        x[k][0] = src[a[k]];
-        if (b[k] >= 0) x[k][1] = src[b[k]];
+      turns[k] = false;
+      if (i < tasks) {
+        int head = i / steps;
+        const int j = i - head * steps;
+        turns[k] = head < turning;
+        const bool first = head < row.g[0].n;
+        head -= first ? 0 : turns[k] ? row.g[0].n : turning;
+        const bool pair = turns[k] && j < paired;
+        a[k] = pair ? j : 2 * j;
+        b[k] = pair ? j + paired : 2 * j + 1 < pieces ? 2 * j + 1 : -1;
+        const uint4* from = reinterpret_cast<const uint4*>(first ? row.g[0].src : turns[k] ? row.g[1].src : row.g[2].src) + (size_t)head * pieces;
+        to[k] = reinterpret_cast<uint4*>((first ? row.g[0].dst : turns[k] ? row.g[1].dst : row.g[2].dst) +
+                                         head * (first ? row.g[0].dst_step : turns[k] ? row.g[1].dst_step : row.g[2].dst_step));
+        x[k][0] = from[a[k]];
+        if (b[k] >= 0) x[k][1] = from[b[k]];
       }
     }
+    if (i0 == (int)threadIdx.x) {                         // (every thread comes here once)
+      angles(turn, position, cs);
+      __syncthreads();
+    }
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
+    for (int k = 0; k < BATCH; ++k) {
       if (a[k] < 0) continue;
-      if (!UNTURNED) {
+      if (turns[k]) {
         float u[N], v[N];
         Piece<T>::get(x[k][0], u);
         Piece<T>::get(x[k][1], v);
@@ -115,54 +135,60 @@ __device__ __forceinline__ void stream_heads(const Heads& h, const Turn& turn, i
             if (pb < turn.half) { const float2 y = turned(v[e], v[e + 1], cs[pb]); v[e] = y.x; v[e + 1] = y.y; }
           }
         } else if (a[k] < paired) {
+          // (two pairs' angles per access: a warp's lanes lie 64 bytes apart in bf16, four to a bank)
+          const float4* const c = reinterpret_cast<const float4*>(cs + a[k] * N);
 #pragma unroll
-          for (int e = 0; e < N; ++e) {
-            const float2 y = turned(u[e], v[e], cs[a[k] * N + e]);
-            u[e] = y.x;
-            v[e] = y.y;
+          for (int e = 0; e < N; e += 2) {
+            const float4 f = c[e / 2];
+            const float2 y = turned(u[e], v[e], make_float2(f.x, f.y)), z = turned(u[e + 1], v[e + 1], make_float2(f.z, f.w));
+            u[e] = y.x; v[e] = y.y;
+            u[e + 1] = z.x; v[e + 1] = z.y;
           }
         }
         x[k][0] = Piece<T>::put(u);
         x[k][1] = Piece<T>::put(v);
       }
-      uint4* dst = reinterpret_cast<uint4*>(h.dst + head[k] * h.dst_step);
-      dst[a[k]] = x[k][0];
-      if (b[k] >= 0) dst[b[k]] = x[k][1];
+      to[k][a[k]] = x[k][0];
+      if (b[k] >= 0) to[k][b[k]] = x[k][1];
     }
+    if (i0 - (int)threadIdx.x + BATCH * THREADS >= tasks) break;         // (the same for all)
   }
 }
 // halves as pairs whose partners do not lie whole pieces apart: one pair, or one element that stays, per thread
 template <typename T>
-__device__ __forceinline__ void stream_elements(const Heads& h, const Turn& turn, int d, const float2* cs) {
-  const int steps = d - turn.half;
-  for (int i = threadIdx.x; i < h.n * steps; i += THREADS) {
-    const int head = i / steps, j = i - head * steps;
-    const T* src = reinterpret_cast<const T*>(h.src) + (size_t)head * d;
-    T* dst = reinterpret_cast<T*>(h.dst + head * h.dst_step);
-    if (j < turn.half) {
-      const float2 y = turned(to_f(src[j]), to_f(src[j + turn.half]), cs[j]);
-      dst[j] = from_f<T>(y.x);
-      dst[j + turn.half] = from_f<T>(y.y);
-    } else {
-      dst[j + turn.half] = src[j + turn.half];
+__device__ __forceinline__ void stream_elements(const Row& row, const Turn& turn, int position, int d, float2* cs) {
+  angles(turn, position, cs);
+  __syncthreads();
+  for (int g = 0; g < 3; ++g) {
+    const int half = g < 2 ? turn.half : 0, steps = d - half;
+    for (int i = threadIdx.x; i < row.g[g].n * steps; i += THREADS) {
+      const int head = i / steps, j = i - head * steps;
+      const T* src = reinterpret_cast<const T*>(row.g[g].src) + (size_t)head * d;
+      T* dst = reinterpret_cast<T*>(row.g[g].dst + head * row.g[g].dst_step);
+      if (j < half) {
+        const float2 y = turned(to_f(src[j]), to_f(src[j + half]), cs[j]);
+        dst[j] = from_f<T>(y.x);
+        dst[j + half] = from_f<T>(y.y);
+      } else {
+        dst[j + half] = src[j + half];
+      }
     }
   }
 }
-template <typename T>
-__device__ __forceinline__ void turn_heads(const Heads& h, const Turn& turn, int d, const float2* cs) {
-  if (turn.interleaved || turn.half % Piece<T>::N == 0) stream_heads<T, false>(h, turn, d, cs);
-  else stream_elements<T>(h, turn, d, cs);
+template <typename T, int BATCH>
+__device__ __forceinline__ void turn_row(const Row& row, const Turn& turn, int position, int d, float2* cs) {
+  if (turn.interleaved || turn.half % Piece<T>::N == 0) stream_row<T, BATCH>(row, turn, position, d, cs);
+  else stream_elements<T>(row, turn, position, d, cs);
 }
 
-template <typename T>
-__global__ void __launch_bounds__(THREADS) k_rotary(Turn turn, int heads, int d, const char* x, long long ld, char* out,
+template <typename T, int BATCH>
+__global__ void __launch_bounds__(THREADS, BATCH == 1 ? 12 : 1) k_rotary(Turn turn, int heads, int d, const char* x, long long ld, char* out,
                                                     long long ld_out, const int32_t* positions) {
-  __shared__ float2 cs[MAX_HALF];
+  __shared__ __align__(16) float2 cs[MAX_HALF];
   pdl_enter(POSS_K_ROTARY);
   const size_t row = blockIdx.x;
-  angles(turn, positions[row], cs);
-  __syncthreads();
-  turn_heads<T>({x + row * ld, out + row * ld_out, (size_t)d * sizeof(T), heads}, turn, d, cs);
+  const Row r = {{{x + row * ld, out + row * ld_out, (size_t)d * sizeof(T), heads}, {nullptr, nullptr, 0, 0}, {nullptr, nullptr, 0, 0}}};
+  turn_row<T, BATCH>(r, turn, positions[row], d, cs);
 }
 
 struct AppendArgs {
@@ -175,9 +201,9 @@ struct AppendArgs {
   const int32_t *prefix_len, *n_rows, *positions;
   int32_t* status;
 };
-template <typename T>
-__global__ void __launch_bounds__(THREADS) k_append_rotary(AppendArgs a, Turn turn) {
-  __shared__ float2 cs[MAX_HALF];
+template <typename T, int BATCH>
+__global__ void __launch_bounds__(THREADS, BATCH == 1 ? 12 : 1) k_append_rotary(AppendArgs a, Turn turn) {
+  __shared__ __align__(16) float2 cs[MAX_HALF];
   pdl_enter(POSS_K_APPEND_ROTARY);
   const size_t row = blockIdx.x;
   const int b = blockIdx.x / a.rows, r = blockIdx.x - b * a.rows;
@@ -189,18 +215,17 @@ __global__ void __launch_bounds__(THREADS) k_append_rotary(AppendArgs a, Turn tu
   const int slot = s.prefix + r, place = slot / a.g.page;
   if (!a.positions) position = slot;
   const int p = page_at(a.g.tables + (size_t)b * a.g.max_pages, a.g.max_pages, a.g.n_pages, place);
-  angles(turn, position, cs);
-  __syncthreads();
-  if (a.Hq) turn_heads<T>({a.q + row * a.ld_q, a.out_q + row * a.ld_out_q, (size_t)a.g.d * sizeof(T), a.Hq}, turn, a.g.d, cs);
-  if (p < 0) {
-    if (threadIdx.x == 0) raise_status(a.status, POSS_E_INVALID);
-    return;
-  }
+  if (p < 0 && threadIdx.x == 0) raise_status(a.status, POSS_E_INVALID);
   const size_t head_bytes = (size_t)a.g.page * a.g.d * sizeof(T);
-  char* const dk = a.pool + (page_offset(a.g, a.layer, p, 0, 0) + (size_t)(slot - place * a.g.page) * a.g.d) * sizeof(T);
-  turn_heads<T>({a.k + row * a.ld_kv, dk, head_bytes, a.g.Hkv}, turn, a.g.d, cs);
-  stream_heads<T, true>({a.v + row * a.ld_kv, dk + a.g.Hkv * head_bytes, head_bytes, a.g.Hkv}, turn, a.g.d, cs);
+  char* const dk = a.pool + (page_offset(a.g, a.layer, p < 0 ? 0 : p, 0, 0) + (size_t)(slot - place * a.g.page) * a.g.d) * sizeof(T);
+  const int kv = p < 0 ? 0 : a.g.Hkv;                     // (without a page the queries alone)
+  const Row t = {{{a.q + row * a.ld_q, a.out_q + row * a.ld_out_q, (size_t)a.g.d * sizeof(T), a.Hq},
+                  {a.k + row * a.ld_kv, dk, head_bytes, kv},
+                  {a.v + row * a.ld_kv, dk + a.g.Hkv * head_bytes, head_bytes, kv}}};
+  turn_row<T, BATCH>(t, turn, position, a.g.d, cs);
 }
+
+bool many_rows(int64_t n) { return n > 10 * current_sm_count(); }
 
 int turn_check(int head_dim, int rot_dim, float magnitude, const double* freq) {
   if (rot_dim < 2 || rot_dim % 2 || rot_dim > head_dim || !isfinite(magnitude) || !freq) return POSS_E_INVALID;
@@ -268,7 +293,8 @@ int poss_rotary(const void* x, int64_t ld_x, void* out, int64_t ld_out, int dtyp
   int64_t launches = 0;
   Launcher L{reinterpret_cast<cudaStream_t>(stream), &launches, POSS_OK};
   const Turn turn = {freq, rot_dim / 2, interleaved != 0, magnitude};
-  launch_pdl(L, dtype == POSS_BF16 ? k_rotary<bf16> : k_rotary<float>, dim3((unsigned)n), dim3(THREADS), 0, turn, heads, head_dim,
+  const bool many = many_rows(n);
+  launch_pdl(L, dtype == POSS_BF16 ? (many ? k_rotary<bf16, 1> : k_rotary<bf16, 3>) : many ? k_rotary<float, 1> : k_rotary<float, 3>, dim3((unsigned)n), dim3(THREADS), 0, turn, heads, head_dim,
              reinterpret_cast<const char*>(x), ld_x * es, reinterpret_cast<char*>(out), ld_out * es, positions);
   return L.err;
 }
@@ -313,7 +339,9 @@ int poss_pages_append_rotary(const poss_page_pool* pool, int layer, void* kv_pag
   a.ld_kv = ld_kv * es; a.ld_q = ld_q * es; a.ld_out_q = ld_out_q * es;
   a.prefix_len = prefix_len; a.n_rows = n_rows; a.positions = positions; a.status = status;
   const Turn turn = {freq, rot_dim / 2, interleaved != 0, magnitude};
-  launch_pdl(L, pool->dtype == POSS_BF16 ? k_append_rotary<bf16> : k_append_rotary<float>, dim3((unsigned)(batch * rows)),
+  const bool many = many_rows((int64_t)batch * rows);
+  launch_pdl(L, pool->dtype == POSS_BF16 ? (many ? k_append_rotary<bf16, 1> : k_append_rotary<bf16, 3>)
+                                         : many ? k_append_rotary<float, 1> : k_append_rotary<float, 3>, dim3((unsigned)(batch * rows)),
              dim3(THREADS), 0, a, turn);
   return L.err;
 }
