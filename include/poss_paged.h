@@ -127,8 +127,9 @@ POSS_API int poss_paged_tree_attention(const poss_page_pool* pool, int layer, co
  * (The rows' slots are new: what mass held there is of no account.)  All other entries, and those of a sequence without rows, are left
  * as they were; an unseen slot draws nothing, a missing page's slots neither.  row_weights float[batch][rows] (NULL: 1 each), such as a
  * tree's draft probabilities; those behind n_rows are not read.  Terms are added in fp32, in one order: equal calls give equal bits.
- * 2^x is off by 2^-22, the maxima and sums are the attention's own.  mass must not overlap q, out or row_weights.  Scratch: its own
- * size (below).  All else, errors too, as poss_paged_tree_attention. */
+ * 2^x is off by 2^-22, the maxima and sums are the attention's own.  mass must not overlap q, out or row_weights.  Scratch: calls of few
+ * rows keep their scores there (4 bytes per row, query head and slot that max_pages has room for), so that one made for several shapes
+ * takes the greatest of their sizes, which need not be that of the most rows.  All else, errors too, as poss_paged_tree_attention. */
 POSS_API size_t poss_paged_attention_mass_workspace_bytes(const poss_page_pool* pool, int batch, int rows, int n_q_heads,
                                                  int max_pages);
 POSS_API int poss_paged_tree_attention_mass(const poss_page_pool* pool, int layer, const void* kv_pages, float* mass,

@@ -40,6 +40,7 @@ void launch_paged_attn_tc(Launcher& L, const PagedAttnArgs& a, const void* pool,
 // Tensor maps of the tcgen05 kernels.  The layer as a matrix of slots: rows (page, keys / values, head, slot), head_dim columns, a box of
 // `slots` rows times 64 columns; rows_total is the first row behind it.  The queries: columns, heads of a group, groups (KV heads), tree
 // rows, sequences, a box of `tree_rows` tree rows of one KV head times 64 columns; rows behind the call's last one arrive as zeros.
+bool paged_take_lost_load();             // whether this launch is to lose a load (poss_debug_paged_lose_load); counts it
 bool paged_kv_map(CUtensorMap* map, const PagedAttnArgs& a, const void* layer, int slots);
 bool paged_q_map(CUtensorMap* map, const PagedAttnArgs& a, int tree_rows);
 

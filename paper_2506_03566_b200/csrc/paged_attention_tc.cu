@@ -1120,6 +1120,11 @@ EncodeTiledFn encode_fn() {
 }
 }  // namespace
 
+bool paged_take_lost_load() {
+  int lost = g_lost_loads.load();
+  while (lost > 0 && !g_lost_loads.compare_exchange_weak(lost, lost - 1)) {}
+  return lost > 0;
+}
 bool paged_kv_map(CUtensorMap* map, const PagedAttnArgs& a, const void* layer, int slots) {
   const EncodeTiledFn encode = encode_fn();
   const cuuint64_t dim[2] = {(cuuint64_t)a.g.d, (cuuint64_t)a.g.n_pages * 2 * a.g.Hkv * a.g.page};
@@ -1181,9 +1186,7 @@ void launch_paged_attn_tc(Launcher& L, const PagedAttnArgs& a, const void* pool,
   k.slot_rows = QR / a.G;
   k.row_cap = row_cap_of(a.rows, a.G);
   k.rows_total = a.g.n_pages * 2 * a.g.Hkv * a.g.page;
-  int lost = g_lost_loads.load();
-  while (lost > 0 && !g_lost_loads.compare_exchange_weak(lost, lost - 1)) {}
-  k.inject_lost_load = lost > 0;
+  k.inject_lost_load = paged_take_lost_load();
   CUtensorMap map, map_q;
   if (!paged_kv_map(&map, a, k.layer, a.g.page < KT ? a.g.page : KT) || !paged_q_map(&map_q, a, k.slot_rows)) {
     L.err = POSS_E_CUDA;

@@ -62,6 +62,7 @@ struct Args {
   int pass_rows;                        // tree rows per pass
   int rows_total;                       // rows of the pool's layer: the first coordinate behind it
   int page_shift;
+  int inject_lost_load;
 };
 __device__ __forceinline__ Work work_of(const PagedAttnArgs& a, int b) {
   const SeqLen n = seq_len_of(a.prefix_len[b], a.n_rows ? a.n_rows[b] : a.rows, a.rows, (long long)a.g.max_pages * a.g.page);
@@ -419,7 +420,7 @@ __global__ void __launch_bounds__(N_THREADS, 1) k_slot_mass_tc(const __grid_cons
           if (ok && lane == 0) {
             mbar_expect_tx(bar(c.q_full), k.pass_rows * a.G * HD * 2);
 #pragma unroll
-            for (int cb = 0; cb < Z::CB; ++cb) tma_load_5d(base + cb * Q_BLOCK, &map_q, bar(c.q_full), cb * 64, p.head, r0, p.b);
+            for (int cb = k.inject_lost_load ? Z::CB : 0; cb < Z::CB; ++cb) tma_load_5d(base + cb * Q_BLOCK, &map_q, bar(c.q_full), cb * 64, p.head, r0, p.b);
           }
           queries += ok;
           __syncwarp();
@@ -501,6 +502,7 @@ void launch_paged_mass_tc(Launcher& L, const PagedMassArgs& s, const void* pool)
   k.pass_rows = MAX_LINES / a.G < a.rows ? MAX_LINES / a.G : a.rows;
   k.rows_total = a.g.n_pages * 2 * a.g.Hkv * a.g.page;
   while (1 << k.page_shift < a.g.page) ++k.page_shift;
+  k.inject_lost_load = paged_take_lost_load();
   const bf16* layer = reinterpret_cast<const bf16*>(pool) + page_offset(a.g, a.layer, 0, 0, 0);
   CUtensorMap map, map_q;
   if (!paged_kv_map(&map, a, layer, a.g.page < KT ? a.g.page : KT) || !paged_q_map(&map_q, a, k.pass_rows)) {

@@ -147,6 +147,7 @@ def evict(pages, mass, out_mass, tables, lens, keep, first, recent):
 def scores(logits, tokens, token_rows, topk, temperature):
     """float64 logits [rows][vocab] on the CPU.  Returns a dict of (value, tolerance) or whole numbers."""
     rows, v = logits.shape
+    temperature = float(np.float32(temperature))                      # (the call takes it in 32 bits: 0.2 is 1.5e-8 of itself off)
     x = torch.where(logits.abs() < math.inf, logits, torch.tensor(-math.inf, dtype=torch.float64))
     lse, ent = torch.full((rows,), -math.inf, dtype=torch.float64), torch.zeros(rows, dtype=torch.float64)
     r, b = torch.zeros(rows, dtype=torch.float64), torch.zeros(rows, dtype=torch.float64)

@@ -156,7 +156,7 @@ def test_plain_forms_agree():
         assert list(got) == sorted(always + rest)
     x = torch.randn(3, 50, dtype=torch.float64)
     w = lu.scores(x, [1, 2, 3], None, 4, 0.7)
-    ref = torch.log_softmax(x / 0.7, -1)
+    ref = torch.log_softmax(x / float(np.float32(0.7)), -1)
     assert torch.allclose(w["logp"][0], ref[[0, 1, 2], [1, 2, 3]], rtol=1e-12)
     assert torch.allclose(w["entropy"][0], -(ref.exp() * ref).sum(-1), rtol=1e-12)
     assert torch.equal(w["top_tokens"].long(), torch.topk(x, 4).indices)
