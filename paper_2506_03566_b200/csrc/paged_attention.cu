@@ -23,6 +23,8 @@ struct SimtArgs {
   int q_tiles, ns;
   float scale_log2;
   float* part;      // [batch][Hkv][q_tiles][ns][QB][d + 2]: maximum, sum, outputs
+  float* scores;    // NULL, or [batch][Hkv][rows * G][scores_ld]
+  long long scores_ld;
 };
 
 template <typename T> __device__ __forceinline__ float4 load4(const T* p);
@@ -158,6 +160,11 @@ __global__ void __launch_bounds__(128) k_paged_attn(SimtArgs s, const T* pool) {
       for (int j = 0; j < 4; ++j) {
         x[i][j] = (seen >> (tx + 8 * j)) & 1u ? x[i][j] * s.scale_log2 : -INFINITY;
         mx = fmaxf(mx, x[i][j]);
+      }
+      if (s.scores && qt * QB + 2 * ty + i < nq) {
+        float* to = s.scores + (((size_t)b * a.g.Hkv + kvh) * a.rows * a.G + qt * QB + 2 * ty + i) * s.scores_ld + key0 + tx;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) to[8 * j] = x[i][j];
       }
 #pragma unroll
       for (int d = 4; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
@@ -322,9 +329,14 @@ struct MassTarget {
   const float* weights;     // NULL, or [batch][rows]
 };
 size_t ml_bytes(int batch, int rows, int Hq) { return ((size_t)batch * rows * Hq * sizeof(float2) + 255) / 256 * 256; }
+constexpr size_t MAX_SCORES = (size_t)1 << 29;            // a table with room for far more slots than that reads the keys again
+// Off the tensor cores scores are always cheaper to keep than to form again (3 trees of 15 rows over up to 517 slots in fp32: 24.6 us with the
+// keys read again, 16.4 so; 4 of 100 rows over 1500: 90 and 63), as long as there is room.
 size_t scores_bytes(const poss_page_pool* pool, int batch, int rows, int Hq, int max_pages) {
-  if (!paged_attn_tc_supported(*pool, Hq / pool->n_kv_heads, 1.f)) return 0;
-  return (paged_attn_tc_scores(*pool, batch, rows, Hq, max_pages) + 255) / 256 * 256;
+  const bool tc = paged_attn_tc_supported(*pool, Hq / pool->n_kv_heads, 1.f);
+  size_t n = (size_t)batch * rows * Hq * paged_simt_scores_ld(max_pages, pool->page_slots) * 4;
+  if (tc) n = paged_attn_tc_scores(*pool, batch, rows, Hq, max_pages);
+  return n > MAX_SCORES ? 0 : (n + 255) / 256 * 256;
 }
 
 // both entries; mass NULL: the attention alone
@@ -381,15 +393,14 @@ int attend(const poss_page_pool* pool, int layer, const void* kv_pages, const in
   m.weights = mass->weights;
   m.scale_log2 = scale * 1.4426950408889634f;
   m.scores = nullptr;
-  if (tc && scores_bytes(pool, batch, rows, n_q_heads, max_pages)) {
-    m.scores = reinterpret_cast<float*>(reinterpret_cast<char*>(a.ml) + ml_bytes(batch, rows, n_q_heads));
-    launch_paged_attn_tc(L, a, kv_pages, *pool, &m);
-    return L.err;
-  }
-  if (tc) launch_paged_attn_tc(L, a, kv_pages, *pool);
-  else launch_paged_attn_simt(L, a, kv_pages, pool->dtype);
-  if (L.err != POSS_OK) return L.err;
+  // (a scale that keeps a shape off the tensor cores finds no room for its scores, or not enough)
+  const bool kept = scores_bytes(pool, batch, rows, n_q_heads, max_pages) && tc == paged_attn_tc_supported(*pool, a.G, 1.f);
+  if (kept) m.scores = reinterpret_cast<float*>(reinterpret_cast<char*>(a.ml) + ml_bytes(batch, rows, n_q_heads));
+  if (tc) launch_paged_attn_tc(L, a, kv_pages, *pool, kept ? &m : nullptr);
+  else launch_paged_attn_simt(L, a, kv_pages, pool->dtype, m.scores);
+  if (L.err != POSS_OK || (tc && kept)) return L.err;
   if (tc) launch_paged_mass_tc(L, m, kv_pages);
+  else if (kept) launch_paged_mass_scores(L, m);
   else launch_paged_mass_simt(L, m, kv_pages, pool->dtype);
   return L.err;
 }
@@ -401,9 +412,13 @@ size_t paged_attn_simt_workspace(int batch, int rows, int Hq, int Hkv, int d) {
   return (size_t)(SIMT_BLOCKS + (blocks < SIMT_BLOCKS ? blocks : SIMT_BLOCKS - 1)) * QB * (d + 2) * 4;
 }
 
-void launch_paged_attn_simt(Launcher& L, const PagedAttnArgs& a, const void* pool, int dtype) {
+long long paged_simt_scores_ld(int max_pages, int page) { return ((long long)max_pages * page + KB - 1) / KB * KB; }
+
+void launch_paged_attn_simt(Launcher& L, const PagedAttnArgs& a, const void* pool, int dtype, float* scores) {
   SimtArgs s;
   s.a = a;
+  s.scores = scores;
+  s.scores_ld = paged_simt_scores_ld(a.g.max_pages, a.g.page);
   s.q_tiles = (a.rows * a.G + QB - 1) / QB;
   s.ns = simt_splits((long long)a.batch * a.g.Hkv * s.q_tiles, (long long)a.g.max_pages * a.g.page);
   s.scale_log2 = a.scale * 1.4426950408889634f;

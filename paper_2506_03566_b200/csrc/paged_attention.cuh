@@ -24,7 +24,10 @@ __device__ __forceinline__ float2 paged_ml(float m, float l) {
 
 // SIMT kernel: every type, head dimension and page size
 size_t paged_attn_simt_workspace(int batch, int rows, int Hq, int Hkv, int d);
-void launch_paged_attn_simt(Launcher& L, const PagedAttnArgs& a, const void* pool, int dtype);
+// scores: NULL, or where the rows leave theirs (times scale times log2 e, -inf where a slot is not seen) for the slots' weights,
+// [batch][Hkv][rows * G][paged_simt_scores_ld]
+long long paged_simt_scores_ld(int max_pages, int page);
+void launch_paged_attn_simt(Launcher& L, const PagedAttnArgs& a, const void* pool, int dtype, float* scores = nullptr);
 
 // tcgen05 kernel: bf16, head dimension 64 or 128, pages of 16 .. 256 slots (powers of two), at most 128 query heads per KV head,
 // scale > 0
@@ -55,6 +58,8 @@ struct PagedMassArgs {
 };
 // tcgen05 kernel: the shapes of the attention's
 void launch_paged_mass_tc(Launcher& L, const PagedMassArgs& s, const void* pool);
+// from the scores that the SIMT attention has left
+void launch_paged_mass_scores(Launcher& L, const PagedMassArgs& s);
 // SIMT kernel: every type and shape
 void launch_paged_mass_simt(Launcher& L, const PagedMassArgs& s, const void* pool, int dtype);
 

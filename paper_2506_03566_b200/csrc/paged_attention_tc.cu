@@ -1156,12 +1156,11 @@ bool paged_attn_tc_supported(const poss_page_pool& p, int G, float scale) {
 // Scores go through memory (4 bytes to and fro per line and slot) where that is no more than reading the keys again (2 bytes per element) to
 // form them anew.  16 trees of 4 heads over up to 8191 slots, attention and weights: 1 row 106 us (keys again: 144), 4 rows 114 (150), 8 rows
 // 141 (147), 9 rows, just above, 148; 64 single tokens over up to 8000: 306 (413).
-constexpr size_t MAX_SCORES = (size_t)1 << 29;            // a table with room for far more slots than that reads keys again
 size_t paged_attn_tc_scores(const poss_page_pool& p, int batch, int rows, int Hq, int max_pages) {
   const int lines = rows * (Hq / p.n_kv_heads);
   if (lines > p.head_dim / 4) return 0;
-  const size_t ld = ((size_t)max_pages * p.page_slots + KT - 1) / KT * KT, n = (size_t)batch * p.n_kv_heads * lines * ld * 4;
-  return n <= MAX_SCORES ? n : 0;
+  const size_t ld = ((size_t)max_pages * p.page_slots + KT - 1) / KT * KT;
+  return (size_t)batch * p.n_kv_heads * lines * ld * 4;
 }
 
 size_t paged_attn_tc_workspace(const poss_page_pool& p, int batch, int rows, int Hq, int max_pages) {

@@ -22,9 +22,10 @@ template <> __device__ __forceinline__ float4 load4<bf16>(const bf16* p) {
   return make_float4(lo.x, lo.y, hi.x, hi.y);
 }
 
-// SIMT kernel, every type and shape: a block owns 32 slots of one (sequence, KV head), keeps their keys in shared memory and walks the
+// SIMT kernel, every type and shape, where scores were not kept (a scale of 0 or below on a shape of the tensor cores, a table with room for
+// too many slots): a block owns 32 slots of one (sequence, KV head), keeps their keys in shared memory and walks the
 // query rows (row * G + head) 32 at a time; a thread forms 2 rows x 4 slots of the scores, a thread per slot adds the rows' weights up.
-// Bound by fp32 multiply-adds and the shared-memory reads that feed them: meant for the fp32 check mode and odd shapes.
+// Bound by fp32 multiply-adds and the shared-memory reads that feed them.
 template <typename T, int D>
 __global__ void __launch_bounds__(128) k_slot_mass(PagedMassArgs s, const T* pool) {
   constexpr int LD = D + 4;                               // rows of 8 consecutive keys fall into different banks
@@ -128,6 +129,41 @@ __global__ void __launch_bounds__(128) k_slot_mass(PagedMassArgs s, const T* poo
   }
 }
 
+// From the scores that the attention has left: a block owns 32 slots of one (sequence, KV head), a warp takes every eighth line, a lane a slot;
+// the warps' sums meet in shared memory.  Bound by the read of the scores, and for few rows by a chain of trips.
+constexpr int WARPS = 8;
+__global__ void __launch_bounds__(32 * WARPS) k_slot_mass_scores(PagedMassArgs s, long long ld) {
+  __shared__ float part[WARPS][32];
+  pdl_enter(POSS_K_SLOT_MASS);
+  const PagedAttnArgs& a = s.a;
+  const int b = blockIdx.z, kvh = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const SeqLen n = seq_len_of(a.prefix_len[b], a.n_rows ? a.n_rows[b] : a.rows, a.rows, (long long)a.g.max_pages * a.g.page);
+  const int total = n.prefix + n.rows, lines = n.rows * a.G;
+  if (lines == 0) return;                                 // (without rows nothing is added)
+  const float* const scores = s.scores + ((size_t)b * a.g.Hkv + kvh) * a.rows * a.G * ld;
+  float* const mass = s.mass + ((size_t)b * a.g.Hkv + kvh) * s.mass_slots;
+  for (int key0 = blockIdx.x * 32; key0 < total; key0 += gridDim.x * 32) {
+    const int key = key0 + lane;                          // (scores have room for whole tiles of 32 slots)
+    const float old = warp == 0 && key < n.prefix ? mass[key] : 0.f;
+    float sum = 0.f;
+#pragma unroll 4
+    for (int i = warp; i < lines; i += WARPS) {
+      const size_t row = (size_t)b * a.rows + i / a.G;
+      const float2 ml = a.ml[row * a.Hq + kvh * a.G + i % a.G];
+      const float w = s.weights ? s.weights[row] * ml.y : ml.y, x = __ldcg(scores + i * ld + key);
+      sum += x == -INFINITY ? 0.f : exp2f(x - ml.x) * w;  // (unseen: nothing, even where the row's sum is NaN)
+    }
+    part[warp][lane] = sum;
+    __syncthreads();
+    if (warp == 0 && key < total) {
+#pragma unroll
+      for (int i = 1; i < WARPS; ++i) sum += part[i][lane];
+      mass[key] = old + sum;
+    }
+    __syncthreads();
+  }
+}
+
 template <typename T, int D> void launch_simt(Launcher& L, const PagedMassArgs& s, const void* pool) {
   const long long slots = (long long)s.a.g.max_pages * s.a.g.page;
   launch_pdl(L, k_slot_mass<T, D>, dim3((unsigned)((slots + KB - 1) / KB), s.a.g.Hkv, s.a.batch), dim3(128), 0, s,
@@ -135,6 +171,13 @@ template <typename T, int D> void launch_simt(Launcher& L, const PagedMassArgs& 
 }
 
 }  // namespace
+
+void launch_paged_mass_scores(Launcher& L, const PagedMassArgs& s) {
+  // some sixteen blocks per SM in all, each with 32 slots at least
+  const long long items = (long long)s.a.batch * s.a.g.Hkv, ld = paged_simt_scores_ld(s.a.g.max_pages, s.a.g.page);
+  const long long n = (16 * current_sm_count() + items - 1) / items, most = ld / 32;
+  launch_pdl(L, k_slot_mass_scores, dim3((unsigned)(n < most ? n : most), s.a.g.Hkv, s.a.batch), dim3(32 * WARPS), 0, s, ld);
+}
 
 void launch_paged_mass_simt(Launcher& L, const PagedMassArgs& s, const void* pool, int dtype) {
   const bool h = dtype == POSS_BF16;
