@@ -62,6 +62,21 @@ def test_a_table_with_room_for_far_more_slots():
     assert not mass[0, 0, :, 701:].any()
 
 
+@pytest.mark.parametrize("dtype,d", [(F32, 32), (F32, 128), (BF, 32)])
+def test_a_table_with_room_for_far_more_slots_off_the_tensor_cores(dtype, d):
+    c = Case(96, dtype, 32, 8, d, 1024, [50], 128, [90], extra_places=40)
+    assert c.tables.shape[1] * 1024 * 32 * 128 * 4 > 2 ** 29
+    mass, w = mass_case(c, 5)
+    got = mass.cuda()
+    run_mass(c, got, w)
+    check_mass(c, got, mass, w)
+    c.tables = c.tables[:, :2].copy()                                 # and one without: the attention's own scores
+    mass = mass[..., :2048].contiguous()
+    got = mass.cuda()
+    run_mass(c, got, w)
+    check_mass(c, got, mass, w)
+
+
 def test_lost_loads_run_out_and_the_context_lives_on():
     c = Case(97, BF, 8, 2, 128, 16, [300, 5], 40)
     mass, w = mass_case(c, 4)
