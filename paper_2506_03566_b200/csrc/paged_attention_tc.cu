@@ -914,52 +914,23 @@ __global__ void __launch_bounds__(N_THREADS, 1) k_paged_attn_tc(const __grid_con
 
 // ---------------------------------------------------------------------------------------------------- merge
 // A block: 32 query rows of one item, eight threads per row.  The item's segments lie in consecutive CTAs, in key order.
-// SCORES: the blocks behind them are dealt the slots of the item, 1024 at a time, and add their weights up from the scores: in the same
-// launch, so that a token's call has no third one.  The lines' maxima and sums come from the parts once more.
-template <int HD>
-__device__ __forceinline__ void add_weights(const TcArgs& k, const SeqWork& s, int b, int head, uint32_t total, uint32_t before, int whole,
-                                            int cut_grid, float2 (*s_ml)[32]) {
+// SCORES: the slots' weights, from the scores that the attention has left.  A block is dealt 1024 slots of an item at a time; own: a thread's
+// line's maximum and the inverse of its sum, for the first threads.  Where the blocks of merge and weights are few they share a launch (1 token
+// over 1024 slots 18.2 us, with a launch more 21.6; 16 tokens 31.8 and 33.8) and the lines' sums come from the parts once more; else the
+// weights are a launch of their own, whose blocks need a third of the merge's registers (16 tokens over up to 8191 slots 101 us, in one launch
+// 106).
+struct Lines { float2 ml[32]; };             // by line: maximum, and the inverse of the sum times the row's weight
+__device__ __forceinline__ void add_weights(const TcArgs& k, const SeqWork& s, int b, int head, float2 own, int first_key, int step, Lines& sh) {
   const PagedAttnArgs& a = k.a;
   const int t = threadIdx.x, lines = s.rows * a.G;
-  int first = 0, last = 0, which = 0;
-  if (!whole) {
-    const Cut cut(total, cut_grid);
-    const uint32_t u0 = before + (uint32_t)head * s.tiles;
-    first = cut.cta_of(u0);
-    last = cut.cta_of(u0 + s.tiles - 1);
-    which = cut.begin(first) < u0 ? 1 : 0;
+  if (t < 32) {
+    if (k.row_weights && t < lines) own.y *= k.row_weights[(size_t)b * a.rows + t / a.G];
+    sh.ml[t] = own;
   }
-  const bool parts = first != last;
-  if (parts) {
-    for (int i = t >> 5; i <= last - first; i += 8)
-      if ((t & 31) < lines)
-        s_ml[i][t & 31] = __ldcg(reinterpret_cast<const float2*>(partial_of(k, HD, first + i, i == 0 ? which : 0) + (size_t)k.row_cap * HD) + (t & 31));
-    __syncthreads();
-  }
-  float2 own = make_float2(INFINITY, 0.f);                // thread < 32: its line's maximum and the inverse of its sum times the row's weight
-  if (t < lines) {
-    const size_t row = (size_t)b * a.rows + t / a.G;
-    if (parts) {
-      float m = -INFINITY, l = 0.f;
-      for (int i = 0; i <= last - first; ++i) m = fmaxf(m, s_ml[i][t].x);
-      for (int i = 0; i <= last - first; ++i) {           // (as the merge does)
-        const float2 x = s_ml[i][t];
-        const float c = x.x == -INFINITY ? (x.y == 0.f ? 0.f : 1.f) : ex2(x.x - m);
-        if (c != 0.f) l = fmaf(x.y, c, l);
-      }
-      own = paged_ml(m, l);
-    } else {
-      own = __ldcg(a.ml + row * a.Hq + head * a.G + t % a.G);
-    }
-    own.y *= k.row_weights ? k.row_weights[row] : 1.f;
-  }
-  __syncthreads();
-  if (t < 32) s_ml[0][t] = own;
   __syncthreads();
   const float* const scores = k.scores + ((size_t)b * a.g.Hkv + head) * (a.rows * a.G) * k.scores_ld;
   float* const mass = k.mass + ((size_t)b * a.g.Hkv + head) * k.mass_slots;
-  const int step = (gridDim.x - k.merge_blocks) * 1024;
-  for (int key = (blockIdx.x - k.merge_blocks) * 1024 + 4 * t; key < s.total; key += step) {
+  for (int key = first_key + 4 * t; key < s.total; key += step) {
     float old[4], sum[4];
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
@@ -969,7 +940,7 @@ __device__ __forceinline__ void add_weights(const TcArgs& k, const SeqWork& s, i
 #pragma unroll 4
     for (int i = 0; i < lines; ++i) {
       const float4 y = __ldcg(reinterpret_cast<const float4*>(scores + i * k.scores_ld + key));
-      const float2 c = s_ml[0][i];
+      const float2 c = sh.ml[i];
       const float v[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
@@ -981,6 +952,45 @@ __device__ __forceinline__ void add_weights(const TcArgs& k, const SeqWork& s, i
     for (int x = 0; x < 4; ++x)
       if (key + x < s.total) mass[key + x] = old[x] + sum[x];
   }
+}
+__global__ void __launch_bounds__(256) k_paged_attn_weights(const TcArgs k) {
+  __shared__ Lines sh;
+  pdl_enter(POSS_K_SLOT_MASS);
+  const int b = blockIdx.z, head = blockIdx.y, t = threadIdx.x;
+  const SeqWork s = seq_work(k, b);
+  if (!s.rows) return;
+  float2 own = make_float2(INFINITY, 0.f);
+  if (t < s.rows * k.a.G) own = __ldcg(k.a.ml + ((size_t)b * k.a.rows + t / k.a.G) * k.a.Hq + head * k.a.G + t % k.a.G);
+  add_weights(k, s, b, head, own, blockIdx.x * 1024, gridDim.x * 1024, sh);
+}
+// in the merge's launch: the line's maximum and sum from the segments' (by thread, for those below the number of lines)
+template <int HD>
+__device__ __forceinline__ float2 line_of(const TcArgs& k, const SeqWork& s, int b, int head, uint32_t total, uint32_t before, int whole,
+                                          int cut_grid, float2 (*s_ml)[32]) {
+  const PagedAttnArgs& a = k.a;
+  const int t = threadIdx.x, lines = s.rows * a.G;
+  int first = 0, last = 0, which = 0;
+  if (!whole) {
+    const Cut cut(total, cut_grid);
+    const uint32_t u0 = before + (uint32_t)head * s.tiles;
+    first = cut.cta_of(u0);
+    last = cut.cta_of(u0 + s.tiles - 1);
+    which = cut.begin(first) < u0 ? 1 : 0;
+  }
+  if (first == last) return t < lines ? __ldcg(a.ml + ((size_t)b * a.rows + t / a.G) * a.Hq + head * a.G + t % a.G) : make_float2(INFINITY, 0.f);
+  for (int i = t >> 5; i <= last - first; i += 8)
+    if ((t & 31) < lines)
+      s_ml[i][t & 31] = __ldcg(reinterpret_cast<const float2*>(partial_of(k, HD, first + i, i == 0 ? which : 0) + (size_t)k.row_cap * HD) + (t & 31));
+  __syncthreads();
+  if (t >= lines) return make_float2(INFINITY, 0.f);
+  float m = -INFINITY, l = 0.f;
+  for (int i = 0; i <= last - first; ++i) m = fmaxf(m, s_ml[i][t].x);
+  for (int i = 0; i <= last - first; ++i) {               // (as the merge does)
+    const float2 x = s_ml[i][t];
+    const float c = x.x == -INFINITY ? (x.y == 0.f ? 0.f : 1.f) : ex2(x.x - m);
+    if (c != 0.f) l = fmaf(x.y, c, l);
+  }
+  return paged_ml(m, l);
 }
 template <int HD, bool SCORES>
 __global__ void __launch_bounds__(256) k_paged_attn_tc_merge(const TcArgs k, int max_groups) {
@@ -995,7 +1005,10 @@ __global__ void __launch_bounds__(256) k_paged_attn_tc_merge(const TcArgs k, int
   const SeqWork s = seq_work(k, b);
   if constexpr (SCORES) {
     if ((int)blockIdx.x >= k.merge_blocks) {
-      if (s.rows) add_weights<HD>(k, s, b, head, total, before, whole, cut_grid, s_ml);
+      __shared__ Lines sh;
+      if (s.rows)
+        add_weights(k, s, b, head, line_of<HD>(k, s, b, head, total, before, whole, cut_grid, s_ml), (blockIdx.x - k.merge_blocks) * 1024,
+                    (gridDim.x - k.merge_blocks) * 1024, sh);
       return;
     }
   }
@@ -1090,15 +1103,17 @@ void launch(Launcher& L, const TcArgs& k0, const CUtensorMap& map, const CUtenso
   if (ctas > MAX_CTAS) ctas = MAX_CTAS;
   k.merge_blocks = tiles > 1 ? k.row_cap / 32 : 0;        // (an item of one tile is never cut)
   launch_pdl(L, k_paged_attn_tc<HD, SCORES>, dim3(ctas), dim3(N_THREADS), smem, map, map_q, k);
-  int blocks = k.merge_blocks;
-  if (SCORES) {
-    // weights: some eight blocks per SM in all, each with 1024 slots at least
-    const long long items = (long long)a.batch * a.g.Hkv, most = (tiles * KT + 1023) / 1024;
-    const long long n = (8 * sms + items - 1) / items;
-    blocks += (int)(n < most ? n : most);
+  // weights: some sixteen blocks per SM in all, each with 1024 slots at least
+  const long long items = (long long)a.batch * a.g.Hkv, most = (tiles * KT + 1023) / 1024, n = (16 * sms + items - 1) / items;
+  const int weights = SCORES ? (int)(n < most ? n : most) : 0;
+  const bool together = (k.merge_blocks + weights) * items <= 4 * sms;   // (two waves of blocks, two per SM)
+  const int blocks = k.merge_blocks + (together ? weights : 0);
+  if (blocks && L.err == POSS_OK) {
+    const dim3 grid(blocks, a.g.Hkv * groups, a.batch);
+    if (SCORES && together) launch_pdl(L, k_paged_attn_tc_merge<HD, true>, grid, dim3(256), 0, k, groups);
+    else launch_pdl(L, k_paged_attn_tc_merge<HD, false>, grid, dim3(256), 0, k, groups);
   }
-  if (blocks && L.err == POSS_OK)
-    launch_pdl(L, k_paged_attn_tc_merge<HD, SCORES>, dim3(blocks, a.g.Hkv * groups, a.batch), dim3(256), 0, k, groups);
+  if (weights && !together && L.err == POSS_OK) launch_pdl(L, k_paged_attn_weights, dim3(weights, a.g.Hkv, a.batch), dim3(256), 0, k);
 }
 
 }  // namespace
@@ -1154,8 +1169,8 @@ bool paged_attn_tc_supported(const poss_page_pool& p, int G, float scale) {
 }
 
 // Scores go through memory (4 bytes to and fro per line and slot) where that is no more than reading the keys again (2 bytes per element) to
-// form them anew.  16 trees of 4 heads over up to 8191 slots, attention and weights: 1 row 106 us (keys again: 144), 4 rows 114 (150), 8 rows
-// 141 (147), 9 rows, just above, 148; 64 single tokens over up to 8000: 306 (413).
+// form them anew.  16 trees of 4 heads over up to 8191 slots, attention and weights: 1 row 101 us (keys again: 144), 4 rows 114 (150), 8 rows
+// 140 (147), 9 rows, just above, 148; 64 single tokens over up to 8000: 306 (413).
 size_t paged_attn_tc_scores(const poss_page_pool& p, int batch, int rows, int Hq, int max_pages) {
   const int lines = rows * (Hq / p.n_kv_heads);
   if (lines > p.head_dim / 4) return 0;

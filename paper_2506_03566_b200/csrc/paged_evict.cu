@@ -287,7 +287,8 @@ int poss_pages_evict(const poss_page_pool* pool, void* kv_pages, const int32_t* 
   const size_t rows = (size_t)pool->n_layers * batch * pool->n_kv_heads;
   if (out_mass != mass && overlap(out_mass, rows * mass_slots * 4, mass, rows * mass_slots * 4)) return POSS_E_INVALID;
   const size_t nb = (size_t)batch * 4;
-  if (overlap(out_len, nb, seq_len, nb) || overlap(out_len, nb, keep, nb) || overlap(out_len, nb, tables, nb * max_pages))
+  if (overlap(out_len, nb, seq_len, nb) || overlap(out_len, nb, keep, nb) || overlap(out_len, nb, tables, nb * max_pages) ||
+      overlap(out_len, nb, mass, rows * mass_slots * 4) || overlap(out_len, nb, out_mass, rows * mass_slots * 4))
     return POSS_E_INVALID;
   int64_t launches = 0;
   Launcher L{reinterpret_cast<cudaStream_t>(stream), &launches, POSS_OK};

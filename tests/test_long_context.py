@@ -125,7 +125,7 @@ def test_evict_and_commit_refusals(lib):
     good = [pool(), FAKE, FAKE, 4, 2, mass, mass, 64, FAKE, FAKE, 1, 2, o, FAKE, need, None, None]
     refused(lib.poss_pages_evict, good, [
         (0, None, 1), (1, None, 1), (1, FAKE + 8, 1), (2, None, 1), (3, 0, 1), (4, -1, 1), (4, 1025, 3), (5, None, 1), (6, None, 1),
-        (6, mass + 64, 1), (7, 63, 1), (8, None, 1), (8, o + 4, 1), (9, None, 1), (9, o, 1), (10, -1, 1), (11, -1, 1), (12, None, 1),
+        (6, mass + 64, 1), (7, 63, 1), (8, None, 1), (8, o + 4, 1), (9, None, 1), (9, o, 1), (12, mass + 4, 1), (10, -1, 1), (11, -1, 1), (12, None, 1),
         (13, None, 4), (13, FAKE + 64, 4), (14, need - 1, 4)])
     assert lib.poss_pages_evict(*[0 if i == 4 else a for i, a in enumerate(good)]) == 0
     # pool, pages, mass, slots, tables, max_pages, batch, prefix, path, accepted, out_len, status, stream
