@@ -5,7 +5,7 @@
 // number: no sum crosses threads.  A column's constants (-m, w / l) come from shared memory, the same address for all lanes.
 //
 // A tile is 128 slots of one (sequence, KV head).  The tiles of the whole batch, weighed by their lines, are cut into one contiguous range
-// per CTA, one CTA per SM (16 trees of 1 to 61 rows, cut by tiles alone: 106 us).  More than 256 lines take a pass each over the CTA's
+// per CTA, one CTA per SM (16 trees of 12 to 61 rows, cut by tiles alone: 106 us).  More than 256 lines take a pass each over the CTA's
 // slots; the later ones add to what the first has written.
 //   warps 0-15  weights: four groups of four warps, each every fourth 16 of a tile's columns; they leave their sums in shared memory, and
 //               a tile later one group, in turn, adds the four and writes the tile's weights.  Groups wait for one another only where a
@@ -13,10 +13,13 @@
 //               meanwhile into the other buffer.
 //   warp 16     keys, through a ring of stages (one box per page and 64 columns), and a pass's queries
 //   warp 17     products, one lane
-// What bounds it: a tile takes some 1400 cycles (copies of the keys in small boxes, product, hand-overs) and 7.2 for each line, of which the
-// exponentials alone are 8 per line and scheduler at 16 a cycle: the two do not overlap well.  16 trees of 12 to 61 rows of 4 heads over 4096
-// to 8191 slots: 77 us, of which the exponentials would need 26 and the keys 31.  (Calls of few lines take the weights from the attention's
-// own scores instead: paged_attention_tc.cu.)
+// What bounds it: a tile takes some 1400 cycles (the warps' waits and hand-overs 800 to 900, where they are few lines the copies of the keys
+// instead) and 7.2 for each line (the exponentials alone 8 per line with nothing between them: 32 lanes at 4 a cycle and scheduler).  16 trees
+// of 12 to 61 rows of 4 heads over 4096 to 8191 slots: 77 us, of which the exponentials would need 26 and the keys 31.  Measured and not
+// better there: 8 warps, each all columns of every second tile, 94 us; two groups per tile and parity, each half of the columns, 81 to 88;
+// four buffers of 128 columns, 87; a quarter of the 2^x as a polynomial on the multiply-add pipe, 82; 32 columns at a time in two steps, 89
+// (registers).  Reads of TMEM were measured at 413 bytes a cycle and SM and are no bound.  (Calls of few lines take the weights from the
+// attention's own scores instead: paged_attention_tc.cu.)
 //
 // Every wait is bounded; on expiry the CTA raises POSS_E_TIMEOUT, runs through its (bounded) walk without meaning, waits (bounded) for
 // its copies in flight, frees its TMEM and returns.
