@@ -9,7 +9,7 @@
 // Nothing is looked at while all goes well: a logit far above the base, a banned one (-inf: 0 times its t is NaN), NaN and logits beyond
 // 2^20 show in a step's sums, which are then formed anew, or with care in a pass of their own.  That saves the clamps and the extremes.
 //
-// The K best.  The first step's bound is the K-th best of 16 maxima of disjoint parts of the CTA: K logits are at or above it.  What reaches
+// The K best.  The first step's bound is the K-th best of 32 maxima of disjoint parts of the CTA: K logits are at or above it.  What reaches
 // the bound is listed; behind steps 4, 16, ... and the last the list is cut to its K best, the last of which is the next bound (only
 // greater ones can follow: places rise from step to step).  Listing costs nothing but where a thread's maximum of eight reaches the bound.
 // A list that overflows (hundreds of equal or ever rising logits) makes the CTA read its part again, a slower way: warps keep their K best
