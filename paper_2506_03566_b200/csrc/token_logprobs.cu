@@ -8,15 +8,18 @@
 //   log sum e^(x / T) = ln 2 (base + log2 s),  H = ln 2 (log2 s - w / s).
 // Nothing is looked at while all goes well: a logit far above the base, a banned one (-inf: 0 times its t is NaN), NaN and logits beyond
 // 2^20 show in a step's sums, which are then formed anew, or with care in a pass of their own.  That saves the clamps and the extremes.
+// Logits below -2^20, such as a mask of the type's lowest value, are left out where others make up the sum.
 //
 // The K best.  The first step's bound is the K-th best of 32 maxima of disjoint parts of the CTA: K logits are at or above it.  What reaches
 // the bound is listed; behind steps 4, 16, ... and the last the list is cut to its K best, the last of which is the next bound (only
 // greater ones can follow: places rise from step to step).  Listing costs nothing but where a thread's maximum of eight reaches the bound.
-// A list that overflows (hundreds of equal or ever rising logits) makes the CTA read its part again, a slower way: warps keep their K best
-// in order, one per lane.  Entries are 64-bit numbers that order as (value, token) do, so that an entry's place is the count of those
-// above it; the cluster's first CTA joins the others' lists and sums.
+// A step that is mostly masked (most parts' maxima equal the bound) lists what is above the mask, is cut at once, and leaves the bound to the
+// next step if that was fewer than K.  A list that overflows (ever rising logits), or whose K best are no better than a mask, makes the CTA
+// read its part again, a slower way: warps keep their K best in order, one per lane.  Entries are 64-bit numbers that order as (value, token)
+// do, so that an entry's place is the count of those above it; the cluster's first CTA joins the others' lists and sums.
 // What bounds it: 2048 rows over 128256 bf16 tokens, 525 MB, take 95 us without best tokens (5.5 TB/s; 7 instructions per logit keep the
-// schedulers busy 60 %), 109 with one and 145 with 16, where a CTA's few barriers and a warp's looks at reached bounds cost more than the
+// schedulers busy 60 %), 109 with one and 134 with 10 (with a quarter of the tokens banned in one piece 143 and 179, with all but 0.1 %
+// 150 and 183, with 70 % strewn 169 and 188), where a CTA's few barriers and a warp's looks at reached bounds cost more than the
 // maxima.  One row over 128256 fp32 tokens with 10 best ones 8.9 us: launch, two steps, a cut and the cluster's join.
 #include "paged.cuh"
 #include <cooperative_groups.h>
@@ -35,6 +38,7 @@ constexpr int KMAX = POSS_MAX_TOPK;
 constexpr int MAX_CLUSTER = 8;
 constexpr int PARTS = 32;                    // of eight threads each: their maxima give the first bound
 constexpr int LIST = 512;                    // entries that may wait for the next cut
+constexpr int AT_ONCE = 8;                   // logits of a thread on their way in the slower ways
 
 struct Args {
   const void* logits;
@@ -162,7 +166,11 @@ struct Stream {
     if (plain<false>(x, c)) return;
     const float m = max_of(x), top = rintf(m * c);
     if (m == -INFINITY) return;                           // (banned all)
-    if (!(fabsf(top) < SMALL)) { rare = true; return; }
+    if (top <= -SMALL) {                                  // nothing beside a logit that is not as low; else the base tells of it
+      if (s == 0.f) base = -FLT_MAX;
+      return;
+    }
+    if (!(top < SMALL)) { rare = true; return; }
     if (!(base >= top)) {
       if (s != 0.f) {
         const float d = fmaxf(base - top, -200.f), f = ex2(d);
@@ -181,21 +189,27 @@ struct Stream {
 // first (one that overflows is -inf; those that count are near the reference, where they lose nothing).
 template <typename T> __device__ __noinline__ Sums careful(const T* row, int e0, int e1, float c) {
   float ref = -INFINITY, s = 0.f, w = 0.f;
-  for (int i = e0 + (int)threadIdx.x; i < e1; i += THREADS) {
-    const float x = to_f(row[i]);
-    if (!(fabsf(x) < INFINITY)) continue;
-    float t = (x - ref) * c;
-    if (!(t <= 4.f)) {
-      const float d = fmaxf((ref - x) * c, -200.f), f = s == 0.f ? 0.f : ex2(d);
-      w = s == 0.f ? 0.f : f * fmaf(s, d, w);
-      s *= f;
-      ref = x;
-      t = 0.f;
+  for (int i = e0 + (int)threadIdx.x; i < e1; i += THREADS * AT_ONCE) {
+    float xs[AT_ONCE];
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; ++u) xs[u] = i + u * THREADS < e1 ? to_f(row[i + u * THREADS]) : -INFINITY;
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; ++u) {
+      const float x = xs[u];
+      if (!(fabsf(x) < INFINITY)) continue;
+      float t = (x - ref) * c;
+      if (!(t <= 4.f)) {
+        const float d = fmaxf((ref - x) * c, -200.f), f = s == 0.f ? 0.f : ex2(d);
+        w = s == 0.f ? 0.f : f * fmaf(s, d, w);
+        s *= f;
+        ref = x;
+        t = 0.f;
+      }
+      t = fmaxf(t, -200.f);
+      const float e = ex2(t);
+      s += e;
+      w = fmaf(e, t, w);
     }
-    t = fmaxf(t, -200.f);
-    const float e = ex2(t);
-    s += e;
-    w = fmaf(e, t, w);
   }
   return {s == 0.f ? 0.0 : (double)ref * (double)c, s, w};
 }
@@ -249,29 +263,42 @@ template <typename T> __device__ __noinline__ void best_slowly(const T* row, int
   __syncthreads();
   float lv = -INFINITY;                      // the lane's entry of the warp's list
   int li = 0x7fffffff;
-  for (int i0 = e0 + warp * 32; i0 < e1; i0 += THREADS) {
-    const int i = i0 + lane;
-    float x = i < e1 ? to_f(row[i]) : -INFINITY;
-    if (!(fabsf(x) < INFINITY)) x = -INFINITY;
+  auto bound = [&] {
     float others = lane < WARPS ? sh->warp_bound[lane] : -INFINITY;
 #pragma unroll
     for (int o = WARPS / 2; o > 0; o >>= 1) others = fmaxf(others, __shfl_xor_sync(0xffffffffu, others, o));
     const float own = __shfl_sync(0xffffffffu, lv, K - 1);
-    const float from = fmaxf(above(own), __shfl_sync(0xffffffffu, others, 0));   // (places rise)
-    unsigned who = __ballot_sync(0xffffffffu, x >= from);
-    if (!who) continue;
-    while (who) {
-      const int src = __ffs(who) - 1;
-      who &= who - 1;
-      const float v = __shfl_sync(0xffffffffu, x, src);
-      const int vi = i0 + src, pos = __popc(__ballot_sync(0xffffffffu, before(lv, li, v, vi)));
-      const float uv = __shfl_up_sync(0xffffffffu, lv, 1);
-      const int ui = __shfl_up_sync(0xffffffffu, li, 1);
-      if (lane == pos) { lv = v; li = vi; }
-      else if (lane > pos) { lv = uv; li = ui; }
+    return fmaxf(above(own), __shfl_sync(0xffffffffu, others, 0));   // (places rise)
+  };
+#pragma unroll 1
+  for (int j0 = e0 + warp * 32; j0 < e1; j0 += THREADS * AT_ONCE) {
+    float xs[AT_ONCE], m = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; ++u) xs[u] = j0 + u * THREADS + lane < e1 ? to_f(row[j0 + u * THREADS + lane]) : -INFINITY;
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; ++u) {
+      if (!(fabsf(xs[u]) < INFINITY)) xs[u] = -INFINITY;
+      m = fmaxf(m, xs[u]);
     }
-    const float now = __shfl_sync(0xffffffffu, lv, K - 1);
-    if (lane == 0) sh->warp_bound[warp] = now;
+    if (!__any_sync(0xffffffffu, m >= bound())) continue;
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; ++u) {
+      const float x = xs[u];
+      unsigned who = __ballot_sync(0xffffffffu, x >= bound());
+      if (!who) continue;
+      while (who) {
+        const int src = __ffs(who) - 1;
+        who &= who - 1;
+        const float v = __shfl_sync(0xffffffffu, x, src);
+        const int vi = j0 + u * THREADS + src, pos = __popc(__ballot_sync(0xffffffffu, before(lv, li, v, vi)));
+        const float uv = __shfl_up_sync(0xffffffffu, lv, 1);
+        const int ui = __shfl_up_sync(0xffffffffu, li, 1);
+        if (lane == pos) { lv = v; li = vi; }
+        else if (lane > pos) { lv = uv; li = ui; }
+      }
+      const float now = __shfl_sync(0xffffffffu, lv, K - 1);
+      if (lane == 0) sh->warp_bound[warp] = now;
+    }
   }
   if (lane < K) sh->list[warp * K + lane] = lv > -INFINITY ? key_of(lv, li) : 0ull;
   __syncthreads();
@@ -302,8 +329,10 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 3 : 4) k_token_logpr
   Stream sum = {NAN, 0.f, 0.f, false};
   float lo = -FLT_MAX;                       // what may be among the best: at or above it
   constexpr int FIRST_CUT = 4;
-  int next_cut = FIRST_CUT;
+  int next_cut = FIRST_CUT, span = 3 * FIRST_CUT;         // steps between that cut and the one behind it
   bool overflow = false;
+  int bound_at = 0;                          // the step whose maxima give a bound
+  float skipped = -INFINITY;                 // what equals it or is less may not be listed
   const int full = (p1 - p0) / (THREADS * PIECES);        // steps without a gap
   auto fetch = [&](int it, uint4* w) {
     const uint4* const from = body + p0 + it * (THREADS * PIECES) + t;
@@ -352,7 +381,7 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 3 : 4) k_token_logpr
         for (int j = 0; j < PER; ++j) x[j] = fabsf(x[j]) < INFINITY ? x[j] : -INFINITY;
         maxima();
       }
-      if (it == 0) {
+      if (it == bound_at) {
         float mp = m;
 #pragma unroll
         for (int o = 4; o > 0; o >>= 1) mp = fmaxf(mp, __shfl_xor_sync(0xffffffffu, mp, o));
@@ -365,8 +394,16 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 3 : 4) k_token_logpr
 #pragma unroll
         for (int o = 0; o < PARTS; ++o) r += before(sh.part_max[o], o, own, lane);
         const unsigned who = __ballot_sync(0xffffffffu, r == K - 1);
-        lo = fmaxf(lo, __shfl_sync(0xffffffffu, own, __ffs(who) - 1));
-      } else if (it == steps && next_cut > FIRST_CUT) {   // single ones lie before or behind the others: an equal one may be earlier
+        const float b = __shfl_sync(0xffffffffu, own, __ffs(who) - 1);
+        lo = fmaxf(lo, b);
+        // Most parts have nothing better: a mask, whatever its value.  (2048 rows over 128256 bf16 tokens, 10 best of the 0.1 % above the type's
+        // lowest value, 516 -> 183 us; rows without a mask 131 -> 134)
+        if (__popc(__ballot_sync(0xffffffffu, own == b)) > PARTS - KMAX) {
+          if (b > -INFINITY) { lo = fmaxf(lo, above(b)); skipped = fmaxf(skipped, b); }
+          next_cut = it + 1;
+          span = 1;
+        }
+      } else if (it == steps && span != 3 * FIRST_CUT) {  // after a cut: single ones lie before or behind the others, an equal one may be earlier
         const unsigned long long last = sh.list[K - 1];   // (not written since the last cut)
         if (last) lo = value_of(last);
       }
@@ -385,21 +422,29 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 3 : 4) k_token_logpr
         }
       }
       if (it + 1 == next_cut || it + 1 == all_steps) {
-        next_cut *= 4;
         __syncthreads();
         const int n = sh.n;
         overflow |= n > LIST;                             // (the same for all; the list is of no use from here on)
-        if (!overflow) {
+        next_cut = it + 1 + span;
+        span = bound_at == it ? span : 4 * span;
+        if (overflow) {
+          lo = INFINITY;                                  // (nothing more is listed)
+        } else {
           cut(sh.list, n, K, &sh.n);
           const unsigned long long last = sh.list[K - 1];
           if (last) lo = above(value_of(last));
+          else bound_at = it + 1;                         // (as good as all banned so far)
         }
       }
     }
   }
   // ---- the CTA's sums and list, the slower ways
   const int e0 = rank == 0 ? 0 : head + p0 * N, e1 = rank == cs - 1 ? a.V : head + p1 * N;
-  const bool rare = __syncthreads_or(sum.rare);
+  bool rare = __syncthreads_or(sum.rare);
+  if (skipped > -INFINITY && !overflow) {                 // (the same for all, the list in order)
+    const unsigned long long last = sh.list[K - 1];
+    overflow = !(last && value_of(last) > skipped);
+  }
   if (overflow) best_slowly(base, e0, e1, K, &sh);
   Sums all;                                               // of the CTA, then of the row: warp 0 has them
   if (!rare) {
@@ -412,7 +457,10 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 3 : 4) k_token_logpr
 #pragma unroll
     for (int o = WARPS / 2; o > 0; o >>= 1) x = joined(x, shfl_xor(x, o));
     all = {x.s == 0.f ? 0.0 : (double)x.base, x.s, x.w};
-  } else {
+    // low ones were left out: right where the sum is of others (what is missing is 2^-255 of it)
+    if (!(x.s != 0.f && x.base >= 256.f - SMALL)) rare = __syncthreads_or(x.s != 0.f || sum.base == -FLT_MAX);
+  }
+  if (rare) {
     all = careful(base, e0, e1, a.c);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) all = joined(all, shfl_xor(all, o));

@@ -153,3 +153,40 @@ def test_scores_of_a_verified_tree():
     got = lib().poss_token_logprobs(logits, i32(tokens), token_rows=i32(parents), topk=3)
     lu.check_scores(got, lu.scores(logits.cpu().double(), tokens, parents, 3, 1.0))
     assert torch.equal(got["top_tokens"][:, 0], arg) and got["logp"][0] == 0
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("rows,vocab", [(302, 41003), (302, 24576), (12, 100001)])
+def test_masked_vocabularies(dtype, rows, vocab):
+    """Rows of several steps that begin with banned tokens or keep few: masks of -inf, of the type's lowest value and of plain numbers."""
+    gen = torch.Generator().manual_seed(8)
+    x = (torch.randn(rows, vocab, generator=gen) * 3).to(dtype)
+    few = torch.rand(rows, vocab, generator=gen) < 0.001
+    place = torch.arange(vocab)
+    masks = [-math.inf, torch.finfo(dtype).min, -1e4, -1e9]
+    for r in range(rows):
+        v = masks[r // 8 % 4]
+        kind = r % 8
+        if kind == 0:
+            x[r, :20000] = v                                          # whole steps of nothing
+        elif kind == 1:
+            x[r][~few[r]] = v
+        elif kind == 2:
+            x[r][place % 3 != 0] = v
+        elif kind == 3:
+            x[r][place % 4999 != 17] = v                              # fewer left than best ones are wanted, or hardly more
+        elif kind == 4:
+            x[r][place % 4999 != 17] = v                              # a few, and then a flood above some of them
+            x[r, 9000:17500] = 0.25
+        elif kind == 5:
+            x[r] = (place // 8192).float()                            # steps that are equal in themselves, rising
+        elif kind == 6:
+            x[r] = -(place // 8192).float()
+            x[r, vocab - 2:] = 0.0                                    # equal ones behind all steps
+        else:
+            x[r, 16400:] = v
+            x[r, :3] = v
+            x[r, vocab - 1] = 1.0
+    tokens = torch.randint(0, vocab, (rows,), generator=gen).tolist()
+    for k, t in ((1, 1.0), (10, 1.0), (16, 0.7)):
+        check(x, tokens, None, k, t)
