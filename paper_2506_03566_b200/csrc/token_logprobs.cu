@@ -22,6 +22,7 @@
 // 150 and 183, with 70 % strewn 169 and 188), where a CTA's few barriers and a warp's looks at reached bounds cost more than the
 // maxima.  One row over 128256 fp32 tokens with 10 best ones 8.9 us: launch, two steps, a cut and the cluster's join.
 #include "paged.cuh"
+#include <atomic>
 #include <cooperative_groups.h>
 #include <float.h>
 
@@ -35,7 +36,7 @@ constexpr int THREADS = 256, WARPS = THREADS / 32;
 constexpr int PER = 32;                      // logits of a thread and step
 constexpr int STEP = THREADS * PER;
 constexpr int KMAX = POSS_MAX_TOPK;
-constexpr int MAX_CLUSTER = 8;
+constexpr int MAX_CLUSTER = 8;               // (log_cs 0 to 3)
 constexpr int PARTS = 32;                    // of eight threads each: their maxima give the first bound
 constexpr int LIST = 512;                    // entries that may wait for the next cut
 constexpr int AT_ONCE = 8;                   // logits of a thread on their way in the slower ways
@@ -528,13 +529,34 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 3 : 4) k_token_logpr
   }
 }
 
-// CTAs per row: one step each at the least, and no more than are resident at once (four per SM of 148).  61 rows over 32000 bf16 tokens with
-// the 10 best: 10.9, 9.8, 9.2 and 10.9 us with 1, 2, 4 and 8; one row over 128256 fp32 tokens 19.8, 15.0, 10.7, 8.8; 200 rows over 128256 bf16
-// tokens with the best one 30, 23, 25, 29; 500 rows 36, 41, 49, 64.
-int cluster_of(int rows, int vocab) {
-  int cs = 1;
-  while (cs < MAX_CLUSTER && (long long)rows * cs * 2 <= 4 * 148 && (long long)vocab > (long long)STEP * cs) cs *= 2;
-  return cs;
+// How many clusters of 2^log_cs CTAs the device holds at once (a cluster's SMs are neighbours, so that fewer fit than their CTAs would)
+template <typename T> int clusters_at_once(int log_cs) {
+  static std::atomic<int> known[PerDeviceFlags::MAX_DEVICES][4];           // one more than the answer
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= PerDeviceFlags::MAX_DEVICES) return 0;
+  int n = known[dev][log_cs].load(std::memory_order_relaxed);
+  if (!n) {
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim.x = 1 << log_cs; at.val.clusterDim.y = 1; at.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(1 << log_cs);
+    cfg.blockDim = dim3(THREADS);
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    int most = 0;
+    if (cudaOccupancyMaxActiveClusters(&most, k_token_logprobs<T>, &cfg) != cudaSuccess) return 0;
+    known[dev][log_cs].store(n = most + 1, std::memory_order_relaxed);
+  }
+  return n - 1;
+}
+// CTAs per row: one step each at the least, and no more than are resident at once.  61 rows over 32000 bf16 tokens with the 10 best: 10.9, 9.8,
+// 9.2 and 10.9 us with 1, 2, 4 and 8; one row over 128256 fp32 tokens 19.8, 15.0, 10.7, 8.8; 48 rows over 71943 bf16 tokens with the best one
+// 10.7 with 8, 54 rows 14.5 (with 4 11.8).
+template <typename T> int log_cluster_of(int rows, int vocab) {
+  int log_cs = 0;
+  while (1 << log_cs < MAX_CLUSTER && (long long)vocab > (long long)STEP << log_cs && rows <= clusters_at_once<T>(log_cs + 1)) ++log_cs;
+  return log_cs;
 }
 
 }  // namespace
@@ -571,9 +593,7 @@ extern "C" int poss_token_logprobs(const void* logits, int64_t ld, int dtype, in
   a.tokens = tokens; a.token_rows = token_rows;
   a.out_logp = out_logp; a.out_lse = out_lse; a.out_entropy = out_entropy;
   a.out_top = out_top_tokens; a.out_top_logp = out_top_logp;
-  const int cs = cluster_of(rows, vocab);
-  int log_cs = 0;
-  while (1 << log_cs < cs) ++log_cs;
+  const int log_cs = dtype == POSS_BF16 ? log_cluster_of<bf16>(rows, vocab) : log_cluster_of<float>(rows, vocab), cs = 1 << log_cs;
   cudaLaunchAttribute at[2];
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at[0].val.programmaticStreamSerializationAllowed = 1;
