@@ -209,10 +209,11 @@ __global__ void __launch_bounds__(CHOOSE_THREADS) k_evict_choose(EvictArgs a) {
 }
 
 // Block: (sequence, layer, head), keys / values, and one of `parts` parts of the columns.  A step: four pieces of 16 bytes per thread.
+// A step's targets are read behind its barrier, while others may be a step further: they have a third buffer.
 template <int ES>
 __global__ void __launch_bounds__(MOVE_THREADS) k_evict_move(EvictArgs a, char* pool, int log_parts) {
   constexpr int PIECES = 4;
-  __shared__ long long s_src[2][MOVE_THREADS * PIECES / 2], s_dst[2][MOVE_THREADS * PIECES / 2];   // (two pieces per row at the least)
+  __shared__ long long s_src[2][MOVE_THREADS * PIECES / 2], s_dst[3][MOVE_THREADS * PIECES / 2];   // (two pieces per row at the least)
   pdl_enter(POSS_K_EVICT_MOVE);
   const int t = threadIdx.x, part = blockIdx.x & ((1 << log_parts) - 1), kv = blockIdx.x >> log_parts & 1;
   const int row = blockIdx.x >> log_parts >> 1, head = row % a.g.Hkv, lb = row / a.g.Hkv, b = lb % a.batch, layer = lb / a.batch;
@@ -229,31 +230,33 @@ __global__ void __launch_bounds__(MOVE_THREADS) k_evict_move(EvictArgs a, char* 
     const int p = page_at(table, a.g.max_pages, a.g.n_pages, place);
     return (long long)(page_offset(a.g, layer, p < 0 ? 0 : p, kv, head) + (size_t)(slot - place * a.g.page) * a.g.d) * ES;
   };
-  auto look_up = [&](int r0, int buf) {
+  auto look_up = [&](int r0, int buf, int to) {
     for (int r = t; r < min(rows, keep - r0); r += MOVE_THREADS) {
       s_src[buf][r] = where(src[r0 + r]);
-      s_dst[buf][r] = where(r0 + r);
+      s_dst[to][r] = where(r0 + r);
     }
   };
-  int buf = 0;
-  look_up(hole, 0);
+  int buf = 0, to = 0;
+  look_up(hole, 0, 0);
   __syncthreads();
 #pragma unroll 1
-  for (int r0 = hole; r0 < keep; r0 += rows, buf ^= 1) {
-    const int n = min(rows, keep - r0);
+  for (int r0 = hole; r0 < keep; r0 += rows) {
+    const int n = min(rows, keep - r0), next_to = to == 2 ? 0 : to + 1;
     uint4 x[PIECES];
 #pragma unroll
     for (int j = 0; j < PIECES; ++j) {
       const int i = t + j * MOVE_THREADS, r = i >> shift;
       if (r < n) x[j] = *reinterpret_cast<const uint4*>(pool + s_src[buf][r] + (i - (r << shift)) * 16);
     }
-    if (r0 + rows < keep) look_up(r0 + rows, buf ^ 1);
+    if (r0 + rows < keep) look_up(r0 + rows, buf ^ 1, next_to);
     __syncthreads();                                      // the step's rows are in registers, the next one's places known
 #pragma unroll
     for (int j = 0; j < PIECES; ++j) {
       const int i = t + j * MOVE_THREADS, r = i >> shift;
-      if (r < n) *reinterpret_cast<uint4*>(pool + s_dst[buf][r] + (i - (r << shift)) * 16) = x[j];
+      if (r < n) *reinterpret_cast<uint4*>(pool + s_dst[to][r] + (i - (r << shift)) * 16) = x[j];
     }
+    buf ^= 1;
+    to = next_to;
   }
 }
 
