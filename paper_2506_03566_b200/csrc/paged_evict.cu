@@ -19,7 +19,7 @@ POSS_TRACE_REGISTER()
 
 namespace {
 
-constexpr int CHOOSE_THREADS = 512, CHOOSE_WARPS = 16, MOVE_THREADS = 256;
+constexpr int CHOOSE_THREADS = 512, CHOOSE_WARPS = 16;
 constexpr int PER = 16;                      // slots per thread and chunk
 constexpr int CHUNK = CHOOSE_THREADS * PER;
 constexpr int BINS = 2048;
@@ -209,11 +209,14 @@ __global__ void __launch_bounds__(CHOOSE_THREADS) k_evict_choose(EvictArgs a) {
 }
 
 // Block: (sequence, layer, head), keys / values, and one of `parts` parts of the columns.  A step: four pieces of 16 bytes per thread.
-// A step's targets are read behind its barrier, while others may be a step further: they have a third buffer.
-template <int ES>
-__global__ void __launch_bounds__(MOVE_THREADS) k_evict_move(EvictArgs a, char* pool, int log_parts) {
-  constexpr int PIECES = 4;
-  __shared__ long long s_src[2][MOVE_THREADS * PIECES / 2], s_dst[3][MOVE_THREADS * PIECES / 2];   // (two pieces per row at the least)
+// Places are looked up a step ahead; AHEAD (few blocks): the slots that they are of two steps ahead, so that a step waits for one trip to memory
+// and not two, for registers that many blocks need better (four sequences of 8191 slots in eight layers 106 us, 115 so; two sequences of 4653
+// in seven layers of 2 heads 40, 29 so).  A step's targets are read behind its barrier, while others may be a step further: they have a third
+// buffer.
+template <int ES, int THREADS, bool AHEAD>
+__global__ void __launch_bounds__(THREADS) k_evict_move(EvictArgs a, char* pool, int log_parts) {
+  constexpr int PIECES = 4, ROWS = PIECES / 2;            // pieces, and rows at the most, of a thread (two pieces per row at the least)
+  __shared__ long long s_src[2][THREADS * ROWS], s_dst[3][THREADS * ROWS];
   pdl_enter(POSS_K_EVICT_MOVE);
   const int t = threadIdx.x, part = blockIdx.x & ((1 << log_parts) - 1), kv = blockIdx.x >> log_parts & 1;
   const int row = blockIdx.x >> log_parts >> 1, head = row % a.g.Hkv, lb = row / a.g.Hkv, b = lb % a.batch, layer = lb / a.batch;
@@ -222,7 +225,7 @@ __global__ void __launch_bounds__(MOVE_THREADS) k_evict_move(EvictArgs a, char* 
   const long long slots = (long long)a.g.max_pages * a.g.page;
   const int32_t* src = a.src + (size_t)row * slots;
   const int32_t* table = a.g.tables + (size_t)b * a.g.max_pages;
-  const int per_row = a.g.d * ES / 16 >> log_parts, rows = MOVE_THREADS * PIECES / per_row;   // (a power of two)
+  const int per_row = a.g.d * ES / 16 >> log_parts, rows = THREADS * PIECES / per_row;   // (a power of two)
   const int shift = __ffs(per_row) - 1;
   pool += part * per_row * 16;
   auto where = [&](int slot) {
@@ -230,13 +233,34 @@ __global__ void __launch_bounds__(MOVE_THREADS) k_evict_move(EvictArgs a, char* 
     const int p = page_at(table, a.g.max_pages, a.g.n_pages, place);
     return (long long)(page_offset(a.g, layer, p < 0 ? 0 : p, kv, head) + (size_t)(slot - place * a.g.page) * a.g.d) * ES;
   };
+  int from[ROWS];
+  auto fetch = [&](int r0) {
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+      const int r = t + i * THREADS;
+      from[i] = r < min(rows, keep - r0) ? src[r0 + r] : 0;
+    }
+  };
   auto look_up = [&](int r0, int buf, int to) {
-    for (int r = t; r < min(rows, keep - r0); r += MOVE_THREADS) {
-      s_src[buf][r] = where(src[r0 + r]);
-      s_dst[to][r] = where(r0 + r);
+    if constexpr (AHEAD) {
+#pragma unroll
+      for (int i = 0; i < ROWS; ++i) {
+        const int r = t + i * THREADS;
+        if (r < min(rows, keep - r0)) {
+          s_src[buf][r] = where(from[i]);
+          s_dst[to][r] = where(r0 + r);
+        }
+      }
+      fetch(r0 + rows);
+    } else {
+      for (int r = t; r < min(rows, keep - r0); r += THREADS) {
+        s_src[buf][r] = where(src[r0 + r]);
+        s_dst[to][r] = where(r0 + r);
+      }
     }
   };
   int buf = 0, to = 0;
+  if (AHEAD) fetch(hole);
   look_up(hole, 0, 0);
   __syncthreads();
 #pragma unroll 1
@@ -245,14 +269,14 @@ __global__ void __launch_bounds__(MOVE_THREADS) k_evict_move(EvictArgs a, char* 
     uint4 x[PIECES];
 #pragma unroll
     for (int j = 0; j < PIECES; ++j) {
-      const int i = t + j * MOVE_THREADS, r = i >> shift;
+      const int i = t + j * THREADS, r = i >> shift;
       if (r < n) x[j] = *reinterpret_cast<const uint4*>(pool + s_src[buf][r] + (i - (r << shift)) * 16);
     }
     if (r0 + rows < keep) look_up(r0 + rows, buf ^ 1, next_to);
     __syncthreads();                                      // the step's rows are in registers, the next one's places known
 #pragma unroll
     for (int j = 0; j < PIECES; ++j) {
-      const int i = t + j * MOVE_THREADS, r = i >> shift;
+      const int i = t + j * THREADS, r = i >> shift;
       if (r < n) *reinterpret_cast<uint4*>(pool + s_dst[to][r] + (i - (r << shift)) * 16) = x[j];
     }
     buf ^= 1;
@@ -304,12 +328,20 @@ int poss_pages_evict(const poss_page_pool* pool, void* kv_pages, const int32_t* 
   a.src = reinterpret_cast<int32_t*>(reinterpret_cast<char*>(workspace) + round256(rows * 4));
   launch_pdl(L, k_evict_choose, dim3((unsigned)rows), dim3(CHOOSE_THREADS), 0, a);
   if (L.err != POSS_OK) return L.err;
-  // columns are shared out while that leaves a piece or more to each and the device has room: fewer steps, one behind the other
+  // columns are shared out while that leaves two pieces or more to each and the device has room, and blocks are larger where there are few and
+  // a table has room for some steps: fewer steps, one behind the other (one sequence of 8191 slots, 8 heads, 7000 stay: 44 -> 41 us; three of
+  // 700 slots 10.7, with large blocks 11.0)
   int log_parts = 0;
-  const int pieces = pool->head_dim * (pool->dtype == POSS_BF16 ? 2 : 4) / 16;
-  while (log_parts < 2 && pieces >> (log_parts + 1) >= 2 && (rows << (log_parts + 2)) <= 4 * (size_t)current_sm_count()) ++log_parts;
-  launch_pdl(L, pool->dtype == POSS_BF16 ? k_evict_move<2> : k_evict_move<4>, dim3((unsigned)(rows << (1 + log_parts))),
-             dim3(MOVE_THREADS), 0, a, reinterpret_cast<char*>(kv_pages), log_parts);
+  const int es = pool->dtype == POSS_BF16 ? 2 : 4, pieces = pool->head_dim * es / 16;
+  const size_t sms = current_sm_count();
+  const bool steps = (int64_t)max_pages * pool->page_slots > 2048;
+  while (log_parts < (steps ? 3 : 2) && pieces >> (log_parts + 1) >= 2 && (rows << (log_parts + 2)) <= 4 * sms) ++log_parts;
+  const size_t blocks = rows << (1 + log_parts);
+  auto move = [&](auto kernel, int threads) {
+    launch_pdl(L, kernel, dim3((unsigned)blocks), dim3(threads), 0, a, reinterpret_cast<char*>(kv_pages), log_parts);
+  };
+  if (blocks <= 2 * sms && steps) es == 2 ? move(k_evict_move<2, 512, true>, 512) : move(k_evict_move<4, 512, true>, 512);
+  else es == 2 ? move(k_evict_move<2, 256, false>, 256) : move(k_evict_move<4, 256, false>, 256);
   return L.err;
 }
 
