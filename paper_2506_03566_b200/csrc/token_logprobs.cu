@@ -18,9 +18,9 @@
 // read its part again, a slower way: warps keep their K best in order, one per lane.  Entries are 64-bit numbers that order as (value, token)
 // do, so that an entry's place is the count of those above it; the cluster's first CTA joins the others' lists and sums.
 // What bounds it: 2048 rows over 128256 bf16 tokens, 525 MB, take 95 us without best tokens (5.5 TB/s; 7 instructions per logit keep the
-// schedulers busy 60 %), 109 with one and 134 with 10 (with a quarter of the tokens banned in one piece 143 and 179, with all but 0.1 %
+// schedulers busy 60 %), 110 with one and 134 with 10 (with a quarter of the tokens banned in one piece 143 and 179, with all but 0.1 %
 // 150 and 183, with 70 % strewn 169 and 188), where a CTA's few barriers and a warp's looks at reached bounds cost more than the
-// maxima.  One row over 128256 fp32 tokens with 10 best ones 8.9 us: launch, two steps, a cut and the cluster's join.
+// maxima.  One row over 128256 fp32 tokens with 10 best ones 9.2 us: launch, two steps, a cut and the cluster's join.
 #include "paged.cuh"
 #include <atomic>
 #include <cooperative_groups.h>
