@@ -524,7 +524,7 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 3 : 4) k_token_logpr
     for (int i = t; i < a.n_tokens; i += THREADS) {
       const int of = a.token_rows[i];
       if (of == row) token(i);
-      else if (row == 0 && (of < 0 || of >= a.rows)) a.out_logp[i] = of < 0 ? 0.f : -INFINITY;
+      else if (row == 0 && (of < 0 || of >= a.rows)) a.out_logp[i] = of < 0 || a.tokens[i] < 0 ? 0.f : -INFINITY;
     }
   }
 }

@@ -190,3 +190,11 @@ def test_masked_vocabularies(dtype, rows, vocab):
     tokens = torch.randint(0, vocab, (rows,), generator=gen).tolist()
     for k, t in ((1, 1.0), (10, 1.0), (16, 0.7)):
         check(x, tokens, None, k, t)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+def test_no_token_is_none_in_any_row(dtype):
+    """A token below 0 scores 0 in a row behind the last one too; a token in such a row is banned."""
+    x = torch.randn(3, 50, generator=torch.Generator().manual_seed(5)).to(dtype)
+    got = check(x, [-1, -5, 7, -1, 7, -1], [3, 1 << 30, 3, -1, -1, 2], 0)
+    assert got["logp"].cpu().tolist() == [0, 0, -math.inf, 0, 0, 0]
