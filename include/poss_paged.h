@@ -143,14 +143,22 @@ POSS_API int poss_paged_tree_attention_mass(const poss_page_pool* pool, int laye
  * lower slot (-0 equals 0, NaN is below all).  They move to slots 0 .. keep[b] - 1 in their order, keys and values, and their masses to
  * out_mass (same shape; may be mass).  A sequence with seq_len[b] <= keep[b] keeps its slots (its masses are copied).  out_len int32
  * [batch] = slots that stay.  Slots and out_mass entries behind them are left as they were; poss_pages_remap gives surplus pages back.
- * Keys stay rotated as they are: positions of later rows go on.  The slots must lie in pages that no other sequence holds and that a
- * table names once.  A sequence with seq_len out of range, keep[b] < 0 or, where slots have to go, keep[b] < first + recent, or without
+ * Keys stay rotated as they are: positions of later rows go on.  The pages of places `first` to keep[b] - 1 are written: no other
+ * sequence may hold them, none of the same call either, and a table names a page once.  poss_pages_evict takes the caller's word for it;
+ * poss_pages_evict_refs looks it up in refs int32[n_pages], the holders of every page as poss_pages_remap counts them (NULL: the caller's
+ * word): a sequence that would write to a page of more than one holder (a fork, a pinned prefix behind `first`) keeps its slots, as one
+ * without a page that it needs.  (Forks and prefixes that are to be cut all the same: let `first` reach to the end of the shared pages, or
+ * cut them before they are shared.)  A sequence with seq_len out of range, keep[b] < 0 or, where slots have to go, keep[b] < first + recent, or without
  * a page that it needs, keeps its slots and gets out_len = seq_len (status; its out_mass entries are left as they were).
- * out_mass equals mass or does not overlap it; out_len overlaps no input.  Errors: INVALID, SHAPE, CAPACITY, WORKSPACE. */
+ * out_mass equals mass or does not overlap it, nor refs; out_len overlaps no input.  Errors: INVALID, SHAPE, CAPACITY, WORKSPACE. */
 POSS_API size_t poss_pages_evict_workspace_bytes(const poss_page_pool* pool, int batch, int max_pages);
 POSS_API int poss_pages_evict(const poss_page_pool* pool, void* kv_pages, const int32_t* tables, int max_pages, int batch,
                      const float* mass, float* out_mass, int64_t mass_slots, const int32_t* seq_len, const int32_t* keep, int first,
                      int recent, int32_t* out_len, void* workspace, size_t workspace_bytes, int32_t* status, poss_stream stream);
+POSS_API int poss_pages_evict_refs(const poss_page_pool* pool, void* kv_pages, const int32_t* tables, int max_pages, int batch,
+                          const int32_t* refs, const float* mass, float* out_mass, int64_t mass_slots, const int32_t* seq_len,
+                          const int32_t* keep, int first, int recent, int32_t* out_len, void* workspace, size_t workspace_bytes,
+                          int32_t* status, poss_stream stream);
 
 /* poss_pages_compact whose accepted slots take their masses with them: mass[..][prefix_len[b] + k] = mass[..][prefix_len[b] +
  * path[b][k]] for k = 1 .. n_accepted[b], in every layer and KV head.  (What lies behind is set by the attention that follows.) */

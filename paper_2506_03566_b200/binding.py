@@ -134,6 +134,9 @@ EXPORTS = {
     "poss_pages_evict": (C.c_int, [C.POINTER(poss_page_pool), C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_void_p,
                                    C.c_int64, C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_size_t,
                                    C.c_void_p, C.c_void_p]),
+    "poss_pages_evict_refs": (C.c_int, [C.POINTER(poss_page_pool), C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_void_p,
+                                        C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_void_p,
+                                        C.c_size_t, C.c_void_p, C.c_void_p]),
     "poss_pages_compact_mass": (C.c_int, [C.POINTER(poss_page_pool), C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int, C.c_int] +
                                 [C.c_void_p] * 6),
     "poss_token_logprobs": (C.c_int, [C.c_void_p, C.c_int64, C.c_int, C.c_int, C.c_int, C.c_float, C.c_void_p, C.c_void_p, C.c_int,

@@ -528,7 +528,7 @@ POSS_CALL(attention_mass, 13) {
   return x[10];
 }
 
-POSS_CALL(evict, 11) {  // kv_pages, mass, tables, seq_len, keep, first, recent, out_mass, out_len, workspace, status
+POSS_CALL(evict, 12) {  // kv_pages, mass, tables, seq_len, keep, first, recent, out_mass, out_len, workspace, status, refs
   const Pool pool(x[0]);
   const int dev = pool.dev;
   const Table t(x[2], "tables", dev);
@@ -547,10 +547,11 @@ POSS_CALL(evict, 11) {  // kv_pages, mass, tables, seq_len, keep, first, recent,
   } else {
     out = ints<int32_t>(x[8], {b}, "out_len", dev);
   }
+  const int32_t* refs = opt_ints(x[11], {pool.p.n_pages}, "refs", dev);
   const Scratch ws(x[9], poss_pages_evict_workspace_bytes(&pool.p, b, t.max_pages), dev);
   call("poss_pages_evict", dev, [&](poss_stream stream) {
-    return poss_pages_evict(&pool.p, pool.pages, t.at, t.max_pages, b, mass.at, out_mass.at, mass.slots, len, keep, first, recent, out,
-                            ws.at, ws.bytes, status, stream);
+    return poss_pages_evict_refs(&pool.p, pool.pages, t.at, t.max_pages, b, refs, mass.at, out_mass.at, mass.slots, len, keep, first, recent,
+                                 out, ws.at, ws.bytes, status, stream);
   });
   if (made.defined()) return THPVariable_Wrap(std::move(made));
   Py_INCREF(x[8]);

@@ -30,7 +30,7 @@ struct EvictArgs {
   const float* mass;
   float* out_mass;
   long long mass_slots;                      // weights per (layer, sequence, head)
-  const int32_t *seq_len, *keep;
+  const int32_t *seq_len, *keep, *refs;      // refs: NULL, or the holders of every page
   int32_t *out_len, *status;
   int32_t* src;                              // [layers][batch][heads][slots]: the slot that moves to each place
   int32_t* hole;                             // [layers][batch][heads]: the first place that changes; out_len where none does
@@ -86,7 +86,12 @@ __global__ void __launch_bounds__(CHOOSE_THREADS) k_evict_choose(EvictArgs a) {
   // (the pages are looked at while the weights are on their way)
   const int32_t* table = a.g.tables + (size_t)b * a.g.max_pages;
   if (cuts)
-    for (int i = t; i < (n + a.g.page - 1) / a.g.page; i += CHOOSE_THREADS) ok &= page_at(table, a.g.max_pages, a.g.n_pages, i) >= 0;
+    for (int i = t; i < (n + a.g.page - 1) / a.g.page; i += CHOOSE_THREADS) {
+      const int p = page_at(table, a.g.max_pages, a.g.n_pages, i);
+      ok &= p >= 0;
+      // a page that others hold is read alone: no place from `first` on lies in it.  (The same for all layers and heads: so is the new length.)
+      if (a.refs && p >= 0 && keep > a.first && (long long)(i + 1) * a.g.page > a.first && i * a.g.page < keep) ok &= a.refs[p] <= 1;
+    }
   for (int i = t; i < BINS; i += CHOOSE_THREADS) s_bins[i] = 0;
   if (t == 0) s_hole = keep;
   ok = __syncthreads_and(ok);
@@ -286,20 +291,10 @@ __global__ void __launch_bounds__(THREADS) k_evict_move(EvictArgs a, char* pool,
 
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 
-}  // namespace
-
-extern "C" {
-
-size_t poss_pages_evict_workspace_bytes(const poss_page_pool* pool, int batch, int max_pages) {
-  if (page_pool_check(pool) != POSS_OK || page_table_check(pool, max_pages, batch) != POSS_OK) return 0;
-  const size_t rows = (size_t)pool->n_layers * batch * pool->n_kv_heads;
-  if (rows >= (1ull << 30)) return 0;
-  return round256(rows * 4) + round256(rows * (size_t)max_pages * pool->page_slots * 4);
-}
-
-int poss_pages_evict(const poss_page_pool* pool, void* kv_pages, const int32_t* tables, int max_pages, int batch, const float* mass,
-                     float* out_mass, int64_t mass_slots, const int32_t* seq_len, const int32_t* keep, int first, int recent,
-                     int32_t* out_len, void* workspace, size_t workspace_bytes, int32_t* status, poss_stream stream) {
+// both entries; refs NULL: the caller answers for it that nobody else holds the pages
+int evict(const poss_page_pool* pool, void* kv_pages, const int32_t* tables, int max_pages, int batch, const int32_t* refs, const float* mass,
+          float* out_mass, int64_t mass_slots, const int32_t* seq_len, const int32_t* keep, int first, int recent, int32_t* out_len,
+          void* workspace, size_t workspace_bytes, int32_t* status, poss_stream stream) {
   int rc = page_pool_check(pool);
   if (rc != POSS_OK) return rc;
   if (batch < 0 || first < 0 || recent < 0) return POSS_E_INVALID;
@@ -315,7 +310,8 @@ int poss_pages_evict(const poss_page_pool* pool, void* kv_pages, const int32_t* 
   if (out_mass != mass && overlap(out_mass, rows * mass_slots * 4, mass, rows * mass_slots * 4)) return POSS_E_INVALID;
   const size_t nb = (size_t)batch * 4;
   if (overlap(out_len, nb, seq_len, nb) || overlap(out_len, nb, keep, nb) || overlap(out_len, nb, tables, nb * max_pages) ||
-      overlap(out_len, nb, mass, rows * mass_slots * 4) || overlap(out_len, nb, out_mass, rows * mass_slots * 4))
+      overlap(out_len, nb, mass, rows * mass_slots * 4) || overlap(out_len, nb, out_mass, rows * mass_slots * 4) ||
+      overlap(out_len, nb, refs, (size_t)pool->n_pages * 4) || overlap(out_mass, rows * mass_slots * 4, refs, (size_t)pool->n_pages * 4))
     return POSS_E_INVALID;
   int64_t launches = 0;
   Launcher L{reinterpret_cast<cudaStream_t>(stream), &launches, POSS_OK};
@@ -323,7 +319,7 @@ int poss_pages_evict(const poss_page_pool* pool, void* kv_pages, const int32_t* 
   a.g = page_geo(pool, tables, max_pages);
   a.batch = batch; a.first = first; a.recent = recent;
   a.mass = mass; a.out_mass = out_mass; a.mass_slots = mass_slots;
-  a.seq_len = seq_len; a.keep = keep; a.out_len = out_len; a.status = status;
+  a.seq_len = seq_len; a.keep = keep; a.refs = refs; a.out_len = out_len; a.status = status;
   a.hole = reinterpret_cast<int32_t*>(workspace);
   a.src = reinterpret_cast<int32_t*>(reinterpret_cast<char*>(workspace) + round256(rows * 4));
   launch_pdl(L, k_evict_choose, dim3((unsigned)rows), dim3(CHOOSE_THREADS), 0, a);
@@ -343,6 +339,32 @@ int poss_pages_evict(const poss_page_pool* pool, void* kv_pages, const int32_t* 
   if (blocks <= 2 * sms && steps) es == 2 ? move(k_evict_move<2, 512, true>, 512) : move(k_evict_move<4, 512, true>, 512);
   else es == 2 ? move(k_evict_move<2, 256, false>, 256) : move(k_evict_move<4, 256, false>, 256);
   return L.err;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t poss_pages_evict_workspace_bytes(const poss_page_pool* pool, int batch, int max_pages) {
+  if (page_pool_check(pool) != POSS_OK || page_table_check(pool, max_pages, batch) != POSS_OK) return 0;
+  const size_t rows = (size_t)pool->n_layers * batch * pool->n_kv_heads;
+  if (rows >= (1ull << 30)) return 0;
+  return round256(rows * 4) + round256(rows * (size_t)max_pages * pool->page_slots * 4);
+}
+
+int poss_pages_evict(const poss_page_pool* pool, void* kv_pages, const int32_t* tables, int max_pages, int batch, const float* mass,
+                     float* out_mass, int64_t mass_slots, const int32_t* seq_len, const int32_t* keep, int first, int recent,
+                     int32_t* out_len, void* workspace, size_t workspace_bytes, int32_t* status, poss_stream stream) {
+  return evict(pool, kv_pages, tables, max_pages, batch, nullptr, mass, out_mass, mass_slots, seq_len, keep, first, recent, out_len,
+               workspace, workspace_bytes, status, stream);
+}
+
+int poss_pages_evict_refs(const poss_page_pool* pool, void* kv_pages, const int32_t* tables, int max_pages, int batch,
+                          const int32_t* refs, const float* mass, float* out_mass, int64_t mass_slots, const int32_t* seq_len,
+                          const int32_t* keep, int first, int recent, int32_t* out_len, void* workspace, size_t workspace_bytes,
+                          int32_t* status, poss_stream stream) {
+  return evict(pool, kv_pages, tables, max_pages, batch, refs, mass, out_mass, mass_slots, seq_len, keep, first, recent, out_len, workspace,
+               workspace_bytes, status, stream);
 }
 
 }  // extern "C"

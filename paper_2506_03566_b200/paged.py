@@ -124,10 +124,13 @@ def poss_pages_evict_workspace_bytes(kv_pages, batch, max_pages):
     return load_library().poss_pages_evict_workspace_bytes(_pool_struct(kv_pages), batch, max_pages)
 
 
-def poss_pages_evict(kv_pages, mass, tables, seq_len, keep, first=0, recent=0, out_mass=None, out_len=None, workspace=None, status=None):
+def poss_pages_evict(kv_pages, mass, tables, seq_len, keep, first=0, recent=0, out_mass=None, out_len=None, workspace=None, status=None,
+                     refs=None):
     """Cuts every sequence to keep[b] slots (int32 [batch]): the first, the last and, of the others, those of greatest mass, for each
-    layer and KV head; they move to the front in their order, their masses to out_mass (None: mass itself).  Returns the new lengths."""
-    return _calls().evict(kv_pages, mass, tables, seq_len, keep, first, recent, out_mass, out_len, workspace, status)
+    layer and KV head; they move to the front in their order, their masses to out_mass (None: mass itself).  With the `refs` of
+    poss_pages_remap a sequence that would write to a page with other holders (a fork, a pinned prefix behind `first`) keeps its slots and
+    raises the status; without them the caller answers for it that there is none.  Returns the new lengths."""
+    return _calls().evict(kv_pages, mass, tables, seq_len, keep, first, recent, out_mass, out_len, workspace, status, refs)
 
 
 def poss_pages_compact(kv_pages, tables, prefix_len, path, n_accepted, out_len=None, status=None, mass=None):

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from tests import long_util as lu
-from tests.test_gpu_long_context import bits, check_mass, evict_case, mass_case, run_mass
+from tests.test_gpu_long_context import bits, check_mass, evict_case, graph_of, mass_case, run_mass
 from tests.test_gpu_paged import BF, F32, Case, cu, i32, lib
 from tests.test_gpu_token_scores import check
 
@@ -115,6 +115,61 @@ def test_eviction_at_once_on_two_streams():
     torch.cuda.synchronize()
     for gp, gm in sets:
         assert torch.equal(gp.cpu(), want[0]) and torch.equal(gm.cpu(), want[1])
+
+
+@pytest.mark.parametrize("dtype,layers,hkv,d", [(BF, 2, 2, 64), (F32, 1, 3, 32)])
+def test_eviction_of_forks_and_pinned_prefixes(dtype, layers, hkv, d):
+    """With the holders of every page, a sequence that would write to a page of another holder keeps its slots, in every layer and head."""
+    pages, _, tables = evict_case(23, dtype, layers, hkv, d, 16, [100, 60], "random")
+    pages = torch.cat([pages, torch.zeros_like(pages[:, :4])], 1)             # (room for the forks' own pages)
+    refs = np.zeros(pages.shape[1], np.int32)
+    refs[tables[tables >= 0]] = 1
+    gp, status = pages.cuda(), torch.zeros(1, dtype=torch.int32, device="cuda")
+    forks = lib().poss_pages_remap(gp, cu(tables), i32([100, 60]), i32(refs), parents=i32([0, 0, 1]), room=i32([0, 0, 0]))
+    t, held = forks["tables"], forks["refs"]
+    tab, lens, start = t.cpu().numpy(), [100, 100, 60], gp.cpu()
+    assert int(forks["n_free"]) >= 0 and (tab[0, :6] == tab[1, :6]).all() and tab[0, 6] != tab[1, 6]
+    mass = torch.rand(layers, 3, hkv, tab.shape[1] * 16, generator=torch.Generator().manual_seed(2))
+    gm = mass.cuda()
+
+    def cut(keep, first, recent, want_len, refs=held, raised=0):
+        status.zero_()
+        to = torch.full_like(gm, 9.0)
+        n = lib().poss_pages_evict(gp, gm, t, i32(lens), i32(keep), first=first, recent=recent, out_mass=to, status=status, refs=refs)
+        assert n.cpu().tolist() == want_len and int(status) == raised
+        ok = [i for i in range(3) if want_len[i] == min(lens[i], keep[i])]
+        want = lu.evict(start, mass[:, ok], torch.full_like(mass[:, ok], 9.0), tab[ok], [lens[i] for i in ok], [keep[i] for i in ok], first, recent)
+        assert torch.equal(bits(gp.cpu()), bits(want[0])) and torch.equal(to[:, ok].cpu(), want[1])
+        assert all((to[:, i] == 9).all() for i in range(3) if i not in ok)
+        gp.copy_(start)
+
+    cut([40, 99, 30], 2, 4, [100, 100, 30], raised=1)                 # both siblings' shared pages stay as they were
+    cut([98, 97, 60], 96, 1, [98, 97, 60])                            # what they share ends before the first place that changes
+    cut([98, 97, 60], 95, 1, [100, 100, 60], raised=1)                # the place before lies in a shared page
+    cut([95, 100, 60], 95, 0, [95, 100, 60])                          # none changes
+    pinned = held.clone()
+    pinned[int(tab[2, 1])] += 1                                       # slots 16 to 31 of the third
+    cut([100, 100, 16], 4, 4, [100, 100, 16], refs=pinned)            # (its places end before them)
+    cut([100, 100, 17], 4, 4, [100, 100, 60], refs=pinned, raised=1)
+    cut([100, 100, 40], 32, 4, [100, 100, 40], refs=pinned)
+    alone = lib().poss_pages_remap(gp, t, i32(lens), held, parents=i32([0, -1, 2]))
+    assert torch.equal(alone["tables"][0], t[0]) and int(alone["refs"].max()) == 1
+    t, tab, lens = alone["tables"], alone["tables"].cpu().numpy(), [100, 0, 60]
+    cut([40, 5, 30], 2, 4, [40, 0, 30], refs=alone["refs"])           # the sibling has gone: the pages are its own
+    # a captured call goes by the holders of its replay
+    live, out = alone["refs"].clone(), torch.zeros(3, dtype=torch.int32, device="cuda")
+    live[int(tab[0, 0])] = 2
+    n0, keep = i32(lens), i32([40, 0, 30])
+    g = graph_of(lambda: lib().poss_pages_evict(gp, gm, t, n0, keep, first=2, recent=4, out_mass=torch.empty_like(gm), out_len=out, refs=live))
+    gp.copy_(start)
+    g.replay()
+    assert out.cpu().tolist() == [100, 0, 30]
+    live[int(tab[0, 0])] = 1
+    gp.copy_(start)
+    g.replay()
+    assert out.cpu().tolist() == [40, 0, 30]
+    with pytest.raises(ValueError, match="refs"):
+        lib().poss_pages_evict(gp, gm, t, n0, keep, refs=live[1:])
 
 
 # ------------------------------------------------------------------ token scores

@@ -134,6 +134,18 @@ def test_evict_and_commit_refusals(lib):
                                                 (6, 1025, 3)])
 
 
+def test_eviction_with_holders_refusals(lib):
+    need = lib.poss_pages_evict_workspace_bytes(pool(), 2, 4)
+    mass, o, refs = FAKE + (1 << 32), FAKE + (1 << 31), FAKE + (1 << 30)
+    # pool, pages, tables, max_pages, batch, refs, mass, out_mass, slots, len, keep, first, recent, out_len, ws, bytes, status, stream
+    good = [pool(), FAKE, FAKE, 4, 2, refs, mass, mass, 64, FAKE, FAKE, 1, 2, o, FAKE, need, None, None]
+    refused(lib.poss_pages_evict_refs, good, [
+        (0, None, 1), (1, None, 1), (2, None, 1), (3, 0, 1), (4, -1, 1), (4, 1025, 3), (5, o, 1), (5, o + 4 - 64 * 4, 1), (5, mass, 1),
+        (6, None, 1), (7, None, 1), (7, refs + 4, 1), (8, 63, 1), (9, None, 1), (9, o, 1), (10, None, 1), (11, -1, 1), (12, -1, 1), (13, None, 1),
+        (13, refs + 64 * 4 - 4, 1), (14, None, 4), (15, need - 1, 4)])
+    assert lib.poss_pages_evict_refs(*[0 if i == 4 else a for i, a in enumerate(good)]) == 0
+
+
 def test_token_score_refusals(lib):
     out = [FAKE + (i << 28) for i in range(1, 6)]
     # logits, ld, dtype, rows, vocab, temperature, tokens, rows_of, n, logp, lse, entropy, k, top, top_logp, stream
