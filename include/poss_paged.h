@@ -80,7 +80,9 @@ POSS_API int poss_rotary(const void* x, int64_t ld_x, void* out, int64_t ld_out,
 /* poss_pages_append of rows that are not rotated yet, and the rotation of their queries, in one launch: k turned into the pages, v as
  * it is, q [batch][rows][n_q_heads][head_dim] turned into out_q of the same shape (rows ld_q and ld_out_q elements apart; out_q may be
  * q; n_q_heads 0: no queries).  positions int32[batch][rows]; NULL: the slot that the row goes to.  (A tree's row sits at its prefix plus
- * its depth; after an eviction positions go on where they were and slots do not.)  All else as poss_pages_append; the queries of a row
+ * its depth; after an eviction positions go on where they were and slots do not.)  out_q overlaps neither k nor v: in place, and with
+ * rows ld_kv apart like theirs (a projection of all three), rows may lie between one another, but no element is of two; elsewhere it lies
+ * before or behind them.  kv_pages overlaps none of the four.  All else as poss_pages_append; the queries of a row
  * whose page is missing are turned all the same, rows behind n_rows leave out_q as it was.  Errors: INVALID, SHAPE, CAPACITY. */
 POSS_API int poss_pages_append_rotary(const poss_page_pool* pool, int layer, void* kv_pages, const int32_t* tables, int max_pages,
                              int batch, int rows, const void* k, const void* v, int64_t ld_kv, int n_q_heads, const void* q,

@@ -236,6 +236,13 @@ bool crossed(const void* out, int64_t ld_out, const void* in, int64_t ld_in, siz
   if (out == in && ld_out == ld_in) return false;
   return overlap(out, (size_t)(n - 1) * ld_out + bytes, in, (size_t)(n - 1) * ld_in + bytes);
 }
+// n rows of a_bytes and n of b_bytes, both ld >= either bytes apart: do two of them, of any places, share a byte
+bool rows_meet(const void* a, size_t a_bytes, const void* b, size_t b_bytes, int64_t ld, int64_t n) {
+  const int64_t apart = (int64_t)(reinterpret_cast<uintptr_t>(a) - reinterpret_cast<uintptr_t>(b)), near = -apart / ld;
+  for (int64_t m = near - 1; m <= near + 1; ++m)          // (row i of a and row i - m of b)
+    if (m > -n && m < n && m * ld + apart < (int64_t)b_bytes && -(m * ld + apart) < (int64_t)a_bytes) return true;
+  return false;
+}
 
 }  // namespace
 
@@ -322,12 +329,20 @@ int poss_pages_append_rotary(const poss_page_pool* pool, int layer, void* kv_pag
     const int64_t row = n_q_heads * d, n = (int64_t)batch * rows;
     if (ld_q < row || ld_out_q < row || (ld_q * es) % 16 || (ld_out_q * es) % 16) return POSS_E_INVALID;
     if (crossed(out_q, ld_out_q * es, q, ld_q * es, row * es, n)) return POSS_E_INVALID;
-    // (in place the three may be parts of one projection, whose rows lie between one another)
-    const size_t kv_bytes = (size_t)((n - 1) * ld_kv + pool->n_kv_heads * d) * es;
-    if (out_q != q && (overlap(out_q, ((n - 1) * ld_out_q + row) * es, k, kv_bytes) ||
-                       overlap(out_q, ((n - 1) * ld_out_q + row) * es, v, kv_bytes)))
-      return POSS_E_INVALID;
+    // (in place the three may be parts of one projection, whose rows lie between one another: its columns must not meet then)
+    const size_t kv_row = pool->n_kv_heads * d * es, kv_bytes = (size_t)(n - 1) * ld_kv * es + kv_row;
+    for (const void* in : {k, v})
+      if (out_q == q && ld_q == ld_kv ? rows_meet(out_q, row * es, in, kv_row, ld_kv * es, n)
+                                      : overlap(out_q, ((n - 1) * ld_out_q + row) * es, in, kv_bytes))
+        return POSS_E_INVALID;
   }
+  // one row's slots may be written while another's elements are read
+  const size_t rows_before = (size_t)batch * rows - 1, pool_bytes = (size_t)pool->n_layers * pool->n_pages * 2 * pool->n_kv_heads * pool->page_slots * d * es;
+  const size_t kv_span = (rows_before * ld_kv + pool->n_kv_heads * d) * es, q_span = (rows_before * ld_q + n_q_heads * d) * es;
+  if (overlap(kv_pages, pool_bytes, k, kv_span) || overlap(kv_pages, pool_bytes, v, kv_span)) return POSS_E_INVALID;
+  if (n_q_heads && (overlap(kv_pages, pool_bytes, q, q_span) ||
+                    overlap(kv_pages, pool_bytes, out_q, (rows_before * ld_out_q + n_q_heads * d) * es)))
+    return POSS_E_INVALID;
   int64_t launches = 0;
   Launcher L{reinterpret_cast<cudaStream_t>(stream), &launches, POSS_OK};
   AppendArgs a;

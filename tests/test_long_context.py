@@ -100,6 +100,32 @@ def test_append_rotary_refusals(lib):
     assert lib.poss_pages_append_rotary(*[0 if i == 5 else a for i, a in enumerate(good)]) == 0
 
 
+def test_append_rotary_refuses_rows_that_meet(lib):
+    """Queries that turn in place between keys and values of one projection may lie between their rows; no element is of two, and none lies
+    in the pages."""
+    es, d, ld = 2, 64, 12 * 64                                        # rows of 8 query heads, 2 of keys, 2 of values, apart as one projection
+    x, pages = FAKE + (1 << 30), FAKE + (1 << 31)
+    pool_bytes = 2 * 64 * 2 * 2 * 16 * d * es
+
+    def call(q=x, k=x + 8 * d * es, v=x + 10 * d * es, out=None, ld_q=ld, ld_out=None, kv_pages=pages, heads=8):
+        out, ld_out = q if out is None else out, ld_q if ld_out is None else ld_out
+        return lib.poss_pages_append_rotary(pool(), 0, kv_pages, FAKE, 4, 2, 3, k, v, ld, heads, q, ld_q, out, ld_out, FAKE, None, None, FAKE, d,
+                                            0, 1.0, None, None)
+
+    head, row = d * es, ld * es
+    for q, k, v in [(x, x + 7 * head, x + 10 * head), (x, x, x + 10 * head), (x, x + 8 * head, x + 7 * head),     # the last query heads
+                    (x + 2 * head, x + head, x + 10 * head), (x, x + 8 * head - 16, x + 10 * head), (x + 10 * head, x + 5 * head, x + 4 * head),
+                    (x, x + 8 * head, x + 11 * head),                 # the last value head is the next row's first query head
+                    (x + row, x + 8 * head, x + 11 * head), (x, x + row + 7 * head, x + 10 * head), (x, x + 8 * head, x + 4 * row + 7 * head)]:
+        assert call(q, k, v) == 1, (q - x, k - x, v - x)
+    assert call(ld_q=8 * d) == 1                                      # in place, but other rows than theirs
+    assert call(out=x + (1 << 20), k=x + (1 << 20) + 8 * head) == 1   # elsewhere: not between them
+    far = x + (1 << 24)
+    for other in ({"q": pages}, {"q": pages + pool_bytes - 16}, {"k": pages + 256}, {"v": pages + pool_bytes - 16}, {"q": far, "out": pages - 16},
+                  {"q": pages - 5 * row, "out": far}, {"k": pages - 5 * row - 2 * head + 16}, {"heads": 0, "k": pages}):
+        assert call(**other) == 1, other
+
+
 def test_mass_refusals(lib):
     need = lib.poss_paged_attention_mass_workspace_bytes(pool(), 2, 3, 4, 4)
     assert need > lib.poss_paged_attention_workspace_bytes(pool(), 2, 3, 4, 4) > 0 and need % 256 == 0
