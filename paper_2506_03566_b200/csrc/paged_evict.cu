@@ -30,7 +30,7 @@ struct EvictArgs {
   const float* mass;
   float* out_mass;
   long long mass_slots;                      // weights per (layer, sequence, head)
-  const int32_t *seq_len, *keep, *refs;      // refs: NULL, or the holders of every page
+  const int32_t *seq_len, *keep;
   int32_t *out_len, *status;
   int32_t* src;                              // [layers][batch][heads][slots]: the slot that moves to each place
   int32_t* hole;                             // [layers][batch][heads]: the first place that changes; out_len where none does
@@ -57,7 +57,8 @@ __device__ __forceinline__ int scan(int v, int* sums, int* total) {
   return x - v + __reduce_add_sync(0xffffffffu, lane < warp ? w : 0);
 }
 
-__global__ void __launch_bounds__(CHOOSE_THREADS) k_evict_choose(EvictArgs a) {
+// refs: NULL, or the holders of every page.  (Not among EvictArgs, 8 bytes of which more cost both kernels together 1.5 us of 106.)
+__global__ void __launch_bounds__(CHOOSE_THREADS) k_evict_choose(EvictArgs a, const int32_t* refs) {
   static_assert(PER * CHOOSE_WARPS <= CHOOSE_THREADS && CHOOSE_WARPS * 32 == CHOOSE_THREADS, "a count per row and warp");
   __shared__ int s_bins[BINS], s_sums[4][CHOOSE_WARPS], s_bin, s_left, s_count, s_hole;
   __shared__ int s_sure[PER * CHOOSE_WARPS], s_tie[PER * CHOOSE_WARPS];
@@ -86,11 +87,12 @@ __global__ void __launch_bounds__(CHOOSE_THREADS) k_evict_choose(EvictArgs a) {
   // (the pages are looked at while the weights are on their way)
   const int32_t* table = a.g.tables + (size_t)b * a.g.max_pages;
   if (cuts)
-    for (int i = t; i < (n + a.g.page - 1) / a.g.page; i += CHOOSE_THREADS) {
+    for (int i = t; i < (n + a.g.page - 1) / a.g.page; i += CHOOSE_THREADS) ok &= page_at(table, a.g.max_pages, a.g.n_pages, i) >= 0;
+  // a page that others hold is read alone: no place from `first` on lies in it.  (The same for all layers and heads: so is the new length.)
+  if (refs && cuts && keep > a.first)
+    for (int i = a.first / a.g.page + t; i * (long long)a.g.page < keep; i += CHOOSE_THREADS) {
       const int p = page_at(table, a.g.max_pages, a.g.n_pages, i);
-      ok &= p >= 0;
-      // a page that others hold is read alone: no place from `first` on lies in it.  (The same for all layers and heads: so is the new length.)
-      if (a.refs && p >= 0 && keep > a.first && (long long)(i + 1) * a.g.page > a.first && i * a.g.page < keep) ok &= a.refs[p] <= 1;
+      ok &= p >= 0 && refs[p] <= 1;
     }
   for (int i = t; i < BINS; i += CHOOSE_THREADS) s_bins[i] = 0;
   if (t == 0) s_hole = keep;
@@ -319,10 +321,10 @@ int evict(const poss_page_pool* pool, void* kv_pages, const int32_t* tables, int
   a.g = page_geo(pool, tables, max_pages);
   a.batch = batch; a.first = first; a.recent = recent;
   a.mass = mass; a.out_mass = out_mass; a.mass_slots = mass_slots;
-  a.seq_len = seq_len; a.keep = keep; a.refs = refs; a.out_len = out_len; a.status = status;
+  a.seq_len = seq_len; a.keep = keep; a.out_len = out_len; a.status = status;
   a.hole = reinterpret_cast<int32_t*>(workspace);
   a.src = reinterpret_cast<int32_t*>(reinterpret_cast<char*>(workspace) + round256(rows * 4));
-  launch_pdl(L, k_evict_choose, dim3((unsigned)rows), dim3(CHOOSE_THREADS), 0, a);
+  launch_pdl(L, k_evict_choose, dim3((unsigned)rows), dim3(CHOOSE_THREADS), 0, a, refs);
   if (L.err != POSS_OK) return L.err;
   // columns are shared out while that leaves two pieces or more to each and the device has room, and blocks are larger where there are few and
   // a table has room for some steps: fewer steps, one behind the other (one sequence of 8191 slots, 8 heads, 7000 stay: 44 -> 41 us; three of
