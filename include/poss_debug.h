@@ -97,6 +97,9 @@ POSS_API int poss_debug_page_of_slot(const int32_t* h_table, int max_pages, int 
  * second of a call of the latter: their queries), the bounded wait runs out after about a second, the call's status word
  * becomes POSS_E_TIMEOUT and its outputs are undefined. */
 POSS_API int poss_debug_paged_lose_load(int launches);
+/* The same behind the next `spared` such launches, which lose nothing: with 1 and 1 the attention of a call that forms weights from the
+ * keys goes on and its weights' launch runs out.  Errors: INVALID. */
+POSS_API int poss_debug_paged_lose_load_after(int spared, int launches);
 
 /* Number of kernels this context has launched so far (host counter). */
 POSS_API int64_t poss_launch_count(const poss_ctx* ctx);

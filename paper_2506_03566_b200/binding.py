@@ -142,6 +142,7 @@ EXPORTS = {
     "poss_token_logprobs": (C.c_int, [C.c_void_p, C.c_int64, C.c_int, C.c_int, C.c_int, C.c_float, C.c_void_p, C.c_void_p, C.c_int,
                                       C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p]),
     "poss_debug_paged_lose_load": (C.c_int, [C.c_int]),
+    "poss_debug_paged_lose_load_after": (C.c_int, [C.c_int, C.c_int]),
     "poss_debug_page_of_slot": (C.c_int, [C.POINTER(C.c_int32), C.c_int, C.c_int, C.c_int, C.c_int64,
                                           C.POINTER(C.c_int), C.POINTER(C.c_int)]),
 }

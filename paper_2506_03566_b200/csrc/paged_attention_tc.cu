@@ -1075,7 +1075,7 @@ __global__ void __launch_bounds__(256) k_paged_attn_tc_merge(const TcArgs k, int
   if (!SCORES && a.ml && slice == 0) a.ml[((size_t)b * a.rows + r) * a.Hq + head * a.G + qh] = paged_ml(m, l);
 }
 
-std::atomic<int> g_lost_loads{0};
+std::atomic<int> g_spared_loads{0}, g_lost_loads{0};   // launches that go on before, and those that lose a load
 
 constexpr size_t PLAN_BYTES = (sizeof(PlanOut) + 255) / 256 * 256;
 // lines of an item that can hold query rows: one slot's, or both
@@ -1136,9 +1136,12 @@ EncodeTiledFn encode_fn() {
 }  // namespace
 
 bool paged_take_lost_load() {
-  int lost = g_lost_loads.load();
-  while (lost > 0 && !g_lost_loads.compare_exchange_weak(lost, lost - 1)) {}
-  return lost > 0;
+  auto take = [](std::atomic<int>& left) {
+    int n = left.load();
+    while (n > 0 && !left.compare_exchange_weak(n, n - 1)) {}
+    return n > 0;
+  };
+  return !take(g_spared_loads) && take(g_lost_loads);
 }
 bool paged_kv_map(CUtensorMap* map, const PagedAttnArgs& a, const void* layer, int slots) {
   const EncodeTiledFn encode = encode_fn();
@@ -1220,8 +1223,12 @@ void launch_paged_attn_tc(Launcher& L, const PagedAttnArgs& a, const void* pool,
   else launch<64, true>(L, k, map, map_q, units, tiles, groups);
 }
 
-extern "C" int poss_debug_paged_lose_load(int launches) {
-  if (launches < 0) return POSS_E_INVALID;
+extern "C" int poss_debug_paged_lose_load(int launches) { return poss_debug_paged_lose_load_after(0, launches); }
+
+extern "C" int poss_debug_paged_lose_load_after(int spared, int launches) {
+  if (spared < 0 || launches < 0) return POSS_E_INVALID;
+  g_lost_loads.store(0);                                  // (a launch meanwhile loses nothing)
+  g_spared_loads.store(spared);
   g_lost_loads.store(launches);
   return POSS_OK;
 }

@@ -90,6 +90,24 @@ def test_lost_loads_run_out_and_the_context_lives_on():
     assert int(c.gpu_status) == 0
 
 
+@pytest.mark.parametrize("heads,d", [((8, 2), 128), ((4, 4), 64)])
+def test_a_lost_load_of_the_weights_alone_raises_the_status(heads, d):
+    """The attention of the call goes on; the launch that forms weights from the keys waits for its queries in vain and says so."""
+    c = Case(98, BF, *heads, d, 16, [700, 5], 40)
+    mass, w = mass_case(c, 4)
+    want = mass.cuda()
+    out = run_mass(c, want, w).clone()
+    assert int(c.gpu_status) == 0
+    assert lib().load_library().poss_debug_paged_lose_load_after(1, 1) == 0
+    got = run_mass(c, mass.cuda(), w)
+    assert int(c.gpu_status) == 6 and torch.equal(bits(got), bits(out))
+    again = mass.cuda()
+    assert torch.equal(bits(run_mass(c, again, w)), bits(out)) and torch.equal(again, want) and int(c.gpu_status) == 0
+    # both launches have been counted: one spared, one that lost its load
+    assert lib().load_library().poss_debug_paged_lose_load_after(2, 0) == 0
+    assert torch.equal(bits(run_mass(c, mass.cuda(), w)), bits(out)) and int(c.gpu_status) == 0
+
+
 # ------------------------------------------------------------------ eviction
 @pytest.mark.parametrize("kind", ["ties", "equal", "random", "rising"])
 def test_eviction_of_long_sequences(kind):

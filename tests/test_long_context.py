@@ -183,6 +183,12 @@ def test_token_score_refusals(lib):
     assert lib.poss_token_logprobs(FAKE, 100, 1, 0, 100, 1.0, None, None, 0, None, None, None, 0, None, None, None) == 0
 
 
+def test_lost_load_hook_refusals(lib):
+    for spared, launches, code in [(-1, 1, 1), (1, -1, 1), (3, 0, 0), (0, 0, 0)]:
+        assert lib.poss_debug_paged_lose_load_after(spared, launches) == code
+    assert lib.poss_debug_paged_lose_load(-1) == 1 and lib.poss_debug_paged_lose_load(0) == 0
+
+
 def test_plain_forms_agree():
     """The eviction's choice against a loop over ranks; the scores against torch's log-softmax."""
     rng = np.random.default_rng(0)
