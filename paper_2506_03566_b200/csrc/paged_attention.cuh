@@ -54,7 +54,9 @@ struct PagedMassArgs {
   long long mass_slots;
   const float* weights;                // NULL, or [batch][rows]
   float scale_log2;
-  float* scores;                       // NULL, or scratch of paged_attn_tc_scores bytes
+  // NULL, or scratch for the scores [batch][Hkv][rows * G][ld]: of the tcgen05 attention ld whole tiles of 64 slots (paged_attn_tc_scores bytes),
+  // of the SIMT attention paged_simt_scores_ld, and batch * rows * Hq * ld * 4 bytes
+  float* scores;
 };
 // tcgen05 kernel: the shapes of the attention's
 void launch_paged_mass_tc(Launcher& L, const PagedMassArgs& s, const void* pool);

@@ -13,10 +13,12 @@
 //               meanwhile into the other buffer.
 //   warp 16     keys, through a ring of stages (one box per page and 64 columns), and a pass's queries
 //   warp 17     products, one lane
-// What bounds it: a tile takes some 1400 cycles (the warps' waits and hand-overs 800 to 900, where they are few lines the copies of the keys
-// instead) and 7.2 for each line (the exponentials alone 8 per line with nothing between them: 32 lanes at 4 a cycle and scheduler).  16 trees
-// of 12 to 61 rows of 4 heads over 4096 to 8191 slots: 77 us, of which the exponentials would need 26 and the keys 31.  Measured and not
-// better there: 8 warps, each all columns of every second tile, 94 us; two groups per tile and parity, each half of the columns, 81 to 88;
+// What bounds it: nothing alone.  16 trees of 12 to 61 rows of 4 heads over 4096 to 8191 slots take 77 us, of which the exponentials (8 cycles
+// per tile and line: 128 lanes at 16 a cycle and SM) would need 28 and the keys 31; by the counters the exponentials' pipe is busy 38 % of the
+// time, the schedulers issue 1.9 instructions of 4 a cycle, and warps mostly wait for fixed latencies, loads of TMEM and shared memory.  Clocks
+// read in one warp show 10 to 17 cycles per line in the powers and sums and some 500 per tile in waits and hand-overs; a least-squares fit
+// over all CTAs gives 1394 per tile and 7.2 per line, fewer than the exponentials alone take: it splits the two wrongly, though their sum is
+// right for trees of these sizes, which is what the cut of the work goes by.  Measured and not better there: 8 warps, each all columns of every second tile, 94 us; two groups per tile and parity, each half of the columns, 81 to 88;
 // four buffers of 128 columns, 87; a quarter of the 2^x as a polynomial on the multiply-add pipe, 82; 32 columns at a time in two steps, 89
 // (registers).  Reads of TMEM were measured at 413 bytes a cycle and SM and are no bound.  (Calls of few lines take the weights from the
 // attention's own scores instead: paged_attention_tc.cu.)
@@ -44,8 +46,8 @@ constexpr int Q_BLOCK = MAX_LINES * 128;
 constexpr int MAX_STAGES = 6;
 constexpr uint32_t TMEM_COLS = 512;     // two buffers of 256 columns
 
-// What a tile costs beside its lines, in lines: 1400 cycles (copy, product, hand-overs) and 7.2 for each line, from the times of all CTAs
-// for 16 trees of 12 to 61 rows.
+// What a tile costs beside its lines, in lines: 1394 cycles and 7.2 for each line, the fit over the times of all CTAs for 16 trees of 12 to 61
+// rows.
 constexpr uint32_t TILE_WEIGHT = 192;
 
 template <int HD> struct Shape {

@@ -9,8 +9,9 @@
 //
 // One block per row: all threads stream the row's heads, two pieces of 16 bytes at a time; while the first are on their way a thread per
 // pair leaves cosine and sine in shared memory.  With halves as pairs the two pieces are partners, so a row may be turned in place.
-// What bounds it: memory for prompts (8192 rows of 48 heads in bf16, 201 MB: 37.8 us, 5.3 TB/s); a chain of trips (lengths and position,
-// table, data) for a token: 3.1 us.
+// What bounds it: memory for prompts of wide rows (8192 rows of 48 heads of 128 in bf16, 201 MB: 37.8 us, 5.3 TB/s; in fp32, 403 MB: 65 us, 6.2
+// TB/s); a chain of trips (lengths and position, table, data) for a token: 3.1 us.  Narrow rows leave most of a block's threads without a
+// task and are bound by the blocks' chains: 32768 rows of 12 heads of 64, 101 MB, take 50 us, 131072 rows of 10 heads of 32, 168 MB, 166.
 #include "paged.cuh"
 #include <math.h>
 
@@ -225,6 +226,7 @@ __global__ void __launch_bounds__(THREADS, BATCH == 1 ? 12 : 1) k_append_rotary(
   turn_row<T, BATCH>(t, turn, position, a.g.d, cs);
 }
 
+// (by 976 and 8192 rows of 48 heads)
 bool many_rows(int64_t n) { return n > 10 * current_sm_count(); }
 
 int turn_check(int head_dim, int rot_dim, float magnitude, const double* freq) {

@@ -17,10 +17,16 @@
 // next step if that was fewer than K.  A list that overflows (ever rising logits), or whose K best are no better than a mask, makes the CTA
 // read its part again, a slower way: warps keep their K best in order, one per lane.  Entries are 64-bit numbers that order as (value, token)
 // do, so that an entry's place is the count of those above it; the cluster's first CTA joins the others' lists and sums.
-// What bounds it: 2048 rows over 128256 bf16 tokens, 525 MB, take 95 us without best tokens (5.5 TB/s; 7 instructions per logit keep the
-// schedulers busy 60 %), 110 with one and 134 with 10 (with a quarter of the tokens banned in one piece 143 and 179, with all but 0.1 %
-// 150 and 183, with 70 % strewn 169 and 188), where a CTA's few barriers and a warp's looks at reached bounds cost more than the
-// maxima.  One row over 128256 fp32 tokens with 10 best ones 9.2 us: launch, two steps, a cut and the cluster's join.
+// w / s and log2 s are at most some 20 (a thread's base is its first step's maximum, until a step passes it by some 17): as fp32 quotient and sum
+// that leaves an entropy off by 2e-6 at the worst, besides what the terms' own roundings make.
+// Given tokens with rows of their own (a tree's) are looked for by every row's first CTA, rows x n_tokens reads: 2048 tokens of 2048 rows 4 us,
+// 32768 tokens 85.
+// What bounds it: 2048 rows over 128256 bf16 tokens, 525 MB, take 93 to 95 us without best tokens (5.5 TB/s), 110 with one and 134 with 10 (with
+// a quarter of the tokens banned in one piece 143 and 179, with all but 0.1 % 150 and 183, with 70 % strewn 169 and 188), where a CTA's few
+// barriers and a warp's looks at reached bounds cost more than the maxima.  Nothing is full by the counters: with the best one DRAM 55 %, the
+// exponentials' pipe 60 %, 2.4 instructions of 4 a cycle; the last of 4.6 waves of CTAs is two thirds full.  1024 rows over as many fp32 tokens,
+// the same bytes: 80 us (6.5 TB/s), 85 with one, 93 with 10.  One row over 128256 fp32 tokens with 10 best ones 9.2 us: launch, two steps, a
+// cut and the cluster's join.
 #include "paged.cuh"
 #include <atomic>
 #include <cooperative_groups.h>
@@ -154,7 +160,7 @@ struct Stream {
       w1 = fma2(ev, v, w1);
     }
     const float gs = (s0.x + s0.y) + (s1.x + s1.y), gw = (w0.x + w0.y) + (w1.x + w1.y);
-    if (!(gs + fabsf(gw) < 0x1p21f)) return false;        // (NaN, or logits some 2^16 above the base: t is no longer exact enough)
+    if (!(gs + fabsf(gw) < 0x1p21f)) return false;        // (NaN, or a logit some 17 above the base in units of log2)
     s += gs;
     w += gw;
     return true;
