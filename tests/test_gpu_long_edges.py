@@ -108,6 +108,26 @@ def test_a_lost_load_of_the_weights_alone_raises_the_status(heads, d):
     assert torch.equal(bits(run_mass(c, mass.cuda(), w)), bits(out)) and int(c.gpu_status) == 0
 
 
+@pytest.mark.parametrize("hkv,d,page", [(2, 128, 16), (20, 64, 1)])
+def test_commit_in_bf16_takes_the_weights_along(hkv, d, page):
+    """Paths of every length up to the longest, across pages; more heads than a block has warps."""
+    c = Case(99, BF, 2 * hkv, hkv, d, page, [15, 0, 100], 40)
+    mass, _ = mass_case(c, 6)
+    path, acc = np.zeros((3, 17), np.int32), [16, 1, 0]
+    path[0, 1:17] = [1, 2, 4, 5, 7, 9, 12, 13, 17, 20, 22, 30, 31, 33, 38, 39]
+    path[1, 1] = 39
+    a, b, gm = c.pages.cuda(), c.pages.cuda(), mass.cuda()
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    n1 = lib().poss_pages_compact(a, cu(c.tables), i32(c.prefix), cu(path), i32(acc))
+    n2 = lib().poss_pages_compact(b, cu(c.tables), i32(c.prefix), cu(path), i32(acc), mass=gm, status=status)
+    assert torch.equal(a, b) and n1.cpu().tolist() == n2.cpu().tolist() == [32, 2, 101] and int(status) == 0
+    want = mass.clone()
+    for i in range(3):
+        for k in range(1, acc[i] + 1):
+            want[:, i, :, c.prefix[i] + k] = mass[:, i, :, c.prefix[i] + int(path[i, k])]
+    assert torch.equal(gm.cpu(), want)
+
+
 # ------------------------------------------------------------------ eviction
 @pytest.mark.parametrize("kind", ["ties", "equal", "random", "rising"])
 def test_eviction_of_long_sequences(kind):
